@@ -415,6 +415,107 @@ int tl_sp_ag_attention(tl_ctx* ctx, const void* q, const void* const* k_shards /
 int tl_attn_query(const tl_ctx* ctx, int S, int heads, int head_dim, int causal, int* info /*host, 8 ints*/);
 
 /*
+ * Serving from a paged key/value cache: what stands between the projection that makes queries, keys and values (tl_ag_gemm) and
+ * the one behind the attention (tl_gemm_rs) in a step of a serving loop.  Four calls, once per step or once per layer:
+ *   tl_paged_slots         (per step)   block tables, slots, positions and row offsets of the batch, from the requests' lengths
+ *   tl_paged_schedule      (per step)   the attention's work table (dynamic mapping: filled on the device at run time)
+ *   tl_qk_norm_rope_cache  (per layer)  norms and rotation of the heads, keys and values into the cache
+ *   tl_paged_attention     (per layer)  attention of the new tokens over the cached keys
+ * No call reads a length on the host: a step can be captured into a HIP graph and replayed with other lengths.
+ *
+ * Cache: k_cache and v_cache hold n_pages pages of page_size tokens, bf16; the row of token r of page p and key head h starts at
+ * element p*page_stride + (h*page_size + r)*head_dim.  A token's slot is p*page_size + r.  Nothing is read from a page that no
+ * table lists, and what lies behind a request's last token has no influence on any result, whatever it holds.
+ */
+typedef struct tl_paged_dims {
+  int batch;                 /* requests: rows of block_table, at most 4096 */
+  int max_tokens;            /* rows of q, slots, positions, ...: new tokens of all requests together at most, up to 2^18 */
+  int max_new;               /* new tokens of one request at most; 0 = max_tokens.  Smaller is faster: 1 for a decode step */
+  int max_blocks;            /* columns of block_table; max_blocks*page_size <= 2^28 */
+  int page_size;             /* tokens of a page: 16, 32, 64, 128 or 256 */
+  int n_pages;               /* pages of the cache; n_pages*page_size < 2^31 */
+  int heads_q, heads_kv;     /* this rank's heads; heads_kv divides heads_q (query head i reads key head i / (heads_q/heads_kv)) */
+  int head_dim;              /* 128 */
+  int window;                /* 0: a token sees every earlier one of its request and itself; w > 0: itself and the w-1 before it */
+  long long page_stride;     /* elements from a page to the next, in k_cache and in v_cache; 0 = heads_kv*page_size*head_dim */
+} tl_paged_dims;
+
+/* Sizes for `dims` (host call): bytes of `schedule` and of the attention's workspace; info[0..7] = query rows of a tile, rows up to
+ * which a request counts as few, keys per block, items of the few-row class and of the tile class per key head at most, workgroups
+ * per key head for which either class is cut, query heads per key head. */
+int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims /*host*/, size_t* schedule_bytes /*host*/, size_t* ws_bytes /*host*/,
+                   int* info /*host, 8 ints*/);
+
+/*
+ * Block tables and slot maps of a step, from the requests' lengths.  Request b has ctx_lens[b] tokens in the cache, in the first
+ * ceil(ctx_lens[b]/page_size) pages of its row of block_table, and new_lens[b] new ones (0: it takes no part).  New pages come
+ * from the free list in its order, request by request.  Enqueued on `stream`.
+ *   ctx_lens, new_lens  dev int[batch] (negative counts as 0)
+ *   free_pages          dev int[n_free]: the free list;  free_from dev int[1]: entries used before this call (NULL: none)
+ *   free_to             dev int[1] (written; NULL: not wanted): entries used after it
+ *   block_table         dev int[batch, max_blocks]: the entries of new pages are written, all others left as they are
+ *   query_start         dev int[batch+1] (written): first row of every request's new tokens, then their number
+ *   seq_lens            dev int[batch] (written): tokens of the request after the step
+ *   slots, positions    dev int[max_tokens] (written): slot and position of every new token; -1 and 0 in the rows behind the last
+ *   counts              dev int[4] (written): new tokens, pages taken, pages that the list lacked, tokens that did not fit
+ * A request gets at most max_new tokens and as many as its table has room for; tokens beyond max_tokens rows are cut off at the
+ * end.  A page that the list lacks has entry and slots -1: such a token is neither stored nor attended to (counts[2] tells).
+ * In place: seq_lens may be ctx_lens, and free_to may be free_from (a captured step then feeds itself); nothing else may overlap.
+ */
+int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* ctx_lens /*dev*/, const int* new_lens /*dev*/, const int* free_pages /*dev*/,
+                   int n_free, const int* free_from /*dev*/, int* free_to /*dev*/, int* block_table /*dev*/, int* query_start /*dev*/, int* seq_lens /*dev*/,
+                   int* slots /*dev*/, int* positions /*dev*/, int* counts /*dev*/, void* stream);
+
+/*
+ * RMS norm of every query and key head and the position rotation, in one pass, computed in fp32 and rounded once:
+ *   y = x / sqrt(mean(x^2) + eps) * weight  per head;  then for every pair (i, j) of the first rot_dim elements
+ *   (y_i, y_j) -> (y_i cos - y_j sin, y_j cos + y_i sin),  (i, j) = (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0.
+ *   q dev [T rows of heads_q*128], k dev [T rows of heads_kv*128] bf16, rows q_stride / k_stride elements apart (a packed
+ *     projection's rows can be taken where they lie); q_out, k_out likewise (written; may be q and k themselves)
+ *   q_weight, k_weight dev bf16[128], both or neither (NULL: no norm);  positions dev int[T]
+ *   cos_sin dev fp32 [max_position, rot_dim]: cosines of the rot_dim/2 angles of a position, then their sines
+ *   rot_dim a multiple of 16 up to 128; 0 = no rotation (positions and cos_sin may be NULL)
+ * A row whose position is outside [0, max_position) is left as it was.  Strides multiples of 8, pointers 16-byte aligned.
+ * Before tl_sp_ag_attention: on the local query and key shards.
+ */
+int tl_qk_norm_rope(tl_ctx* ctx, const void* q /*dev*/, long long q_stride, const void* k /*dev*/, long long k_stride, void* q_out /*dev*/,
+                    long long q_out_stride, void* k_out /*dev*/, long long k_out_stride, int T, int heads_q, int heads_kv, int head_dim,
+                    const void* q_weight /*dev*/, const void* k_weight /*dev*/, float eps, const int* positions /*dev*/, const float* cos_sin /*dev*/,
+                    int max_position, int rot_dim, int interleaved, void* stream);
+
+/* The same for the max_tokens rows of a step, with keys, and values as they are, stored in the cache at slots[row] (dev int
+ * [max_tokens], from tl_paged_slots).  A row whose slot is outside [0, n_pages*page_size), such as -1, is padding: nothing of it
+ * is written, q_out included.  Two rows with one slot leave either's key and value there. */
+int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const void* q /*dev*/, long long q_stride, const void* k /*dev*/,
+                          long long k_stride, const void* v /*dev*/, long long v_stride, void* q_out /*dev*/, long long q_out_stride, void* k_cache /*dev*/,
+                          void* v_cache /*dev*/, const int* slots /*dev*/, const void* q_weight /*dev*/, const void* k_weight /*dev*/, float eps,
+                          const int* positions /*dev*/, const float* cos_sin /*dev*/, int max_position, int rot_dim, int interleaved, void* stream);
+
+/* The work table of tl_paged_attention, from query_start [batch+1] and seq_lens [batch] (dev; as tl_paged_slots writes them): the
+ * requests' query tiles, and the runs into which long key axes are cut so that all compute units have work.  It serves every
+ * layer of the step that has the same dims; under other dims the attention finds no work in it and writes nothing.
+ *   schedule dev, schedule_bytes of tl_paged_query, 16-byte aligned (written).  Enqueued on `stream`. */
+int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* query_start /*dev*/, const int* seq_lens /*dev*/, int* schedule /*dev*/,
+                      size_t schedule_bytes, void* stream);
+
+/*
+ * Attention of every request's new tokens over its keys in the cache, the new ones included (they are stored first):
+ *   o[t,i,:] = bf16( sum_j softmax_j( scale * q[t,i,:] . K[j,h,:] ) V[j,h,:] ),  h = i / (heads_q/heads_kv),  j the positions that
+ *   the token sees: not after its own, inside the window, on pages that exist (entries of block_table outside [0, n_pages) do not).
+ * fp32 scores, statistics and accumulation, probabilities rounded to bf16 before they multiply V.  A token that sees nothing has
+ * o = 0 and lse = -inf.  A key or value that a token does not see has no influence on it, infinities and NaN included.
+ *   q dev [max_tokens rows of heads_q*128] bf16, q_stride elements apart;  o likewise (written; rows behind the last request are
+ *     left as they were);  lse dev fp32 [max_tokens, heads_q] (written; NULL: not wanted): log of the sum of exponentials
+ *   block_table dev int[batch, max_blocks];  schedule from tl_paged_schedule with the same dims
+ *   workspace dev, ws_bytes of tl_paged_query, 16-byte aligned: partial results of cut key axes, nothing is kept in it; one call at
+ *     a time (calls and graphs that follow each other may share it)
+ * Deterministic.  Strides multiples of 8, pointers 16-byte aligned.  Enqueued on `stream`.
+ */
+int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const void* q /*dev*/, long long q_stride, const void* k_cache /*dev*/,
+                       const void* v_cache /*dev*/, const int* block_table /*dev*/, const int* schedule /*dev*/, void* o /*dev*/, long long o_stride,
+                       float* lse /*dev*/, float scale, void* workspace /*dev*/, size_t ws_bytes, void* stream);
+
+/*
  * Schedule dump for bit-exact checks (host call, no GPU work).  Writes int records in schedule order
  * (position p is taken by persistent workgroup p % G in its round p / G):
  *   TL_OP_AG_GEMM : 8 ints per consumer tile: tile_id, bm, bn, row_lo, row_hi, chan_lo, chan_hi, 0

@@ -41,6 +41,12 @@ class tl_config(ctypes.Structure):
                 ("rs_direct_push", ctypes.c_int), ("ag_k_chunks", ctypes.c_int), ("link_gbps", ctypes.c_int)]
 
 
+class tl_paged_dims(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("max_tokens", ctypes.c_int), ("max_new", ctypes.c_int), ("max_blocks", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int), ("heads_q", ctypes.c_int), ("heads_kv", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("window", ctypes.c_int), ("page_stride", ctypes.c_longlong)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it first (python -c 'import __graft_entry__ as g; g.build()' "
                       "or python paper_2503_20313_amd/build.py). There is no CPU fallback.")
@@ -78,6 +84,14 @@ _lib.tl_sp_ag_attention.argtypes = [_vp, _vp, ctypes.POINTER(_vp), ctypes.POINTE
                                     _vp, _vp]
 _lib.tl_attn_query.restype = _i
 _lib.tl_attn_query.argtypes = [_vp, _i, _i, _i, _i, ctypes.POINTER(_i)]
+
+_dp, _ll, _f = ctypes.POINTER(tl_paged_dims), ctypes.c_longlong, ctypes.c_float
+_lib.tl_paged_query.argtypes = [_vp, _dp, ctypes.POINTER(_sz), ctypes.POINTER(_sz), ctypes.POINTER(_i)]
+_lib.tl_paged_slots.argtypes = [_vp, _dp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.tl_paged_schedule.argtypes = [_vp, _dp, _vp, _vp, _vp, _sz, _vp]
+_lib.tl_paged_attention.argtypes = [_vp, _dp, _vp, _ll, _vp, _vp, _vp, _vp, _vp, _ll, _vp, _f, _vp, _sz, _vp]
+_lib.tl_qk_norm_rope.argtypes = [_vp, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _i, _i, _vp, _vp, _f, _vp, _vp, _i, _i, _i, _vp]
+_lib.tl_qk_norm_rope_cache.argtypes = [_vp, _dp, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _vp, _vp, _vp, _f, _vp, _vp, _i, _i, _i, _vp]
 
 
 def _ptr(x):
@@ -275,3 +289,43 @@ def tl_sp_ag_attention(ctx, q, k_shards, v_shards, k_gathered, v_gathered, o, S,
     _check(_lib.tl_sp_ag_attention(ctx, _ptr(q), _ptr_array(k_shards), _ptr_array(v_shards), _ptr(k_gathered), _ptr(v_gathered), _ptr(o), S, heads,
                                    head_dim, int(causal), float(scale), _ptr(flags), epoch, _ptr(workspace), ws_bytes, _stream(compute_stream),
                                    _stream(comm_stream)))
+
+
+def _paged(dims):
+    return None if dims is None else ctypes.byref(dims)
+
+
+def tl_paged_query(ctx, dims):
+    sched, ws, info = _sz(), _sz(), (_i * 8)()
+    _check(_lib.tl_paged_query(ctx, _paged(dims), ctypes.byref(sched), ctypes.byref(ws), info))
+    keys = ("tile_rows", "few_rows", "block_keys", "few_items", "tile_items", "few_runs", "tile_runs", "group")
+    return dict(zip(keys, list(info)), schedule_bytes=sched.value, ws_bytes=ws.value)
+
+
+def tl_paged_slots(ctx, dims, ctx_lens, new_lens, free_pages, n_free, free_from, free_to, block_table, query_start, seq_lens, slots, positions, counts,
+                   stream=None):
+    _check(_lib.tl_paged_slots(ctx, _paged(dims), _ptr(ctx_lens), _ptr(new_lens), _ptr(free_pages), n_free, _ptr(free_from), _ptr(free_to), _ptr(block_table),
+                               _ptr(query_start), _ptr(seq_lens), _ptr(slots), _ptr(positions), _ptr(counts), _stream(stream)))
+
+
+def tl_qk_norm_rope(ctx, q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride, T, heads_q, heads_kv, head_dim, q_weight, k_weight, eps, positions,
+                    cos_sin, max_position, rot_dim, interleaved, stream=None):
+    _check(_lib.tl_qk_norm_rope(ctx, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, T, heads_q, heads_kv, head_dim,
+                                _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), _ptr(cos_sin), max_position, rot_dim, int(interleaved),
+                                _stream(stream)))
+
+
+def tl_qk_norm_rope_cache(ctx, dims, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, k_cache, v_cache, slots, q_weight, k_weight, eps, positions,
+                          cos_sin, max_position, rot_dim, interleaved, stream=None):
+    _check(_lib.tl_qk_norm_rope_cache(ctx, _paged(dims), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_out), q_out_stride, _ptr(k_cache),
+                                      _ptr(v_cache), _ptr(slots), _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), _ptr(cos_sin), max_position,
+                                      rot_dim, int(interleaved), _stream(stream)))
+
+
+def tl_paged_schedule(ctx, dims, query_start, seq_lens, schedule, schedule_bytes, stream=None):
+    _check(_lib.tl_paged_schedule(ctx, _paged(dims), _ptr(query_start), _ptr(seq_lens), _ptr(schedule), schedule_bytes, _stream(stream)))
+
+
+def tl_paged_attention(ctx, dims, q, q_stride, k_cache, v_cache, block_table, schedule, o, o_stride, lse, scale, workspace, ws_bytes, stream=None):
+    _check(_lib.tl_paged_attention(ctx, _paged(dims), _ptr(q), q_stride, _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(schedule), _ptr(o), o_stride,
+                                   _ptr(lse), float(scale), _ptr(workspace), ws_bytes, _stream(stream)))

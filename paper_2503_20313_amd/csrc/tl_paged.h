@@ -1,0 +1,43 @@
+// Geometry of the paged-cache operators: what the host resolves from tl_paged_dims and the kernels are given.
+#pragma once
+#include "tl_host.h"
+
+namespace tl {
+
+constexpr int kPagedD = 128;          // head_dim
+constexpr int kMaxBatch = 4096;       // the planning kernels keep a few words per request in LDS
+constexpr int kBlk = 64;              // keys per block: the unit in which the schedule cuts the key axis
+constexpr int kTileRows = 256;        // query rows (token-major, the query heads of a key head side by side) of a tile
+constexpr int kFewRows = 32;          // requests with at most so many rows per key head go to the few-row kernel, one tile each
+
+// Schedule: a header of 16 ints -- dims key, items of the few-row class, items of the tile class -- then the items of both classes.
+constexpr int kSchedHeader = 16;
+// An item is a tile, or a run of its key blocks: request, first token row, tokens, sequence length, tile, first and end key block,
+// first partial slot of the tile, index of the run, runs of the tile, 0, 0.
+constexpr int kItemInts = 12;
+
+struct PagedGeom {
+  int B, T, max_new, max_blocks, page, page_shift, n_pages, Hq, Hk, G, window;
+  long page_stride;        // elements
+  int rt;                  // row tiles of 16 in the few-row kernel (0: that class is empty)
+  int has_tiles;           // requests with more than kFewRows rows may occur
+  int cap_few, cap_tile;   // items per key head at most
+  int run_few, run_tile;   // workgroups per key head the key axis is cut for
+  int rows_few, rows_tile; // rows of a partial result
+  unsigned key;            // of all of the above: a schedule serves only the dims it was made for
+};
+
+int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g);
+
+// Last check before a launch: a real context, and its device is the current one (the stream belongs to that device).
+inline int check_paged_launch(const tl_ctx* ctx, const char* what) {
+  if (int e = check_op_ctx(ctx)) return e;
+  int dev = -1;
+  TL_HIP(hipGetDevice(&dev));
+  if (dev != ctx->device) return fail(TL_ERR_INVALID_ARG, "%s: the context was created on device %d, the current device is %d", what, ctx->device, dev);
+  return TL_OK;
+}
+
+inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+}  // namespace tl

@@ -1,0 +1,1135 @@
+// A paged key/value cache and the attention that reads it: block tables and slot maps from request lengths, the attention's work
+// table, and attention of a chunk of new tokens per request over its cached keys.  gfx950 only, head_dim 128.
+//
+// Cache: page p, key head h, row r at p * page_stride + (h * page_size + r) * 128 elements, so the rows of a page and head are one
+// contiguous piece (4 KiB for the smallest page) and 16 keys never straddle pages.
+#include "tl_gemm_tile.h"
+#include "tl_host.h"
+#include "tl_paged.h"
+#include "tl_softmax.h"
+
+namespace tl {
+
+typedef short short8_t __attribute__((ext_vector_type(8)));
+
+// ======================================================================================
+// Block tables and slot maps.  Two scans over the requests (tokens, then new pages), done by every workgroup for itself in LDS;
+// then a thread per token finds its request by binary search, and a thread per new page writes its table entry.
+// Where several workgroups share the work, what may be written in place (lengths, the head of the free list) is left to a second
+// launch of one workgroup (PART 2), so that no workgroup's inputs change under it.
+// ======================================================================================
+constexpr int kSlotThreads = 1024;
+constexpr int kSlotWaves = kSlotThreads / 64;
+constexpr int kReqPerThread = kMaxBatch / kSlotThreads;
+
+struct SlotsParams {
+  const int *ctx_lens, *new_lens, *free_pages, *free_from;
+  int n_free;
+  int *free_to, *block_table, *query_start, *seq_lens, *slots, *positions, *counts;
+  int B, T, max_new, max_blocks, page, page_shift, n_pages;
+};
+
+// Inclusive scan over the workgroup's threads; *total = the sum.  All threads call it.
+__device__ __forceinline__ int block_scan(int v, int* s_wave, int* total) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  __syncthreads();   // (s_wave may still be read by the previous scan)
+  if (lane == 63) s_wave[wave] = v;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSlotWaves; w++) {
+    const int x = s_wave[w];
+    if (w < wave) before += x;
+    all += x;
+  }
+  *total = all;
+  return v + before;
+}
+
+// The largest i in [0, n) with a[i] <= x, for a[0] <= x and ascending a: of equal entries the last, so empty requests are passed over.
+__device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+template <int PART>  // 0: everything (one workgroup); 1: maps and tables; 2: lengths and counts (one workgroup)
+__global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsParams p) {
+  __shared__ int s_wave[kSlotWaves];
+  __shared__ int s_start[kMaxBatch + 1], s_page[kMaxBatch + 1], s_ctx[kMaxBatch];
+  const int tid = threadIdx.x;
+  const int per = (p.B + kSlotThreads - 1) / kSlotThreads, b0 = tid * per;   // a thread's requests: b0 .. b0 + per - 1
+  const int cap = p.max_blocks * p.page;
+  int len[kReqPerThread];
+  int sum = 0, asked = 0;
+#pragma unroll
+  for (int i = 0; i < kReqPerThread; i++) {
+    len[i] = 0;
+    if (i < per && b0 + i < p.B) {
+      const int c = min(max(p.ctx_lens[b0 + i], 0), cap), want = min(max(p.new_lens[b0 + i], 0), 1 << 18);
+      s_ctx[b0 + i] = c;
+      len[i] = min(min(want, p.max_new), cap - c);
+      sum += len[i];             // (at most 2^12 * 2^18: the sums fit)
+      asked += want - len[i];
+    }
+  }
+  int all_tokens, all_pages, over;
+  int at = block_scan(sum, s_wave, &all_tokens) - sum;
+  // tokens that do not fit the rows are cut off at the end
+  int pages = 0;
+#pragma unroll
+  for (int i = 0; i < kReqPerThread; i++)
+    if (i < per && b0 + i < p.B) {
+      const int lo = min(at, p.T), hi = min(at + len[i], p.T);
+      asked += len[i] - (hi - lo);
+      at += len[i];
+      s_start[b0 + i] = lo;
+      len[i] = hi - lo;
+      const int c = s_ctx[b0 + i];
+      pages += ((c + len[i] + p.page - 1) >> p.page_shift) - ((c + p.page - 1) >> p.page_shift);
+    }
+  int pg = block_scan(pages, s_wave, &all_pages) - pages;
+#pragma unroll
+  for (int i = 0; i < kReqPerThread; i++)
+    if (i < per && b0 + i < p.B) {
+      const int c = s_ctx[b0 + i];
+      s_page[b0 + i] = pg;
+      pg += ((c + len[i] + p.page - 1) >> p.page_shift) - ((c + p.page - 1) >> p.page_shift);
+    }
+  const int n_tokens = min(all_tokens, p.T);
+  const int from = p.free_from ? max(p.free_from[0], 0) : 0;
+  const int left = max(p.n_free - from, 0);          // pages that the list still holds
+  if (PART != 1) block_scan(asked, s_wave, &over);
+  if (tid == 0) { s_start[p.B] = n_tokens; s_page[p.B] = all_pages; }
+  __syncthreads();   // every input that may be written in place has been read
+  if (PART != 2) {
+    const int step = gridDim.x * kSlotThreads;
+    for (int i = blockIdx.x * kSlotThreads + tid; i < all_pages; i += step) {
+      const int b = last_at_most(s_page, p.B, i);
+      const int j = ((s_ctx[b] + p.page - 1) >> p.page_shift) + i - s_page[b];
+      p.block_table[(long)b * p.max_blocks + j] = i < left ? p.free_pages[from + i] : -1;
+    }
+    for (int t = blockIdx.x * kSlotThreads + tid; t < p.T; t += step) {
+      int slot = -1, pos = 0;
+      if (t < n_tokens) {
+        const int b = last_at_most(s_start, p.B, t);
+        const int c = s_ctx[b], have = (c + p.page - 1) >> p.page_shift;
+        pos = c + t - s_start[b];
+        const int blk = pos >> p.page_shift;
+        int page;
+        if (blk < have) page = p.block_table[(long)b * p.max_blocks + blk];   // the partly filled page of the cached tokens
+        else {
+          const int i = s_page[b] + blk - have;
+          page = i < left ? p.free_pages[from + i] : -1;
+        }
+        if ((unsigned)page < (unsigned)p.n_pages) slot = (page << p.page_shift) + (pos & (p.page - 1));
+      }
+      p.slots[t] = slot;
+      p.positions[t] = pos;
+    }
+  }
+  if (PART != 1) {
+    for (int b = tid; b <= p.B; b += kSlotThreads) {
+      p.query_start[b] = s_start[b];
+      if (b < p.B) p.seq_lens[b] = s_ctx[b] + s_start[b + 1] - s_start[b];
+    }
+    if (tid == 0) {
+      const int taken = min(all_pages, left);
+      if (p.free_to) p.free_to[0] = from + taken;
+      p.counts[0] = n_tokens;
+      p.counts[1] = taken;
+      p.counts[2] = all_pages - taken;
+      p.counts[3] = over;
+    }
+  }
+}
+
+// ======================================================================================
+// Schedule: the attention's work table.  A tile is kTileRows query rows of one request (all of a request's rows, if they are at
+// most kFewRows); its keys are the blocks its rows can see.  Tiles whose key axis is longer than `chunk` blocks are cut into runs,
+// joined afterwards; chunk = the work divided by the workgroups there are, or a little more where that makes everything
+// run side by side.  Items of a request stand with the longest tiles first.
+// ======================================================================================
+struct SchedParams {
+  const int *query_start, *seq_lens;
+  int* out;
+  PagedGeom g;
+};
+
+constexpr int kMinChunkFew = 4, kMinChunkTile = 8;   // blocks of a run at least
+constexpr int kChunks = 8;                            // chunk lengths tried
+
+struct Request { int q0, n, seq; };
+
+// A request as the caller's arrays describe it, kept inside the rows and the table whatever they hold.
+__device__ __forceinline__ Request request_of(const SchedParams& p, int b) {
+  const PagedGeom& g = p.g;
+  Request r;
+  r.q0 = min(max(p.query_start[b], 0), g.T);
+  r.n = min(min(max(p.query_start[b + 1], 0), g.T) - r.q0, g.max_new);
+  r.n = max(r.n, 0);
+  r.seq = min(max(p.seq_lens[b], 0), g.max_blocks * g.page);
+  return r;
+}
+
+// Key blocks that rows [tile*rows, +rows) of a request see.
+__device__ __forceinline__ void tile_span(const PagedGeom& g, const Request& r, int tile, int rows, int* lo, int* hi) {
+  const int t0 = tile * rows / g.G, t1 = min((tile * rows + rows - 1) / g.G, r.n - 1);
+  const int end = max(r.seq - r.n + t1 + 1, 0);
+  const int start = g.window ? max(r.seq - r.n + t0 - g.window + 1, 0) : 0;
+  *hi = (end + kBlk - 1) / kBlk;
+  *lo = min(start / kBlk, *hi);
+}
+
+__global__ void __launch_bounds__(kSlotThreads) paged_schedule_kernel(const SchedParams p) {
+  const PagedGeom& g = p.g;
+  __shared__ int s_wave[kSlotWaves];
+  __shared__ int s_first[kMaxBatch + 1];     // tiles of the requests before this one
+  __shared__ unsigned long long s_work;
+  __shared__ int s_runs[kChunks];
+  __shared__ unsigned char s_off[kMaxBatch];  // requests left out: starts that do not ascend could make more tiles than there is room for
+  const int tid = threadIdx.x;
+  const int per = (g.B + kSlotThreads - 1) / kSlotThreads, b0 = tid * per;
+  {
+    int mine = 0, total;
+    for (int i = 0; i < per && b0 + i < g.B; i++) mine += request_of(p, b0 + i).n;      // (at most 2^12 * 2^18)
+    int at = block_scan(mine, s_wave, &total) - mine;
+    for (int i = 0; i < per && b0 + i < g.B; i++) {
+      at += request_of(p, b0 + i).n;
+      s_off[b0 + i] = at > g.T;
+    }
+    __syncthreads();
+  }
+  for (int cls = 0; cls < 2; cls++) {
+    const bool few = cls == 0;
+    const int cap = few ? g.cap_few : g.cap_tile;
+    int* items = p.out + kSchedHeader + (few ? 0 : (long)g.cap_few * kItemInts);
+    int n_items = 0;
+    if (cap > 0) {
+      const int rows = few ? kFewRows : kTileRows, wgs = few ? g.run_few : g.run_tile;
+      auto tiles_of = [&](int b) -> int {
+        const Request r = request_of(p, b);
+        if (s_off[b]) return 0;
+        const long rr = (long)r.n * g.G;
+        const bool is_few = g.rt > 0 && rr <= kFewRows;
+        if (few) return is_few && r.n > 0 ? 1 : 0;
+        return is_few ? 0 : (int)((rr + kTileRows - 1) / kTileRows);
+      };
+      int mine = 0, n_tiles;
+      for (int i = 0; i < per && b0 + i < g.B; i++) mine += tiles_of(b0 + i);
+      int at = block_scan(mine, s_wave, &n_tiles) - mine;
+      for (int i = 0; i < per && b0 + i < g.B; i++) {
+        s_first[b0 + i] = at;
+        at += tiles_of(b0 + i);
+      }
+      if (tid == 0) { s_first[g.B] = n_tiles; s_work = 0; }
+      if (tid < kChunks) s_runs[tid] = 0;
+      __syncthreads();
+      // tile number i of the class: the request's tiles from the last to the first
+      auto tile_at = [&](int i, int* b, Request* r, int* tile, int* lo, int* hi) {
+        *b = last_at_most(s_first, g.B, i);
+        *r = request_of(p, *b);
+        *tile = s_first[*b + 1] - 1 - i;
+        tile_span(g, *r, *tile, rows, lo, hi);
+      };
+      unsigned long long work = 0;
+      for (int i = tid; i < n_tiles; i += kSlotThreads) {
+        int b, tile, lo, hi;
+        Request r;
+        tile_at(i, &b, &r, &tile, &lo, &hi);
+        work += (unsigned)(hi - lo);
+      }
+#pragma unroll
+      for (int d = 32; d >= 1; d /= 2) work += __shfl_xor(work, d);
+      if ((tid & 63) == 0) atomicAdd(&s_work, work);
+      __syncthreads();
+      const int base = max((int)((s_work + wgs - 1) / wgs), few ? kMinChunkFew : kMinChunkTile);
+      int runs[kChunks];
+#pragma unroll
+      for (int j = 0; j < kChunks; j++) runs[j] = 0;
+      for (int i = tid; i < n_tiles; i += kSlotThreads) {
+        int b, tile, lo, hi;
+        Request r;
+        tile_at(i, &b, &r, &tile, &lo, &hi);
+#pragma unroll
+        for (int j = 0; j < kChunks; j++) {
+          const int c = (int)(((long)base * (kChunks + j) + kChunks - 1) / kChunks);
+          runs[j] += max((hi - lo + c - 1) / c, 1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kChunks; j++) {
+#pragma unroll
+        for (int d = 32; d >= 1; d /= 2) runs[j] += __shfl_xor(runs[j], d);
+        if ((tid & 63) == 0) atomicAdd(&s_runs[j], runs[j]);
+      }
+      __syncthreads();
+      int chunk = base;
+      for (int j = kChunks - 1; j >= 0; j--)
+        if (s_runs[j] <= wgs) chunk = (int)(((long)base * (kChunks + j) + kChunks - 1) / kChunks);
+      int slot_run = 0;
+      for (int i0 = 0; i0 < n_tiles; i0 += kSlotThreads) {
+        const int i = i0 + tid;
+        int b = 0, tile = 0, lo = 0, hi = 0, n = 0;
+        Request r = {0, 0, 0};
+        if (i < n_tiles) {
+          tile_at(i, &b, &r, &tile, &lo, &hi);
+          n = max((hi - lo + chunk - 1) / chunk, 1);
+        }
+        int total, slots_total;
+        const int to = n_items + block_scan(n, s_wave, &total) - n;
+        const int slot = slot_run + block_scan(n > 1 ? n : 0, s_wave, &slots_total) - (n > 1 ? n : 0);
+        for (int s = 0; s < n; s++) {
+          int* rec = items + (long)(to + s) * kItemInts;   // to + s < cap: see resolve_paged
+          const int k0 = lo + (int)((long)(hi - lo) * s / n), k1 = lo + (int)((long)(hi - lo) * (s + 1) / n);
+          const int v[kItemInts] = {b, r.q0, r.n, r.seq, tile, k0, k1, slot, s, n, 0, 0};
+#pragma unroll
+          for (int e = 0; e < kItemInts; e += 4) {
+            u32x4 q = {(unsigned)v[e], (unsigned)v[e + 1], (unsigned)v[e + 2], (unsigned)v[e + 3]};
+            *(u32x4*)(rec + e) = q;
+          }
+        }
+        n_items += total;
+        slot_run += slots_total;
+      }
+    }
+    if (tid == 0) p.out[1 + cls] = n_items;
+    __syncthreads();
+  }
+  if (tid == 0) p.out[0] = (int)g.key;
+}
+
+// ======================================================================================
+// Attention.
+// ======================================================================================
+struct PagedAttn {
+  PagedGeom g;
+  const bf16_t* q;
+  const bf16_t *k_cache, *v_cache;
+  const int *block_table, *schedule;
+  bf16_t* o;
+  float* lse;               // [T, Hq] or null
+  long q_stride, o_stride;
+  float scale_log2e;
+  float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, then [slot][key head][row][2]: maximum, sum
+  float *ml_few, *ml_tile;
+};
+
+struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs; };
+
+__device__ __forceinline__ Item load_item(const int* rec) {
+  Item i;
+  i.b = rec[0]; i.q0 = rec[1]; i.n = rec[2]; i.seq = rec[3]; i.tile = rec[4]; i.k0 = rec[5]; i.k1 = rec[6]; i.slot = rec[7]; i.run = rec[8]; i.runs = rec[9];
+  return i;
+}
+
+__device__ __forceinline__ bool not_finite(unsigned bits16) { return (bits16 & 0x7f80u) == 0x7f80u; }
+
+// 16 bytes of a value row whose non-finite elements became zeros; any = there were some.
+__device__ __forceinline__ u32x4 finite_only(u32x4 v, bool* any) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    if (not_finite(v[e])) { v[e] &= 0xffff0000u; *any = true; }
+    if (not_finite(v[e] >> 16)) { v[e] &= 0xffffu; *any = true; }
+  }
+  return v;
+}
+
+// Writes one quad of an output row, or of a partial result.
+__device__ __forceinline__ void store_row_quad(const PagedAttn& p, const Item& it, int head, int row, int d4, floatx4 o, float m, float l, float* part, float* ml,
+                                               int part_rows, int tile_row) {
+  if (it.runs == 1) {
+    const int token = row / p.g.G, hq = head * p.g.G + row - token * p.g.G;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;    // a row that sees nothing is zero
+    bf16x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (bf16_t)(o[e] * inv);
+    *(bf16x4*)(p.o + (long)(it.q0 + token) * p.o_stride + (long)hq * kPagedD + d4) = v;
+    if (p.lse && d4 == 0) p.lse[(long)(it.q0 + token) * p.g.Hq + hq] = l == 0.f ? -INFINITY : (m * p.scale_log2e + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  } else {
+    const long s = ((long)(it.slot + it.run) * p.g.Hk + head) * part_rows + tile_row;
+    *(floatx4*)(part + s * kPagedD + d4) = o;
+    if (d4 == 0) { ml[s * 2] = m; ml[s * 2 + 1] = l; }
+  }
+}
+
+// --------------------------------------------------------------------------------------
+// Few rows (single tokens, a handful of speculated ones): bound by reading K and V once.  A workgroup takes an item; its NW waves
+// take units of 32 keys in turn, each with an LDS ring of its own (two units of K and V, filled by direct-to-LDS loads), so a wave
+// never waits for another.  Per unit and tile of 16 rows:
+//   S^T[keys, q] = K . Q^T   (16x16x32 matrix instructions; a lane owns one query row and holds 4 keys of each half unit)
+//   online softmax           (over the lane's 8 keys and the 4 lane groups)
+//   O^T[d, q] += V^T . P^T   (P^T straight from the score registers; V^T by transposing LDS reads in the same key order)
+// The waves' results are joined in LDS at the end.
+// --------------------------------------------------------------------------------------
+constexpr int kUnit = 32;
+constexpr int kUnitBytes = 2 * kUnit * kPagedD * 2;      // K rows, V rows: 16 KiB
+
+template <int RT, int NW>
+__global__ void __launch_bounds__(NW * 64) paged_few_rows_kernel(const PagedAttn p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const PagedGeom& g = p.g;
+  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
+  if (p.schedule[0] != (int)g.key || idx >= p.schedule[1]) return;
+  const Item it = load_item(p.schedule + kSchedHeader + (long)idx * kItemInts);
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, gr = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_rows = it.n * g.G;
+  const int first_pos = it.seq - it.n;
+  const int key_end = min(it.k1 * kBlk, max(it.seq, 0)), key_begin = it.k0 * kBlk;
+  const int units = (max(key_end - key_begin, 0) + kUnit - 1) / kUnit;
+  const int n = units > wave ? (units - wave + NW - 1) / NW : 0;       // this wave's units: wave, wave + NW, ..
+
+  // ---- Q fragments and the positions of the lane's rows
+  bf16x8 qf[RT][4];
+  int pos[RT];
+#pragma unroll
+  for (int u = 0; u < RT; u++) {
+    const int row = min(u * 16 + l15, n_rows - 1);
+    const int token = row / g.G, hq = head * g.G + row - token * g.G;
+    const bf16_t* src = p.q + (long)(it.q0 + token) * p.q_stride + (long)hq * kPagedD + gr * 8;
+#pragma unroll
+    for (int s = 0; s < 4; s++) qf[u][s] = *(const bf16x8*)(src + s * 32);
+    pos[u] = first_pos + token;
+  }
+  const int reach = g.window ? g.window : 0x40000000;     // a query at pos sees keys in (pos - reach, pos]
+  // keys in [clean_lo, clean_hi) are seen by every row
+  const int clean_lo = max(first_pos + it.n - 1 - reach + 1, 0), clean_hi = first_pos + 1;
+
+  // ---- pages: lane 2i + half holds the page of half unit `half` of this wave's unit i (of the 32 units from `window0` on)
+  const int* table = p.block_table + (long)it.b * g.max_blocks;
+  auto key_of = [&](int i) __attribute__((always_inline)) { return key_begin + (wave + i * NW) * kUnit; };
+  int ent = -1;
+  auto load_pages = [&](int i0) __attribute__((always_inline)) {
+    const int key = key_of(i0 + (lane >> 1)) + (lane & 1) * 16;
+    int e = key < key_end ? table[key >> g.page_shift] : -1;
+    ent = (unsigned)e < (unsigned)g.n_pages ? e : -1;
+  };
+  const unsigned smem_u = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  char* ring = smem + wave * (2 * kUnitBytes);
+  const unsigned ring_u = smem_u + wave * (2 * kUnitBytes);
+  // LDS slot (row, pc) holds 16-byte chunk pc ^ (row % 16) of a K row, pc ^ ((row % 4) << 2) of a V row: conflict-free fragment reads
+  const int lr = lane >> 4;
+  unsigned koff[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) koff[j] = (unsigned)(lr * 256 + ((l15 ^ (4 * j + lr)) << 4));
+  const unsigned voff = (unsigned)(lr * 256 + ((l15 ^ (lr << 2)) << 4));
+  auto half_base = [&](const bf16_t* cache, int i, int half) __attribute__((always_inline)) -> const char* {
+    const int pg = max(__builtin_amdgcn_readlane(ent, ((i & 31) << 1) + half), 0);    // (a page that is none: page 0, masked)
+    const int row = (key_of(i) + half * 16) & (g.page - 1);
+    return (const char*)uniform64((unsigned long long)(cache + (long)pg * g.page_stride + ((long)head * g.page + row) * kPagedD));
+  };
+  auto issue = [&](const bf16_t* cache, int i, bool is_k) __attribute__((always_inline)) {
+    const unsigned dst = ring_u + (i & 1) * kUnitBytes + (is_k ? 0 : kUnitBytes / 2);
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      const char* base = half_base(cache, i, half);
+#pragma unroll
+      for (int j = 0; j < 4; j++) lds_load16_sbase(base + j * 1024, is_k ? koff[j] : voff, dst + half * 4096 + j * 1024);
+    }
+  };
+  auto halves_valid = [&](int i) __attribute__((always_inline)) -> int {
+    return (__builtin_amdgcn_readlane(ent, (i & 31) << 1) >= 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ent, ((i & 31) << 1) + 1) >= 0 ? 2 : 0);
+  };
+
+  // ---- LDS read offsets (within a unit)
+  const int k_rd = l15 * 256 + ((gr ^ l15) << 4);
+  const int v_r = l15 >> 2;
+  int v_rd[8];
+#pragma unroll
+  for (int dt = 0; dt < 8; dt++)
+    v_rd[dt] = kUnitBytes / 2 + (gr * 4 + v_r) * 256 + (((dt * 2 + ((lane & 2) >> 1)) ^ (v_r << 2)) << 4) + (lane & 1) * 8;
+
+  floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  floatx4 oacc[RT][8];
+  float m_run[RT], l_run[RT];
+#pragma unroll
+  for (int u = 0; u < RT; u++) {
+    m_run[u] = -INFINITY;
+    l_run[u] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; dt++) oacc[u][dt] = zero4;
+  }
+
+  int valid[2] = {0, 0};
+  if (n > 0) {
+    load_pages(0);
+    valid[0] = halves_valid(0);
+    issue(p.k_cache, 0, true);
+    issue(p.v_cache, 0, false);
+    if (n > 1) {
+      valid[1] = halves_valid(1);
+      issue(p.k_cache, 1, true);
+      issue(p.v_cache, 1, false);
+    }
+  }
+  for (int i = 0; i < n; i++) {
+    const bool more = i + 2 < n;
+    const char* st = ring + (i & 1) * kUnitBytes;
+    const int v2 = (i & 1) ? valid[1] : valid[0];
+    const int key0 = key_of(i);
+    // K of unit i has landed: newer are V of it, and K and V of the next (8 loads each)
+    if (more) wait_vmcnt<24>(); else wait_vmcnt<0>();
+    floatx4 c[RT][2];
+#pragma unroll
+    for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+      for (int s = 0; s < 4; s++) {
+        const bf16x8 kf = *(const bf16x8*)(st + hf * 4096 + (k_rd ^ (s << 6)));
+#pragma unroll
+        for (int u = 0; u < RT; u++) c[u][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u][s], s == 0 ? zero4 : c[u][hf], 0, 0, 0);
+      }
+    if (more) {
+      if (((i + 2) & 31) == 0) load_pages(i + 2);
+      const int v = halves_valid(i + 2);
+      if (i & 1) valid[1] = v; else valid[0] = v;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: their place may be filled again
+      issue(p.k_cache, i + 2, true);
+    }
+    const bool masked = key0 < clean_lo || key0 + kUnit > clean_hi || v2 != 3;
+    bf16x8 pf[RT];
+    float alpha[RT];
+    bool rescale = false;
+#pragma unroll
+    for (int u = 0; u < RT; u++) {
+      if (masked) {
+#pragma unroll
+        for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const int key = key0 + hf * 16 + gr * 4 + e;
+            if (key > pos[u] || key <= pos[u] - reach || !((v2 >> hf) & 1)) c[u][hf][e] = -INFINITY;
+          }
+      }
+      float m = m_run[u];
+#pragma unroll
+      for (int e = 0; e < 4; e++) m = fmaxf(fmaxf(m, c[u][0][e]), c[u][1][e]);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float ms = m == -INFINITY ? 0.f : m;         // nothing seen so far: every exponent below is -inf
+      alpha[u] = __builtin_amdgcn_exp2f((m_run[u] - ms) * p.scale_log2e);
+      rescale |= alpha[u] != 1.f;
+      m_run[u] = m;
+      const float mc = -ms * p.scale_log2e;
+      float sum = 0.f;
+#pragma unroll
+      for (int hf = 0; hf < 2; hf++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(c[u][hf][e], p.scale_log2e, mc));
+          pf[u][hf * 4 + e] = (bf16_t)pv;
+          sum += pv;
+        }
+      l_run[u] = l_run[u] * alpha[u] + sum;
+    }
+    if (__builtin_amdgcn_ballot_w64(rescale)) {
+#pragma unroll
+      for (int u = 0; u < RT; u++)
+#pragma unroll
+        for (int dt = 0; dt < 8; dt++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) oacc[u][dt][e] *= alpha[u];
+    }
+    if (more) wait_vmcnt<24>(); else wait_vmcnt<0>();     // V of unit i
+    // Where some row does not see some key of the unit: rows of V that nobody sees become zero, whatever they hold, and non-finite
+    // values of the others are taken out of the product (a zero weight times infinity is not zero) and added below where they are seen.
+    unsigned long long odd = 0;
+    if (masked) {
+      const int row = lane >> 1, key = key0 + row;
+      const bool seen = key < min(it.seq, key_end) && key > first_pos - reach && ((v2 >> (row >> 4)) & 1);
+      char* at = (char*)st + kUnitBytes / 2 + row * 256 + (lane & 1) * 128;
+      bool any = false;
+#pragma unroll
+      for (int c16 = 0; c16 < 8; c16++) {
+        u32x4 v = {0, 0, 0, 0};
+        if (seen) v = finite_only(*(const u32x4*)(at + c16 * 16), &any);
+        *(u32x4*)(at + c16 * 16) = v;
+      }
+      odd = __builtin_amdgcn_ballot_w64(any);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+#pragma unroll
+    for (int dt = 0; dt < 8; dt++) {
+      const short4_t lo = lds_read_tr(st + v_rd[dt]), hi = lds_read_tr(st + v_rd[dt] + 4096);
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, (short8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int u = 0; u < RT; u++) oacc[u][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u], oacc[u][dt], 0, 0, 0);
+    }
+    while (odd) {   // (rare)
+      const int r = __builtin_amdgcn_readfirstlane(__builtin_ctzll(odd)) >> 1;
+      odd &= ~(3ull << (2 * r));
+      const int key = key0 + r;
+      const int pg = __builtin_amdgcn_readfirstlane(table[key >> g.page_shift]);
+      const bf16_t* vrow = p.v_cache + (long)pg * g.page_stride + ((long)head * g.page + (key & (g.page - 1))) * kPagedD + gr * 4;
+#pragma unroll
+      for (int u = 0; u < RT; u++) {
+        float mine = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          if (e == (r >> 4) * 4 + (r & 3)) mine = (float)pf[u][e];
+        const float w = __shfl(mine, l15 + (((r >> 2) & 3) << 4));
+        const bool sees = key <= pos[u] && key > pos[u] - reach;
+#pragma unroll
+        for (int dt = 0; dt < 8; dt++) {
+          const bf16x4 v = *(const bf16x4*)(vrow + dt * 16);
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float x = (float)v[e];
+            if (sees && !(__builtin_fabsf(x) < INFINITY)) oacc[u][dt][e] += w * x;
+          }
+        }
+      }
+    }
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      issue(p.v_cache, i + 2, false);
+    }
+  }
+
+  // ---- join the waves: row maxima, then scaled rows, then their sums
+  constexpr int ROWS = RT * 16, PITCH = kPagedD + 4;
+  float* s_o = (float*)smem;                        // [NW][ROWS][PITCH]
+  float* s_ml = s_o + NW * ROWS * PITCH;            // [NW][ROWS][2]
+  static_assert((NW * ROWS * PITCH + NW * ROWS * 2) * 4 <= NW * 2 * kUnitBytes, "the join fits the rings");
+  __syncthreads();                                  // the rings are no longer read
+#pragma unroll
+  for (int u = 0; u < RT; u++) {
+    l_run[u] += __shfl_xor(l_run[u], 16);
+    l_run[u] += __shfl_xor(l_run[u], 32);
+    if (gr == 0) {
+      s_ml[(wave * ROWS + u * 16 + l15) * 2] = m_run[u];
+      s_ml[(wave * ROWS + u * 16 + l15) * 2 + 1] = l_run[u];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < RT; u++) {
+    const int row = u * 16 + l15;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; w++) m = fmaxf(m, s_ml[(w * ROWS + row) * 2]);
+    const float f = __builtin_amdgcn_exp2f((m_run[u] - (m == -INFINITY ? 0.f : m)) * p.scale_log2e);
+#pragma unroll
+    for (int dt = 0; dt < 8; dt++) {
+      floatx4 v = oacc[u][dt];
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] *= f;
+      *(floatx4*)(s_o + (wave * ROWS + row) * PITCH + dt * 16 + gr * 4) = v;
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < n_rows * 32; i += NW * 64) {
+    const int row = i >> 5, d4 = (i & 31) * 4;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; w++) m = fmaxf(m, s_ml[(w * ROWS + row) * 2]);
+    const float ms = m == -INFINITY ? 0.f : m;
+    floatx4 o = zero4;
+#pragma unroll
+    for (int w = 0; w < NW; w++) {
+      l += s_ml[(w * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f((s_ml[(w * ROWS + row) * 2] - ms) * p.scale_log2e);
+      const floatx4 v = *(const floatx4*)(s_o + (w * ROWS + row) * PITCH + d4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] += v[e];
+    }
+    store_row_quad(p, it, head, row, d4, o, m, l, p.part_few, p.ml_few, g.rows_few, row);
+  }
+}
+
+// --------------------------------------------------------------------------------------
+// Tiles of 256 rows (chunks of prompts): bound by the matrix products.  8 waves of 32 rows; blocks of 64 keys go through three LDS
+// stages filled by direct-to-LDS loads; a lane owns one query row.  Scores of block b + 1 are computed while block b goes through
+// the softmax, as in the sequence-parallel attention; here a block's rows come from up to four pages, looked up three blocks ahead.
+// --------------------------------------------------------------------------------------
+constexpr int kStageBytes = kBlk * kPagedD * 2;      // K or V rows of a block: 16 KiB
+constexpr int kTileLds = 3 * 2 * kStageBytes;
+constexpr int kTileThreads = 512;
+
+__global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAttn p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ unsigned long long s_odd[8];      // per wave: lanes that met a non-finite value
+  const PagedGeom& g = p.g;
+  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
+  if (p.schedule[0] != (int)g.key || idx >= p.schedule[2]) return;
+  const Item it = load_item(p.schedule + kSchedHeader + ((long)g.cap_few + idx) * kItemInts);
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first_pos = it.seq - it.n;
+  const int reach = g.window ? g.window : 0x40000000;
+  const int n_rows = it.n * g.G, row0 = it.tile * kTileRows;
+  const int tile_t0 = row0 / g.G, tile_t1 = min((row0 + kTileRows - 1) / g.G, it.n - 1);
+  const int key_end = max(min(first_pos + tile_t1 + 1, it.seq), 0);        // keys that some row of the tile sees: [key_lo, key_end)
+  const int key_lo = max(first_pos + tile_t0 - reach + 1, 0);
+  const int clean_lo = max(first_pos + tile_t1 - reach + 1, 0), clean_hi = first_pos + tile_t0 + 1;   // ... that every row sees
+  const int wrow0 = row0 + wave * 32;
+  const bool active = wrow0 < n_rows;
+  const int w_t0 = min(wrow0 / g.G, it.n - 1), w_t1 = min((wrow0 + 31) / g.G, it.n - 1);
+  const int w_last = active ? first_pos + w_t1 : -1;            // last key of the wave's rows
+  const int w_clean_lo = max(first_pos + w_t1 - reach + 1, 0), w_clean_hi = first_pos + w_t0 + 1;
+  const int row = min(wrow0 + l32, n_rows - 1);
+  const int token = row / g.G, hq = head * g.G + row - token * g.G;
+  const int q_pos = first_pos + token;
+
+  bf16x8 qf[8];
+  {
+    const bf16_t* src = p.q + (long)(it.q0 + token) * p.q_stride + (long)hq * kPagedD + h * 8;
+#pragma unroll
+    for (int st = 0; st < 8; st++) qf[st] = *(const bf16x8*)(src + st * 16);
+  }
+
+  // ---- pages of a block: lane l holds the page of its 16 keys number l % 4, or -1
+  const int* table = p.block_table + (long)it.b * g.max_blocks;
+  auto load_pages = [&](int blk) __attribute__((always_inline)) -> int {
+    const int key = blk * kBlk + (lane & 3) * 16;
+    return key < key_end ? table[key >> g.page_shift] : -1;
+  };
+  auto groups_valid = [&](int pg) __attribute__((always_inline)) -> int {
+    return (int)__builtin_amdgcn_ballot_w64((unsigned)pg < (unsigned)g.n_pages) & 15;
+  };
+  // ---- stage loads: a wave-wide load is 4 rows of 256 bytes; wave w issues rows 4w.. and 32 + 4w.. of K and of V.
+  // LDS slot (row, pc) holds 16-byte chunk pc ^ f(row): K: f = row % 16, V: f = (row % 4) << 2
+  const int lr = lane >> 4, pc = lane & 15;
+  const unsigned koff = (unsigned)(lr * 256 + ((pc ^ ((wave & 3) * 4 + lr)) << 4));
+  const unsigned voff = (unsigned)(lr * 256 + ((pc ^ (lr << 2)) << 4));
+  const unsigned smem_u = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
+  auto issue_block = [&](int blk, int stage, int pg) __attribute__((always_inline)) {
+    const unsigned sk = smem_u + (unsigned)__builtin_amdgcn_readfirstlane(stage) * (2 * kStageBytes);
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      int page = __builtin_amdgcn_readlane(pg, i * 2 + (wave >> 2));
+      if ((unsigned)page >= (unsigned)g.n_pages) page = 0;       // no page: any will do, its keys are masked
+      const int prow = (blk * kBlk + i * 32 + wave * 4) & (g.page - 1);
+      const long at = (long)page * g.page_stride + ((long)head * g.page + prow) * kPagedD;
+      const char* kb = (const char*)uniform64((unsigned long long)(p.k_cache + at));
+      const char* vb = (const char*)uniform64((unsigned long long)(p.v_cache + at));
+      const unsigned to = sk + (unsigned)(i * 8 + wave) * 1024;
+      lds_load16_sbase(kb, koff, to);
+      lds_load16_sbase(vb, voff, to + kStageBytes);
+    }
+  };
+
+  // ---- per-lane LDS read offsets (as in the sequence-parallel attention)
+  const int k_lane_off = l32 * 256 + ((h ^ (l32 & 15)) << 4);
+  auto kread = [&](int kb, int i) __attribute__((always_inline)) -> bf16x8 {
+    return *(const bf16x8*)(smem + (i & 1) * 32 * 256 + (kb ^ ((i >> 1) << 5)));
+  };
+  const int v_r = (lane & 15) >> 2;
+  int v_off[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; dt++) {
+    const int col = dt * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    v_off[dt] = (v_r + 4 * h) * 256 + ((col >> 3) ^ (v_r << 2)) * 16 + (col & 4) * 2;
+  }
+  auto vread = [&](const char* sv, int j) __attribute__((always_inline)) -> bf16x8 {
+    const char* pv = sv + (j >> 2) * 16 * 256 + v_off[j & 3];
+    const short4_t lo = lds_read_tr(pv), hi = lds_read_tr(pv + 8 * 256);
+    return __builtin_bit_cast(bf16x8, (short8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  floatx16 zero16;
+#pragma unroll
+  for (int e = 0; e < 16; e++) zero16[e] = 0.f;
+  floatx16 oacc[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; dt++) oacc[dt] = zero16;
+  float m_run = -INFINITY, l_run = 0.f, m_blk;
+
+  auto block_max = [&](const floatx16 (&sc)[2]) __attribute__((always_inline)) -> float {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e++) m = raw_max(raw_max(m, sc[0][e]), sc[1][e]);
+    return halves_max(m);
+  };
+  auto sees = [&](int key) __attribute__((always_inline)) -> bool { return key <= q_pos && key > q_pos - reach; };
+
+  int st_cur = 0, st_nxt = 1, st_ld = 2;
+  int ok_cur = 15, ok_nxt = 15;      // valid groups of 16 keys of blocks blk, blk + 1
+  int pg_ahead = -1;                 // pages of block blk + 2
+  const int end = it.k1;
+
+  auto block = [&](int blk, floatx16 (&c)[2], floatx16 (&n)[2]) __attribute__((always_inline)) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    int ok_ld = 15;
+    if (blk + 2 < end) {
+      ok_ld = groups_valid(pg_ahead);
+      issue_block(blk + 2, st_ld, pg_ahead);
+      pg_ahead = load_pages(blk + 3);
+    }
+    const int kv0 = blk * kBlk;
+    char* sv = smem + st_cur * 2 * kStageBytes + kStageBytes;
+    unsigned long long odd = 0;
+    const bool tile_masked = kv0 < clean_lo || kv0 + kBlk > clean_hi || ok_cur != 15;
+    if (tile_masked) {
+      // rows of V that no row of the tile sees become zero, whatever they hold; non-finite values of the others are taken out of
+      // the product (a zero weight times infinity is not zero) and added below where they are seen
+      const int r = tid >> 3, key = kv0 + r;
+      const bool seen = key < key_end && key >= key_lo && ((ok_cur >> (r >> 4)) & 1);
+      char* at = sv + r * 256 + (tid & 7) * 32;
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        u32x4 v = {0, 0, 0, 0};
+        if (seen) v = finite_only(*(const u32x4*)(at + i * 16), &any);
+        *(u32x4*)(at + i * 16) = v;
+      }
+      s_odd[wave] = __builtin_amdgcn_ballot_w64(any);   // (every lane stores the same: no branch in a loop that holds barriers)
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 8; w++) {                     // 8 lanes to a row, 8 rows to a wave
+        const unsigned long long b = uniform64(s_odd[w]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) odd |= (unsigned long long)(((b >> (8 * j)) & 255) != 0) << (8 * w + j);
+      }
+    }
+    if (kv0 <= w_last) {
+      const int kb = st_nxt * 2 * kStageBytes + k_lane_off;
+      constexpr int RD = 2, RN = RD + 1;
+      bf16x8 fr[RN];
+#pragma unroll
+      for (int i = 0; i < RD; i++) fr[i] = kread(kb, i);
+      __builtin_amdgcn_sched_barrier(0);
+      const bool need_mask = kv0 < w_clean_lo || kv0 + kBlk > w_clean_hi || ok_cur != 15;
+      if (need_mask) {
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int e = 0; e < 16; e++) {
+            const int key = kv0 + t * 32 + (e >> 2) * 8 + h * 4 + (e & 3);
+            if (!sees(key) || !((ok_cur >> (t * 2 + (e >> 3))) & 1)) c[t][e] = -INFINITY;
+          }
+        m_blk = block_max(c);
+      }
+      const float m_new = fmaxf(m_run, m_blk);
+      const float ms = m_new == -INFINITY ? 0.f : m_new;     // nothing seen so far: every exponent below is -inf
+      const float alpha = __builtin_amdgcn_exp2f((m_run - ms) * p.scale_log2e);
+      m_run = m_new;
+      const float mc = -ms * p.scale_log2e;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+          for (int e = 0; e < 16; e++) oacc[dt][e] *= alpha;
+      }
+      bf16x8 pf[4];
+      float psum = 0.f, m_part = -INFINITY, m_next = -INFINITY;
+      static_for<0, 32>([&](auto s_c) {
+        constexpr int f = decltype(s_c)::value;
+        if constexpr (f + RD < 16) fr[(f + RD) % RN] = kread(kb, f + RD);
+        else if constexpr (f + RD < 32) fr[(f + RD) % RN] = vread(sv, f + RD - 16);
+        if constexpr (f < 16) {
+          floatx16& acc = n[f & 1];
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % RN], qf[f >> 1], f < 2 ? zero16 : acc, 0, 0, 0);
+        } else {
+          constexpr int j = f - 16;
+          oacc[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % RN], pf[j >> 2], oacc[j & 3], 0, 0, 0);
+        }
+        if constexpr (f >= 18 && f < 22) {
+          constexpr int q = f - 18;
+#pragma unroll
+          for (int e = q * 4; e < q * 4 + 4; e++) m_part = raw_max3(m_part, n[0][e], n[1][e]);
+        }
+        if constexpr (f == 23) m_next = halves_max(m_part);
+        static_for<0, 32>([&](auto y_c) {
+          constexpr int y = decltype(y_c)::value;
+          if constexpr (y * 7 / 8 == f) {
+            constexpr int gq = y / 8, i = y % 8;
+            const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(c[gq >> 1][(gq & 1) * 8 + i], p.scale_log2e, mc));
+            pf[gq][i] = (bf16_t)pv;
+            psum += pv;
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      l_run = l_run * alpha + psum;
+      m_blk = m_next;
+      unsigned long long left = odd;
+      while (left) {   // (rare)
+        const int r = __builtin_ctzll(left);
+        left &= left - 1;
+        const int key = kv0 + r;
+        float mine = 0.f;
+        const int ph = (r >> 2) & 1;     // lane half that holds the key's weight, in register e of key group r / 16
+        static_for<0, 32>([&](auto y_c) {
+          constexpr int y = decltype(y_c)::value, gq = y / 8, i = y % 8;
+          if (gq == (r >> 4) && i == ((r >> 3) & 1) * 4 + (r & 3)) mine = (float)pf[gq][i];
+        });
+        float lo, hi;
+        both_halves(mine, lo, hi);
+        const float w = ph ? hi : lo;
+        const bool visible = sees(key);
+        const int pg = __builtin_amdgcn_readfirstlane(table[key >> g.page_shift]);
+        const bf16_t* vrow = p.v_cache + (long)pg * g.page_stride + ((long)head * g.page + (key & (g.page - 1))) * kPagedD + h * 4;
+#pragma unroll
+        for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; q4++) {
+            const bf16x4 v = *(const bf16x4*)(vrow + dt * 32 + q4 * 8);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const float x = (float)v[e];
+              if (visible && !(__builtin_fabsf(x) < INFINITY)) oacc[dt][q4 * 4 + e] += w * x;
+            }
+          }
+      }
+    }
+    if (odd) {
+      __syncthreads();
+          // (the next block's first barrier stands between this and its use)
+    }
+    const int st_free = st_cur;
+    st_cur = st_nxt; st_nxt = st_ld; st_ld = st_free;
+    ok_cur = ok_nxt; ok_nxt = ok_ld;
+  };
+
+  if (it.k0 < end) {
+    const int p0 = load_pages(it.k0), p1 = load_pages(it.k0 + 1);
+    pg_ahead = load_pages(it.k0 + 2);
+    ok_cur = groups_valid(p0);
+    issue_block(it.k0, 0, p0);
+    if (it.k0 + 1 < end) {
+      ok_nxt = groups_valid(p1);
+      issue_block(it.k0 + 1, 1, p1);
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+    floatx16 sa[2], sb[2];
+#pragma unroll
+    for (int i = 0; i < 16; i++)
+      sa[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kread(k_lane_off, i), qf[i >> 1], i < 2 ? zero16 : sa[i & 1], 0, 0, 0);
+    m_blk = block_max(sa);
+    for (int blk = it.k0; blk < end; blk += 2) {
+      block(blk, sa, sb);
+      if (blk + 1 < end) block(blk + 1, sb, sa);
+    }
+  }
+
+  float l_lo, l_hi;
+  both_halves(l_run, l_lo, l_hi);
+  const float l = l_lo + l_hi;
+  if (wrow0 + l32 < n_rows) {
+#pragma unroll
+    for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; q4++) {
+        const floatx4 v = {oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
+        store_row_quad(p, it, head, row, dt * 32 + q4 * 8 + h * 4, v, m_run, l, p.part_tile, p.ml_tile, g.rows_tile, wave * 32 + l32);
+      }
+  }
+}
+
+// --------------------------------------------------------------------------------------
+// Joins the runs of a tile: run r's workgroup joins a share of the tile's rows.
+// --------------------------------------------------------------------------------------
+template <bool FEW>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
+  const PagedGeom& g = p.g;
+  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
+  if (p.schedule[0] != (int)g.key || idx >= p.schedule[FEW ? 1 : 2]) return;
+  const Item it = load_item(p.schedule + kSchedHeader + ((FEW ? 0L : (long)g.cap_few) + idx) * kItemInts);
+  if (it.runs == 1) return;
+  const int rows_max = FEW ? kFewRows : kTileRows, part_rows = FEW ? g.rows_few : g.rows_tile;
+  const float* part = FEW ? p.part_few : p.part_tile;
+  const float* ml = FEW ? p.ml_few : p.ml_tile;
+  const int row0 = it.tile * rows_max, n = min(it.n * g.G - row0, rows_max);
+  const int lo = (int)((long)n * it.run / it.runs), hi = (int)((long)n * (it.run + 1) / it.runs);
+  Item whole = it;
+  whole.runs = 1;
+  for (int i = threadIdx.x + lo * 32; i < hi * 32; i += 256) {
+    const int r = i >> 5, d4 = (i & 31) * 4;
+    const long step = (long)g.Hk * part_rows, at = ((long)it.slot * g.Hk + head) * part_rows + r;
+    float m = -INFINITY;
+    for (int s = 0; s < it.runs; s++) m = fmaxf(m, ml[(at + s * step) * 2]);
+    const float ms = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < it.runs; s++) {
+      const float f = __builtin_amdgcn_exp2f((ml[(at + s * step) * 2] - ms) * p.scale_log2e);
+      l += ml[(at + s * step) * 2 + 1] * f;
+      const floatx4 v = *(const floatx4*)(part + (at + s * step) * kPagedD + d4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] += v[e] * f;
+    }
+    store_row_quad(p, whole, head, row0 + r, d4, o, m, l, nullptr, nullptr, 0, 0);
+  }
+}
+
+// ======================================================================================
+// Host side
+// ======================================================================================
+int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
+  if (int e = check_ctx(ctx)) return e;
+  if (!d) return fail(TL_ERR_INVALID_ARG, "dims must not be null");
+  if (d->batch <= 0 || d->max_tokens <= 0 || d->max_blocks <= 0 || d->n_pages <= 0 || d->heads_q <= 0 || d->heads_kv <= 0)
+    return fail(TL_ERR_INVALID_ARG, "tl_paged_dims: batch, max_tokens, max_blocks, n_pages and heads must be positive");
+  if (d->max_new < 0 || d->max_new > d->max_tokens) return fail(TL_ERR_INVALID_ARG, "tl_paged_dims: max_new=%d outside [0, max_tokens=%d]", d->max_new, d->max_tokens);
+  if (d->window < 0) return fail(TL_ERR_INVALID_ARG, "tl_paged_dims: window must not be negative");
+  if (d->batch > kMaxBatch) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: at most %d requests (batch=%d)", kMaxBatch, d->batch);
+  if (d->max_tokens > 1 << 18) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: at most %d new tokens (max_tokens=%d)", 1 << 18, d->max_tokens);
+  if (d->head_dim != kPagedD) return fail(TL_ERR_UNSUPPORTED_SHAPE, "head_dim %d is not supported (128 only)", d->head_dim);
+  if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)))
+    return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: page_size %d is not 16, 32, 64, 128 or 256", d->page_size);
+  if (d->heads_q % d->heads_kv) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: heads_kv=%d must divide heads_q=%d", d->heads_kv, d->heads_q);
+  if (d->heads_q > 1024) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: at most 1024 heads");
+  if ((long)d->n_pages * d->page_size > 0x7fffffffL) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: n_pages*page_size does not fit 32 bits");
+  if ((long)d->max_blocks * d->page_size > 1L << 28) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: a request may have at most 2^28 tokens");
+  const long dense = (long)d->heads_kv * d->page_size * kPagedD;
+  if (d->page_stride != 0 && d->page_stride < dense) return fail(TL_ERR_INVALID_ARG, "tl_paged_dims: page_stride is shorter than a page");
+  if (d->page_stride % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: page_stride must be a multiple of 8 elements");
+  memset(g, 0, sizeof *g);
+  g->B = d->batch; g->T = d->max_tokens; g->max_new = d->max_new ? d->max_new : d->max_tokens; g->max_blocks = d->max_blocks;
+  g->page = d->page_size; g->n_pages = d->n_pages; g->Hq = d->heads_q; g->Hk = d->heads_kv; g->G = d->heads_q / d->heads_kv;
+  while ((1 << g->page_shift) < g->page) g->page_shift++;
+  g->window = d->window < 1 << 29 ? d->window : 0;      // longer than any request: all of it
+  g->page_stride = d->page_stride ? (long)d->page_stride : dense;
+  // Classes.  A tile of the few-row class is a request with at most kFewRows rows; other requests make ceil(rows / kTileRows) tiles.
+  const long most_rows = (long)g->max_new * g->G, all_rows = (long)g->T * g->G;
+  g->rt = g->G > kFewRows ? 0 : (most_rows <= 16 ? 1 : 2);
+  g->has_tiles = most_rows > (g->rt ? kFewRows : 0);
+  // Runs.  chunk >= work / runs, so a tile of b > chunk blocks is cut into ceil(b / chunk) < 2 b / chunk runs: all cut tiles together
+  // make less than 2 * runs of them, and all tiles together at most tiles + runs items.
+  const int cus = ctx->num_cus;
+  g->run_few = ceil_div(cus, g->Hk);
+  g->run_tile = ceil_div(cus, g->Hk);
+  const long tiles = all_rows / kTileRows + (g->rt ? (g->B < all_rows / (kFewRows + 1) + 1 ? g->B : all_rows / (kFewRows + 1) + 1) : g->B);
+  g->cap_few = g->rt ? g->B + g->run_few : 0;
+  g->cap_tile = g->has_tiles ? (int)(tiles + g->run_tile) : 0;
+  g->rows_few = g->rt ? (int)(most_rows < kFewRows ? most_rows : kFewRows) : 0;
+  g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
+  if ((long)g->cap_tile * g->Hk > 0x7fffffffL || (long)g->cap_few * g->Hk > 0x7fffffffL)
+    return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: too many tiles for one launch");
+  unsigned key = 2166136261u;
+  const int v[] = {g->B, g->T, g->max_new, g->max_blocks, g->page, g->n_pages, g->Hq, g->Hk, g->window, cus};
+  for (int x : v) key = (key ^ (unsigned)x) * 16777619u;
+  g->key = key | 1u;                                    // a schedule that was never made is zero
+  return TL_OK;
+}
+
+struct PagedSizes { size_t schedule, ws, part_few, ml_few, part_tile, ml_tile; };
+
+static PagedSizes paged_sizes(const PagedGeom& g) {
+  PagedSizes s;
+  s.schedule = ((size_t)kSchedHeader + ((size_t)g.cap_few + g.cap_tile) * kItemInts) * 4;
+  const size_t few = (size_t)2 * g.run_few * g.Hk * g.rows_few, tile = (size_t)2 * g.run_tile * g.Hk * g.rows_tile;   // partial rows
+  s.part_few = 256;
+  s.ml_few = s.part_few + few * kPagedD * 4;
+  s.part_tile = s.ml_few + (few * 8 + 255) / 256 * 256;
+  s.ml_tile = s.part_tile + tile * kPagedD * 4;
+  s.ws = s.ml_tile + (tile * 8 + 255) / 256 * 256;
+  return s;
+}
+
+}  // namespace tl
+
+using namespace tl;
+
+extern "C" {
+
+int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims, size_t* schedule_bytes, size_t* ws_bytes, int* info) {
+  PagedGeom g;
+  if (int e = resolve_paged(ctx, dims, &g)) return e;
+  if (!schedule_bytes || !ws_bytes || !info) return fail(TL_ERR_INVALID_ARG, "tl_paged_query: null pointer argument");
+  const PagedSizes s = paged_sizes(g);
+  *schedule_bytes = s.schedule;
+  *ws_bytes = s.ws;
+  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.run_few, g.run_tile, g.G};
+  memcpy(info, v, sizeof v);
+  return TL_OK;
+}
+
+int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims, const int* ctx_lens, const int* new_lens, const int* free_pages, int n_free, const int* free_from,
+                   int* free_to, int* block_table, int* query_start, int* seq_lens, int* slots, int* positions, int* counts, void* stream) {
+  PagedGeom g;
+  if (int e = resolve_paged(ctx, dims, &g)) return e;
+  if (!ctx_lens || !new_lens || !block_table || !query_start || !seq_lens || !slots || !positions || !counts || (n_free > 0 && !free_pages))
+    return fail(TL_ERR_INVALID_ARG, "tl_paged_slots: null pointer argument");
+  if (n_free < 0) return fail(TL_ERR_INVALID_ARG, "tl_paged_slots: n_free must not be negative");
+  const void* ptrs[] = {ctx_lens, new_lens, free_pages, free_from, free_to, block_table, query_start, seq_lens, slots, positions, counts};
+  for (const void* q : ptrs)
+    if (!aligned4(q)) return fail(TL_ERR_INVALID_ARG, "tl_paged_slots: device pointers must be 4-byte aligned");
+  if (int e = check_paged_launch(ctx, "tl_paged_slots")) return e;
+  const SlotsParams p = {ctx_lens, new_lens, free_pages, free_from, n_free, free_to, block_table, query_start, seq_lens, slots, positions, counts,
+                         g.B, g.T, g.max_new, g.max_blocks, g.page, g.page_shift, g.n_pages};
+  hipStream_t s = (hipStream_t)stream;
+  const int wgs = g.T > 4 * kSlotThreads ? (g.T + 4 * kSlotThreads - 1) / (4 * kSlotThreads) : 1;
+  if (wgs == 1) hipLaunchKernelGGL(paged_slots_kernel<0>, dim3(1), dim3(kSlotThreads), 0, s, p);
+  else {
+    hipLaunchKernelGGL(paged_slots_kernel<1>, dim3(wgs), dim3(kSlotThreads), 0, s, p);
+    hipLaunchKernelGGL(paged_slots_kernel<2>, dim3(1), dim3(kSlotThreads), 0, s, p);
+  }
+  TL_HIP(hipGetLastError());
+  return TL_OK;
+}
+
+int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims, const int* query_start, const int* seq_lens, int* schedule, size_t schedule_bytes, void* stream) {
+  PagedGeom g;
+  if (int e = resolve_paged(ctx, dims, &g)) return e;
+  if (!query_start || !seq_lens || !schedule) return fail(TL_ERR_INVALID_ARG, "tl_paged_schedule: null pointer argument");
+  if (!aligned4(query_start) || !aligned4(seq_lens) || !aligned16(schedule))
+    return fail(TL_ERR_INVALID_ARG, "tl_paged_schedule: schedule must be 16-byte aligned, the lengths 4-byte aligned");
+  const PagedSizes z = paged_sizes(g);
+  if (schedule_bytes < z.schedule) return fail(TL_ERR_WORKSPACE_TOO_SMALL, "tl_paged_schedule: schedule of %zu bytes, %zu needed", schedule_bytes, z.schedule);
+  if (int e = check_paged_launch(ctx, "tl_paged_schedule")) return e;
+  const SchedParams p = {query_start, seq_lens, schedule, g};
+  hipLaunchKernelGGL(paged_schedule_kernel, dim3(1), dim3(kSlotThreads), 0, (hipStream_t)stream, p);
+  TL_HIP(hipGetLastError());
+  return TL_OK;
+}
+
+int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, long long q_stride, const void* k_cache, const void* v_cache,
+                       const int* block_table, const int* schedule, void* o, long long o_stride, float* lse, float scale, void* workspace, size_t ws_bytes,
+                       void* stream) {
+  PagedGeom g;
+  if (int e = resolve_paged(ctx, dims, &g)) return e;
+  if (!q || !k_cache || !v_cache || !block_table || !schedule || !o || !workspace) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: null pointer argument");
+  if (!(scale > 0.f) || scale > 3.0e38f) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: scale must be positive and finite");
+  if (q_stride < (long long)g.Hq * kPagedD || o_stride < (long long)g.Hq * kPagedD)
+    return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: a row stride is shorter than the row's heads");
+  if (q_stride % 8 || o_stride % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_attention: row strides must be multiples of 8 elements");
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) || !aligned16(schedule) || !aligned16(workspace))
+    return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: device pointers must be 16-byte aligned");
+  if (!aligned4(block_table) || !aligned4(lse)) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: block_table and lse must be 4-byte aligned");
+  const PagedSizes z = paged_sizes(g);
+  if (ws_bytes < z.ws) return fail(TL_ERR_WORKSPACE_TOO_SMALL, "tl_paged_attention: workspace of %zu bytes, %zu needed", ws_bytes, z.ws);
+  if (int e = check_paged_launch(ctx, "tl_paged_attention")) return e;
+  PagedAttn p;
+  memset(&p, 0, sizeof p);
+  p.g = g;
+  p.q = (const bf16_t*)q; p.k_cache = (const bf16_t*)k_cache; p.v_cache = (const bf16_t*)v_cache;
+  p.block_table = block_table; p.schedule = schedule;
+  p.o = (bf16_t*)o; p.lse = lse;
+  p.q_stride = q_stride; p.o_stride = o_stride;
+  p.scale_log2e = scale * 1.4426950408889634f;
+  char* ws = (char*)workspace;
+  p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
+  p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
+  hipStream_t s = (hipStream_t)stream;
+  constexpr int NW = 4, few_lds = NW * 2 * kUnitBytes;
+  if (g.has_tiles) {
+    TL_HIP(hipFuncSetAttribute((const void*)paged_tile_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kTileLds));
+    hipLaunchKernelGGL(paged_tile_kernel, dim3(g.cap_tile * g.Hk), dim3(kTileThreads), kTileLds, s, p);
+    TL_HIP(hipGetLastError());
+  }
+  if (g.rt) {
+    auto few = g.rt == 1 ? paged_few_rows_kernel<1, NW> : paged_few_rows_kernel<2, NW>;
+    TL_HIP(hipFuncSetAttribute((const void*)few, hipFuncAttributeMaxDynamicSharedMemorySize, few_lds));
+    hipLaunchKernelGGL(few, dim3(g.cap_few * g.Hk), dim3(NW * 64), few_lds, s, p);
+    TL_HIP(hipGetLastError());
+    hipLaunchKernelGGL(paged_join_kernel<true>, dim3(g.cap_few * g.Hk), dim3(256), 0, s, p);
+    TL_HIP(hipGetLastError());
+  }
+  if (g.has_tiles) {
+    hipLaunchKernelGGL(paged_join_kernel<false>, dim3(g.cap_tile * g.Hk), dim3(256), 0, s, p);
+    TL_HIP(hipGetLastError());
+  }
+  return TL_OK;
+}
+
+}  // extern "C"

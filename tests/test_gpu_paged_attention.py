@@ -1,0 +1,223 @@
+"""tl_paged_schedule + tl_paged_attention against the plain definition in 64 bits: lengths, head layouts, pages, windows, strides,
+missing pages, values that must not matter, long offsets, graphs and streams."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_20313_amd as tl
+from tests.paged_util import D, Batch, check_attention, ctx, dev, ints, np64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (2, 1), (4, 2), (5, 1), (8, 8), (16, 2), (16, 1), (32, 1)], ids=str)
+@pytest.mark.parametrize("page", [16, 64])
+def test_single_tokens(heads, page):
+    """One new token per request; contexts around the unit of 32 keys, the block of 64 and the page."""
+    cached = [0, 1, 14, 15, 16, 30, 31, 32, 33, 62, 63, 64, 65, 127, 128, 300]
+    b = Batch(cached, [1] * len(cached), *heads, page=page, seed=1)
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("cached", [0, 1, 17, 63, 64, 200])
+@pytest.mark.parametrize("new", [2, 5, 31, 33, 64, 65, 130])
+@pytest.mark.parametrize("heads", [(2, 2), (6, 2)], ids=str)
+def test_one_chunk(cached, new, heads):
+    b = Batch([cached], [new], *heads, page=16, seed=2)
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("heads", [(2, 1), (7, 1), (40, 1), (12, 4)], ids=str)
+@pytest.mark.parametrize("window", [0, 1, 16, 100])
+def test_mixed_batch(heads, window):
+    """Single tokens, chunks, requests without new tokens, in one call; 40 heads to a key head are too many for the few-row kernel."""
+    b = Batch([40, 0, 7, 129, 64, 500, 3], [1, 33, 0, 1, 70, 3, 2], *heads, page=32, window=window, seed=3)
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_page_sizes(page):
+    b = Batch([255, 256, 257, 20], [1, 40, 3, 1], 4, 2, page=page, seed=4)
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("heads,cached,new", [((4, 1), [6000], [1]), ((8, 8), [3000, 10], [1, 1]), ((2, 1), [5000], [40]), ((1, 1), [2500, 0], [300, 1])], ids=str)
+def test_cut_key_axis(heads, cached, new):
+    """Few rows and long contexts: the key axis is cut, the runs are joined."""
+    b = Batch(cached, new, *heads, page=16, seed=5)
+    z = b.buffers(c := ctx())
+    b.schedule_call(c)
+    torch.cuda.synchronize()
+    hdr = b.schedule[:3].tolist()
+    tl.tl_ctx_destroy(c)
+    assert hdr[1] + hdr[2] > len(cached), "this case is meant to cut the key axis"
+    assert hdr[1] <= z["few_items"] and hdr[2] <= z["tile_items"]
+    b.run()
+    check_attention(b)
+
+
+def test_tokens_without_any_key():
+    """More new tokens than the sequence has: the first ones have no position and see nothing."""
+    b = Batch([0, 0, 0], [3, 40, 1], 4, 2, seq_lens=[1, 17, 0], seed=6)
+    b.run()
+    check_attention(b)
+    assert (b.o[:2, :4 * D] == 0).all() and torch.isinf(b.lse[:2]).all()
+
+
+@pytest.mark.parametrize("new", [[1, 1], [50, 3]], ids=str)
+def test_missing_pages(new):
+    """Entries of the table that are no page: their keys are not attended to; a request with none at all gets zeros."""
+    b = Batch([100, 70], new, 8, 2, page=16, seed=7)
+    b.table[0, 1] = -1
+    b.table[0, 3] = b.n_pages
+    b.table[1, :] = -(1 << 31)
+    b.run()
+    check_attention(b)
+    assert (b.o[new[0]:new[0] + new[1], :8 * D] == 0).all()
+
+
+def test_strides():
+    """Pages that lie apart, as where the caches of several layers share a buffer."""
+    b = Batch([90, 31], [20, 1], 4, 2, page=32, page_stride=2 * 32 * D * 3 + 64, seed=8)
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [90, 1]], ids=str)
+def test_offsets_beyond_32_bits(new):
+    """A cache of which most elements lie behind 2^32."""
+    b = Batch([200, 600], new, 2, 1, page=64, page_stride=1 << 28, spare_pages=12, seed=9)
+    assert (b.n_pages - 1) * b.page_stride > 1 << 32
+    b.run()
+    check_attention(b)
+
+
+@pytest.mark.parametrize("kind", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("heads", [(2, 1), (16, 1)], ids=str)
+@pytest.mark.parametrize("window", [0, 20])
+def test_values_of_unseen_keys_do_not_matter(kind, heads, window):
+    """Infinities and NaN in keys and values of later tokens and of tokens before the window reach only the rows that see them."""
+    b = Batch([30, 5, 64], [4, 100, 2], *heads, page=16, window=window, seed=10)
+    for r, at in ((0, 32), (1, 60), (1, 61), (1, 104), (2, 65), (2, 3)):
+        b.v[int(b.table[r, at // 16]), :, at % 16, 5] = kind
+        b.v[int(b.table[r, at // 16]), :, at % 16, 100] = kind
+    b.run()
+    check_attention(b)
+    b.k[int(b.table[1, 90 // 16]), :, 90 % 16, 7] = kind
+    want = b.reference()
+    b.run()
+    o = np64(b.o[:b.rows, :b.Hq * D]).reshape(b.rows, b.Hq, D)
+    assert np.array_equal(np.isfinite(o), np.isfinite(want[0][:b.rows])) and np.array_equal(np.isnan(o), np.isnan(want[0][:b.rows]))
+
+
+def test_large_scores():
+    """Scores in the thousands, of one sign: the running maximum carries them."""
+    b = Batch([100, 10], [70, 1], 2, 1, seed=11, q_std=1.0)
+    b.qkv[:b.rows] *= 256
+    b.k.mul_(16)
+    want = b.reference()
+    b.run()
+    o = np64(b.o[:b.rows, :b.Hq * D]).reshape(b.rows, b.Hq, D)
+    # a score's fp32 error is 130 * 2^-24 of its terms' sizes (7 * 4096): 0.22 at most, the weights' ratio is off by exp(2 * 0.22)
+    # at most, which moves a weighted mean by that share of the values' spread
+    v = np.abs(np64(torch.nan_to_num(b.v.float(), nan=0.0))).max()
+    assert np.abs(o - want[0][:b.rows]).max() <= 0.56 * 2 * v and np.isfinite(o).all()
+    assert np.median(np.abs(o - want[0][:b.rows])) < 0.01
+    assert (np.abs(np64(b.lse[:b.rows]) - want[1][:b.rows]) <= 0.25 + 2.0 ** -20 * np.abs(want[1][:b.rows])).all()
+
+
+def test_same_bits_again_and_lse_is_optional():
+    b = Batch([3000, 40, 1000], [1, 100, 1], 8, 2, page=16, seed=12)
+    o, lse = (x.clone() for x in b.run())
+    o2, lse2 = b.run()
+    assert torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse, lse2)
+    o3, lse3 = b.run(lse=False)
+    assert torch.equal(o.view(torch.int16), o3.view(torch.int16)) and (lse3 == 7).all()
+
+
+def test_a_schedule_of_other_dims_is_not_used():
+    b = Batch([100, 3], [2, 1], 4, 2, seed=13)
+    c = ctx()
+    b.buffers(c)
+    b.schedule_call(c)
+    b.dims.window = 50
+    b.attention_call(c)
+    torch.cuda.synchronize()
+    assert (b.o == 7).all() and (b.lse == 7).all()
+    b.schedule.zero_()              # one that was never made
+    b.attention_call(c)
+    torch.cuda.synchronize()
+    assert (b.o == 7).all()
+    tl.tl_ctx_destroy(c)
+
+
+def test_lengths_that_make_no_sense_stay_in_bounds():
+    """Row starts that do not ascend and lengths outside the table: the schedule keeps to its room and to the rows."""
+    b = Batch([100, 3, 50], [2, 1, 40], 4, 2, seed=14, max_new=0)
+    c = ctx()
+    z = b.buffers(c)
+    b.start_d = ints([-5, b.T + 50, 0, 2 ** 31 - 1])
+    b.seq_d = ints([2 ** 31 - 1, -7, 50])
+    b.table_d.clamp_(max=b.n_pages - 1)
+    guard = torch.full((b.schedule.numel() + 4096,), -1, dtype=torch.int32, device=dev())
+    b.schedule = guard[:b.schedule.numel()]
+    b.schedule_call(c)
+    b.attention_call(c)
+    torch.cuda.synchronize()
+    assert (guard[b.schedule.numel():] == -1).all()
+    assert 0 <= int(b.schedule[1]) <= z["few_items"] and 0 <= int(b.schedule[2]) <= z["tile_items"]
+    tl.tl_ctx_destroy(c)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    """One graph of schedule and attention, replayed with other lengths, eager work and a synchronisation in between; a second
+    graph shares its workspace."""
+    b = Batch([500, 40, 333], [1, 60, 2], 8, 2, page=16, seed=15)
+    c = ctx()
+    b.buffers(c)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b.schedule_call(c, s)
+    b.attention_call(c, s)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            b.schedule_call(c, torch.cuda.current_stream())
+            b.attention_call(c, torch.cuda.current_stream())
+        graphs.append(g)
+    full = list(b.seq)
+    for cut in (0, 17, 250, 3):
+        b.seq = [max(x - cut, n) for x, n in zip(full, b.new)]
+        b.seq_d.copy_(ints(b.seq))
+        for g in graphs:
+            b.o.fill_(7)
+            b.lse.fill_(7)
+            g.replay()
+            torch.cuda.synchronize()
+            check_attention(b)
+    tl.tl_ctx_destroy(c)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    bs = [Batch([2000, 9], [1, 1], 8, 2, seed=16), Batch([300], [200], 8, 2, seed=17)]
+    c = ctx()
+    streams = [torch.cuda.Stream() for _ in bs]
+    for b in bs:
+        b.buffers(c)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for b, s in zip(bs, streams):
+            b.schedule_call(c, s)
+            b.attention_call(c, s)
+    torch.cuda.synchronize()
+    for b in bs:
+        check_attention(b)
+    tl.tl_ctx_destroy(c)
