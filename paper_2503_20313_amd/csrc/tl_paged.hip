@@ -649,13 +649,55 @@ __global__ void __launch_bounds__(NW * 64) paged_few_rows_kernel(const PagedAttn
 // stages filled by direct-to-LDS loads; a lane owns one query row.  Scores of block b + 1 are computed while block b goes through
 // the softmax, as in the sequence-parallel attention; here a block's rows come from up to four pages, looked up three blocks ahead.
 // --------------------------------------------------------------------------------------
+// The sums that the tile kernel's blocks left out: a non-finite value v of a key that only some of the tile's rows see.  Its weight is
+// positive unless the score is -inf, so it adds itself, or NaN in that case.
+__device__ __forceinline__ void add_non_finite(const PagedAttn& p, const Item& it, int head, const bf16x8 (&qf)[8], int q_pos, int reach, int key_lo, int key_end,
+                                               int clean_lo, int clean_hi, floatx16 (&oacc)[4]) {
+  const PagedGeom& g = p.g;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int* table = p.block_table + (long)it.b * g.max_blocks;
+  for (int key = max(it.k0 * kBlk, key_lo); key < min(it.k1 * kBlk, key_end); key++) {
+    const int pg = __builtin_amdgcn_readfirstlane(table[key >> g.page_shift]);
+    if ((unsigned)pg >= (unsigned)g.n_pages) continue;
+    const long at = (long)pg * g.page_stride + ((long)head * g.page + (key & (g.page - 1))) * kPagedD;
+    if (!__builtin_amdgcn_ballot_w64(not_finite(((const unsigned short*)(p.v_cache + at))[lane * 2]) | not_finite(((const unsigned short*)(p.v_cache + at))[lane * 2 + 1]))) continue;
+    const int blk = key & ~(kBlk - 1);
+    bool masked = blk < clean_lo || blk + kBlk > clean_hi;
+    for (int i = 0; i < kBlk && !masked; i += 16)      // (all before clean_hi: inside the table)
+      masked = (unsigned)__builtin_amdgcn_readfirstlane(table[(blk + i) >> g.page_shift]) >= (unsigned)g.n_pages;
+    if (!masked) continue;                             // its block was taken as it is
+    float s = 0.f;
+#pragma unroll
+    for (int st = 0; st < 8; st++) {
+      const bf16x8 k = *(const bf16x8*)(p.k_cache + at + st * 16 + h * 8);
+#pragma unroll
+      for (int e = 0; e < 8; e++) s += (float)k[e] * (float)qf[st][e];
+    }
+    float lo, hi;
+    both_halves(s, lo, hi);
+    s = lo + hi;
+    const bool visible = key <= q_pos && key > q_pos - reach;
+#pragma unroll
+    for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; q4++) {
+        const bf16x4 v = *(const bf16x4*)(p.v_cache + at + dt * 32 + q4 * 8 + h * 4);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float x = (float)v[e];
+          if (visible && !(__builtin_fabsf(x) < INFINITY)) oacc[dt][q4 * 4 + e] += s == -INFINITY ? __builtin_nanf("") : x;
+        }
+      }
+  }
+}
+
 constexpr int kStageBytes = kBlk * kPagedD * 2;      // K or V rows of a block: 16 KiB
 constexpr int kTileLds = 3 * 2 * kStageBytes;
 constexpr int kTileThreads = 512;
 
 __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  __shared__ unsigned long long s_odd[8];      // per wave: lanes that met a non-finite value
+  __shared__ unsigned long long s_odd[8];      // per wave: met values that were not finite
   const PagedGeom& g = p.g;
   const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
   if (p.schedule[0] != (int)g.key || idx >= p.schedule[2]) return;
@@ -753,6 +795,11 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
   int ok_cur = 15, ok_nxt = 15;      // valid groups of 16 keys of blocks blk, blk + 1
   int pg_ahead = -1;                 // pages of block blk + 2
   const int end = it.k1;
+  unsigned long long odd = 0;        // lanes of this wave that took a non-finite value out of a block
+  // some row of the tile does not see some key of the block
+  auto masked_for_some = [&](int blk, int ok) __attribute__((always_inline)) -> bool {
+    return blk * kBlk < clean_lo || blk * kBlk + kBlk > clean_hi || ok != 15;
+  };
 
   auto block = [&](int blk, floatx16 (&c)[2], floatx16 (&n)[2]) __attribute__((always_inline)) {
     wait_vmcnt<0>();
@@ -765,11 +812,9 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
     }
     const int kv0 = blk * kBlk;
     char* sv = smem + st_cur * 2 * kStageBytes + kStageBytes;
-    unsigned long long odd = 0;
-    const bool tile_masked = kv0 < clean_lo || kv0 + kBlk > clean_hi || ok_cur != 15;
-    if (tile_masked) {
+    if (masked_for_some(blk, ok_cur)) {
       // rows of V that no row of the tile sees become zero, whatever they hold; non-finite values of the others are taken out of
-      // the product (a zero weight times infinity is not zero) and added below where they are seen
+      // the product (a zero weight times infinity is not zero) and added at the end where they are seen
       const int r = tid >> 3, key = kv0 + r;
       const bool seen = key < key_end && key >= key_lo && ((ok_cur >> (r >> 4)) & 1);
       char* at = sv + r * 256 + (tid & 7) * 32;
@@ -780,14 +825,8 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
         if (seen) v = finite_only(*(const u32x4*)(at + i * 16), &any);
         *(u32x4*)(at + i * 16) = v;
       }
-      s_odd[wave] = __builtin_amdgcn_ballot_w64(any);   // (every lane stores the same: no branch in a loop that holds barriers)
+      odd |= __builtin_amdgcn_ballot_w64(any);
       __syncthreads();
-#pragma unroll
-      for (int w = 0; w < 8; w++) {                     // 8 lanes to a row, 8 rows to a wave
-        const unsigned long long b = uniform64(s_odd[w]);
-#pragma unroll
-        for (int j = 0; j < 8; j++) odd |= (unsigned long long)(((b >> (8 * j)) & 255) != 0) << (8 * w + j);
-      }
     }
     if (kv0 <= w_last) {
       const int kb = st_nxt * 2 * kStageBytes + k_lane_off;
@@ -850,39 +889,6 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
       });
       l_run = l_run * alpha + psum;
       m_blk = m_next;
-      unsigned long long left = odd;
-      while (left) {   // (rare)
-        const int r = __builtin_ctzll(left);
-        left &= left - 1;
-        const int key = kv0 + r;
-        float mine = 0.f;
-        const int ph = (r >> 2) & 1;     // lane half that holds the key's weight, in register e of key group r / 16
-        static_for<0, 32>([&](auto y_c) {
-          constexpr int y = decltype(y_c)::value, gq = y / 8, i = y % 8;
-          if (gq == (r >> 4) && i == ((r >> 3) & 1) * 4 + (r & 3)) mine = (float)pf[gq][i];
-        });
-        float lo, hi;
-        both_halves(mine, lo, hi);
-        const float w = ph ? hi : lo;
-        const bool visible = sees(key);
-        const int pg = __builtin_amdgcn_readfirstlane(table[key >> g.page_shift]);
-        const bf16_t* vrow = p.v_cache + (long)pg * g.page_stride + ((long)head * g.page + (key & (g.page - 1))) * kPagedD + h * 4;
-#pragma unroll
-        for (int dt = 0; dt < 4; dt++)
-#pragma unroll
-          for (int q4 = 0; q4 < 4; q4++) {
-            const bf16x4 v = *(const bf16x4*)(vrow + dt * 32 + q4 * 8);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              const float x = (float)v[e];
-              if (visible && !(__builtin_fabsf(x) < INFINITY)) oacc[dt][q4 * 4 + e] += w * x;
-            }
-          }
-      }
-    }
-    if (odd) {
-      __syncthreads();
-          // (the next block's first barrier stands between this and its use)
     }
     const int st_free = st_cur;
     st_cur = st_nxt; st_nxt = st_ld; st_ld = st_free;
@@ -910,6 +916,14 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
       if (blk + 1 < end) block(blk + 1, sb, sa);
     }
   }
+
+  // ---- (rare) the non-finite values that were taken out: each makes its column of every row that sees its key what the sum would be
+  s_odd[wave] = odd;
+  __syncthreads();
+  odd = 0;
+#pragma unroll
+  for (int w = 0; w < 8; w++) odd |= uniform64(s_odd[w]);
+  if (odd && active) add_non_finite(p, it, head, qf, q_pos, reach, key_lo, key_end, clean_lo, clean_hi, oacc);
 
   float l_lo, l_hi;
   both_halves(l_run, l_lo, l_hi);
