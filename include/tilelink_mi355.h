@@ -442,7 +442,7 @@ typedef struct tl_paged_dims {
 
 /* Sizes for `dims` (host call): bytes of `schedule` and of the attention's workspace; info[0..7] = query rows of a tile, rows up to
  * which a request counts as few, keys per block, items of the few-row class and of the tile class per key head at most, workgroups
- * per key head for which either class is cut, query heads per key head. */
+ * per key head for which long key axes are cut, max_tokens, query heads per key head. */
 int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims /*host*/, size_t* schedule_bytes /*host*/, size_t* ws_bytes /*host*/,
                    int* info /*host, 8 ints*/);
 
@@ -493,7 +493,8 @@ int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const
 
 /* The work table of tl_paged_attention, from query_start [batch+1] and seq_lens [batch] (dev; as tl_paged_slots writes them): the
  * requests' query tiles, and the runs into which long key axes are cut so that all compute units have work.  It serves every
- * layer of the step that has the same dims; under other dims the attention finds no work in it and writes nothing.
+ * layer of the step that has the same dims; under other dims the attention finds no work in it and writes nothing.  Row starts that
+ * do not ascend from 0 to max_tokens make an empty table.
  *   schedule dev, schedule_bytes of tl_paged_query, 16-byte aligned (written).  Enqueued on `stream`. */
 int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* query_start /*dev*/, const int* seq_lens /*dev*/, int* schedule /*dev*/,
                       size_t schedule_bytes, void* stream);
@@ -507,8 +508,9 @@ int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int
  *   q dev [max_tokens rows of heads_q*128] bf16, q_stride elements apart;  o likewise (written; rows behind the last request are
  *     left as they were);  lse dev fp32 [max_tokens, heads_q] (written; NULL: not wanted): log of the sum of exponentials
  *   block_table dev int[batch, max_blocks];  schedule from tl_paged_schedule with the same dims
- *   workspace dev, ws_bytes of tl_paged_query, 16-byte aligned: partial results of cut key axes, nothing is kept in it; one call at
- *     a time (calls and graphs that follow each other may share it)
+ *   workspace dev, ws_bytes of tl_paged_query, 16-byte aligned, zeroed once: counters that are zero again after every call, and
+ *     partial results of cut key axes, of which nothing is kept.  One call at a time: calls and graphs that follow each other may
+ *     share it, under any dims it is large enough for
  * Deterministic.  Strides multiples of 8, pointers 16-byte aligned.  Enqueued on `stream`.
  */
 int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const void* q /*dev*/, long long q_stride, const void* k_cache /*dev*/,

@@ -154,9 +154,13 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsPa
 
 // ======================================================================================
 // Schedule: the attention's work table.  A tile is kTileRows query rows of one request (all of a request's rows, if they are at
-// most kFewRows); its keys are the blocks its rows can see.  Tiles whose key axis is longer than `chunk` blocks are cut into runs,
-// joined afterwards; chunk = the work divided by the workgroups there are, or a little more where that makes everything
-// run side by side.  Items of a request stand with the longest tiles first.
+// most kFewRows); its keys are the blocks its rows can see.  A tile whose key axis is longer than its class's chunk is cut into
+// runs of equal length, joined afterwards.  The chunk is what every workgroup gets if the work is dealt out evenly -- a block of a tile
+// counts twice a block of few rows: 2.2 us at the matrix products' pace against 1.1 us at the cache's reading --, or up to
+// twice that where it makes all items run side by side.  Tiles of a request stand with the longest first.
+//
+// Bound by latency: one workgroup, a chain of scans.  The lengths are read once, into LDS; small batches take one wave, whose scans
+// need no barriers (B = 1: 14.5 -> 4.1 us against 1024 threads that read the lengths anew for every pass).
 // ======================================================================================
 struct SchedParams {
   const int *query_start, *seq_lens;
@@ -166,143 +170,198 @@ struct SchedParams {
 
 constexpr int kMinChunkFew = 4, kMinChunkTile = 8;   // blocks of a run at least
 constexpr int kChunks = 8;                            // chunk lengths tried
-
-struct Request { int q0, n, seq; };
-
-// A request as the caller's arrays describe it, kept inside the rows and the table whatever they hold.
-__device__ __forceinline__ Request request_of(const SchedParams& p, int b) {
-  const PagedGeom& g = p.g;
-  Request r;
-  r.q0 = min(max(p.query_start[b], 0), g.T);
-  r.n = min(min(max(p.query_start[b + 1], 0), g.T) - r.q0, g.max_new);
-  r.n = max(r.n, 0);
-  r.seq = min(max(p.seq_lens[b], 0), g.max_blocks * g.page);
-  return r;
-}
+constexpr int kTileCost = 2;                          // a tile's block against a few-row block
 
 // Key blocks that rows [tile*rows, +rows) of a request see.
-__device__ __forceinline__ void tile_span(const PagedGeom& g, const Request& r, int tile, int rows, int* lo, int* hi) {
-  const int t0 = tile * rows / g.G, t1 = min((tile * rows + rows - 1) / g.G, r.n - 1);
-  const int end = max(r.seq - r.n + t1 + 1, 0);
-  const int start = g.window ? max(r.seq - r.n + t0 - g.window + 1, 0) : 0;
+__device__ __forceinline__ void tile_span(const PagedGeom& g, int n, int seq, int tile, int rows, int* lo, int* hi) {
+  const int t0 = tile * rows / g.G, t1 = min((tile * rows + rows - 1) / g.G, n - 1);
+  const int end = max(seq - n + t1 + 1, 0);
+  const int start = g.window ? max(seq - n + t0 - g.window + 1, 0) : 0;
   *hi = (end + kBlk - 1) / kBlk;
   *lo = min(start / kBlk, *hi);
 }
 
-__global__ void __launch_bounds__(kSlotThreads) paged_schedule_kernel(const SchedParams p) {
+template <int NT>
+__global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p) {
   const PagedGeom& g = p.g;
-  __shared__ int s_wave[kSlotWaves];
-  __shared__ int s_first[kMaxBatch + 1];     // tiles of the requests before this one
+  constexpr int NW = NT / 64;
+  __shared__ int s_wave[NW], s_wave2[NW];
+  __shared__ int s_q0[kMaxBatch], s_n[kMaxBatch], s_seq[kMaxBatch];
+  __shared__ int s_first[kMaxBatch + 1];     // tiles (of the tile class) of the requests before this one
   __shared__ unsigned long long s_work;
   __shared__ int s_runs[kChunks];
-  __shared__ unsigned char s_off[kMaxBatch];  // requests left out: starts that do not ascend could make more tiles than there is room for
-  const int tid = threadIdx.x;
-  const int per = (g.B + kSlotThreads - 1) / kSlotThreads, b0 = tid * per;
-  {
-    int mine = 0, total;
-    for (int i = 0; i < per && b0 + i < g.B; i++) mine += request_of(p, b0 + i).n;      // (at most 2^12 * 2^18)
-    int at = block_scan(mine, s_wave, &total) - mine;
-    for (int i = 0; i < per && b0 + i < g.B; i++) {
-      at += request_of(p, b0 + i).n;
-      s_off[b0 + i] = at > g.T;
+  const int tid = threadIdx.x, lane = tid & 63;
+  // inclusive scan of two values over the workgroup; totals
+  auto scan2 = [&](int& v, int& w, int* tv, int* tw) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(v, d), u = __shfl_up(w, d);
+      if (lane >= d) { v += o; w += u; }
     }
+    if constexpr (NW == 1) {
+      *tv = __shfl(v, 63); *tw = __shfl(w, 63);
+    } else {
+      __syncthreads();   // (the previous scan's totals may still be read)
+      if (lane == 63) { s_wave[tid >> 6] = v; s_wave2[tid >> 6] = w; }
+      __syncthreads();
+      int before = 0, before2 = 0;
+      *tv = 0; *tw = 0;
+#pragma unroll
+      for (int i = 0; i < NW; i++) {
+        const int x = s_wave[i], y = s_wave2[i];
+        if (i < (tid >> 6)) { before += x; before2 += y; }
+        *tv += x; *tw += y;
+      }
+      v += before; w += before2;
+    }
+  };
+  bool bad = false;      // row starts that do not ascend inside the rows: no request can be trusted
+  for (int b = tid; b < g.B; b += NT) {
+    const int lo = p.query_start[b], hi = p.query_start[b + 1];
+    bad |= lo < 0 || hi < lo || hi > g.T;
+    s_q0[b] = lo;
+    s_n[b] = min(max(hi - lo, 0), g.max_new);
+    s_seq[b] = min(max(p.seq_lens[b], 0), g.max_blocks * g.page);
+  }
+  if (tid == 0) s_work = 0;
+  if (tid < kChunks) s_runs[tid] = 0;
+  if (__syncthreads_or(bad)) {
+    if (tid < kSchedHeader) p.out[tid] = tid == 0 ? (int)g.key : 0;
+    return;
+  }
+  auto is_few = [&](int b) { return g.rt > 0 && s_n[b] * g.G <= kFewRows; };   // (at most 2^28)
+  int n_tiles = 0;
+  if (g.has_tiles) {
+    for (int base = 0; base < g.B; base += NT) {
+      const int b = base + tid;
+      int v = b < g.B && !is_few(b) ? (s_n[b] * g.G + kTileRows - 1) / kTileRows : 0, w = 0, tv, tw;
+      const int mine = v;
+      scan2(v, w, &tv, &tw);
+      if (b < g.B) s_first[b] = n_tiles + v - mine;
+      n_tiles += tv;
+    }
+    if (tid == 0) s_first[g.B] = n_tiles;
     __syncthreads();
   }
+  // tile number i of the tile class: a request's tiles from the last to the first
+  auto tile_at = [&](int i, int* b, int* tile, int* lo, int* hi) {
+    *b = last_at_most(s_first, g.B, i);
+    *tile = s_first[*b + 1] - 1 - i;
+    tile_span(g, s_n[*b], s_seq[*b], *tile, kTileRows, lo, hi);
+  };
+  // few-row tile of request b, if it has one
+  auto few_at = [&](int b, int* lo, int* hi) -> bool {
+    if (b >= g.B || s_n[b] == 0 || !is_few(b)) return false;
+    tile_span(g, s_n[b], s_seq[b], 0, kFewRows, lo, hi);
+    return true;
+  };
+  unsigned long long work = 0;
+  for (int b = tid; b < g.B; b += NT) {
+    int lo, hi;
+    if (few_at(b, &lo, &hi)) work += (unsigned)(hi - lo);
+  }
+  for (int i = tid; i < n_tiles; i += NT) {
+    int b, tile, lo, hi;
+    tile_at(i, &b, &tile, &lo, &hi);
+    work += (unsigned)(hi - lo) * (unsigned long long)kTileCost;
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d /= 2) work += __shfl_xor(work, d);
+  if constexpr (NW > 1) {
+    if (lane == 0) atomicAdd(&s_work, work);
+    __syncthreads();
+    work = s_work;
+  }
+  const unsigned long long share = (work + g.runs - 1) / g.runs;
+  auto chunk_of = [&](int j, bool few) -> int {      // candidate j of a class
+    const unsigned long long c = (share * (kChunks + j) + kChunks - 1) / kChunks;
+    return max((int)(few ? c : (c + kTileCost - 1) / kTileCost), few ? kMinChunkFew : kMinChunkTile);
+  };
+  int cf[kChunks], ct[kChunks], runs[kChunks];
+#pragma unroll
+  for (int j = 0; j < kChunks; j++) { cf[j] = chunk_of(j, true); ct[j] = chunk_of(j, false); runs[j] = 0; }
+  for (int b = tid; b < g.B; b += NT) {
+    int lo, hi;
+    if (!few_at(b, &lo, &hi)) continue;
+#pragma unroll
+    for (int j = 0; j < kChunks; j++) runs[j] += max((int)((unsigned)(hi - lo + cf[j] - 1) / (unsigned)cf[j]), 1);
+  }
+  for (int i = tid; i < n_tiles; i += NT) {
+    int b, tile, lo, hi;
+    tile_at(i, &b, &tile, &lo, &hi);
+#pragma unroll
+    for (int j = 0; j < kChunks; j++) runs[j] += max((int)((unsigned)(hi - lo + ct[j] - 1) / (unsigned)ct[j]), 1);
+  }
+#pragma unroll
+  for (int j = 0; j < kChunks; j++) {
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) runs[j] += __shfl_xor(runs[j], d);
+    if constexpr (NW > 1) {
+      if (lane == 0) atomicAdd(&s_runs[j], runs[j]);
+    }
+  }
+  if constexpr (NW > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kChunks; j++) runs[j] = s_runs[j];
+  }
+  int chunk_few = cf[0], chunk_tile = ct[0];
+#pragma unroll
+  for (int j = kChunks - 1; j >= 0; j--)
+    if (runs[j] <= g.runs) { chunk_few = cf[j]; chunk_tile = ct[j]; }
+
+  // ---- the items of both classes, in order; every wave writes its tiles' runs lane by lane
   for (int cls = 0; cls < 2; cls++) {
     const bool few = cls == 0;
-    const int cap = few ? g.cap_few : g.cap_tile;
-    int* items = p.out + kSchedHeader + (few ? 0 : (long)g.cap_few * kItemInts);
-    int n_items = 0;
-    if (cap > 0) {
-      const int rows = few ? kFewRows : kTileRows, wgs = few ? g.run_few : g.run_tile;
-      auto tiles_of = [&](int b) -> int {
-        const Request r = request_of(p, b);
-        if (s_off[b]) return 0;
-        const long rr = (long)r.n * g.G;
-        const bool is_few = g.rt > 0 && rr <= kFewRows;
-        if (few) return is_few && r.n > 0 ? 1 : 0;
-        return is_few ? 0 : (int)((rr + kTileRows - 1) / kTileRows);
-      };
-      int mine = 0, n_tiles;
-      for (int i = 0; i < per && b0 + i < g.B; i++) mine += tiles_of(b0 + i);
-      int at = block_scan(mine, s_wave, &n_tiles) - mine;
-      for (int i = 0; i < per && b0 + i < g.B; i++) {
-        s_first[b0 + i] = at;
-        at += tiles_of(b0 + i);
+    const int n = few ? (g.rt ? g.B : 0) : n_tiles, chunk = few ? chunk_few : chunk_tile;
+    int* items = p.out + g.sched_few + (few ? 0 : (long)g.cap_few * kItemInts);
+    int n_items = 0, n_slots = 0, n_cut = 0;
+    for (int base = 0; base < n; base += NT) {
+      const int i = base + tid;
+      int b = 0, tile = 0, lo = 0, hi = 0, cnt = 0;
+      if (few) {
+        b = i;
+        if (few_at(i, &lo, &hi)) cnt = max((int)((unsigned)(hi - lo + chunk - 1) / (unsigned)chunk), 1);
+      } else if (i < n) {
+        tile_at(i, &b, &tile, &lo, &hi);
+        cnt = max((int)((unsigned)(hi - lo + chunk - 1) / (unsigned)chunk), 1);
       }
-      if (tid == 0) { s_first[g.B] = n_tiles; s_work = 0; }
-      if (tid < kChunks) s_runs[tid] = 0;
-      __syncthreads();
-      // tile number i of the class: the request's tiles from the last to the first
-      auto tile_at = [&](int i, int* b, Request* r, int* tile, int* lo, int* hi) {
-        *b = last_at_most(s_first, g.B, i);
-        *r = request_of(p, *b);
-        *tile = s_first[*b + 1] - 1 - i;
-        tile_span(g, *r, *tile, rows, lo, hi);
-      };
-      unsigned long long work = 0;
-      for (int i = tid; i < n_tiles; i += kSlotThreads) {
-        int b, tile, lo, hi;
-        Request r;
-        tile_at(i, &b, &r, &tile, &lo, &hi);
-        work += (unsigned)(hi - lo);
-      }
+      // v: items up to this tile; w: partial slots in the low 20 bits, cut tiles above them (both at most 2 * runs, far below 2^11, 2^20)
+      int v = cnt, w = cnt > 1 ? cnt + (1 << 20) : 0, tv, tw;
+      const int w0 = w;
+      scan2(v, w, &tv, &tw);
+      const int to = n_items + v - cnt, slot = n_slots + ((w - w0) & 0xfffff);
+      if (!few && cnt > 1) p.out[kSchedHeader + n_cut + ((w - w0) >> 20)] = to;
+      // the wave's runs, 64 at a time: run number r of the wave belongs to the last lane whose first run is not after it
+      const int first = v - cnt - __shfl(v - cnt, 0), all = __shfl(first + cnt, 63);
+      for (int r0 = 0; r0 < all; r0 += 64) {
+        const int r = r0 + lane;
+        int own = 0;
 #pragma unroll
-      for (int d = 32; d >= 1; d /= 2) work += __shfl_xor(work, d);
-      if ((tid & 63) == 0) atomicAdd(&s_work, work);
-      __syncthreads();
-      const int base = max((int)((s_work + wgs - 1) / wgs), few ? kMinChunkFew : kMinChunkTile);
-      int runs[kChunks];
-#pragma unroll
-      for (int j = 0; j < kChunks; j++) runs[j] = 0;
-      for (int i = tid; i < n_tiles; i += kSlotThreads) {
-        int b, tile, lo, hi;
-        Request r;
-        tile_at(i, &b, &r, &tile, &lo, &hi);
-#pragma unroll
-        for (int j = 0; j < kChunks; j++) {
-          const int c = (int)(((long)base * (kChunks + j) + kChunks - 1) / kChunks);
-          runs[j] += max((hi - lo + c - 1) / c, 1);
+        for (int d = 32; d >= 1; d /= 2) {
+          const int f = __shfl(first, own + d > 63 ? 63 : own + d);
+          if (own + d <= 63 && f <= r) own += d;
+        }
+        const int ob = __shfl(b, own), ot = __shfl(tile, own), olo = __shfl(lo, own), ohi = __shfl(hi, own), oc = __shfl(cnt, own), oto = __shfl(to, own);
+        const int oslot = __shfl(slot, own), s = r - __shfl(first, own);
+        if (r < all) {
+          int* rec = items + (long)(oto + s) * kItemInts;       // (oto + s is below the class's cap: see resolve_paged)
+          const u32x4 q0 = {(unsigned)ob, (unsigned)s_q0[ob], (unsigned)s_n[ob], (unsigned)s_seq[ob]};
+          const u32x4 q1 = {(unsigned)ot, (unsigned)(olo + (int)((long)(ohi - olo) * s / oc)), (unsigned)(olo + (int)((long)(ohi - olo) * (s + 1) / oc)), (unsigned)oslot};
+          const u32x4 q2 = {(unsigned)s, (unsigned)oc, 0, 0};
+          *(u32x4*)rec = q0;
+          *(u32x4*)(rec + 4) = q1;
+          *(u32x4*)(rec + 8) = q2;
         }
       }
-#pragma unroll
-      for (int j = 0; j < kChunks; j++) {
-#pragma unroll
-        for (int d = 32; d >= 1; d /= 2) runs[j] += __shfl_xor(runs[j], d);
-        if ((tid & 63) == 0) atomicAdd(&s_runs[j], runs[j]);
-      }
-      __syncthreads();
-      int chunk = base;
-      for (int j = kChunks - 1; j >= 0; j--)
-        if (s_runs[j] <= wgs) chunk = (int)(((long)base * (kChunks + j) + kChunks - 1) / kChunks);
-      int slot_run = 0;
-      for (int i0 = 0; i0 < n_tiles; i0 += kSlotThreads) {
-        const int i = i0 + tid;
-        int b = 0, tile = 0, lo = 0, hi = 0, n = 0;
-        Request r = {0, 0, 0};
-        if (i < n_tiles) {
-          tile_at(i, &b, &r, &tile, &lo, &hi);
-          n = max((hi - lo + chunk - 1) / chunk, 1);
-        }
-        int total, slots_total;
-        const int to = n_items + block_scan(n, s_wave, &total) - n;
-        const int slot = slot_run + block_scan(n > 1 ? n : 0, s_wave, &slots_total) - (n > 1 ? n : 0);
-        for (int s = 0; s < n; s++) {
-          int* rec = items + (long)(to + s) * kItemInts;   // to + s < cap: see resolve_paged
-          const int k0 = lo + (int)((long)(hi - lo) * s / n), k1 = lo + (int)((long)(hi - lo) * (s + 1) / n);
-          const int v[kItemInts] = {b, r.q0, r.n, r.seq, tile, k0, k1, slot, s, n, 0, 0};
-#pragma unroll
-          for (int e = 0; e < kItemInts; e += 4) {
-            u32x4 q = {(unsigned)v[e], (unsigned)v[e + 1], (unsigned)v[e + 2], (unsigned)v[e + 3]};
-            *(u32x4*)(rec + e) = q;
-          }
-        }
-        n_items += total;
-        slot_run += slots_total;
-      }
+      n_items += tv;
+      n_slots += tw & 0xfffff;
+      n_cut += tw >> 20;
     }
-    if (tid == 0) p.out[1 + cls] = n_items;
-    __syncthreads();
+    if (tid == 0) {
+      p.out[1 + cls] = n_items;
+      if (!few) p.out[3] = n_cut;
+    }
   }
   if (tid == 0) p.out[0] = (int)g.key;
 }
@@ -319,8 +378,9 @@ struct PagedAttn {
   float* lse;               // [T, Hq] or null
   long q_stride, o_stride;
   float scale_log2e;
-  float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, then [slot][key head][row][2]: maximum, sum
+  float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, and [slot][key head][row][2]: maximum, sum
   float *ml_few, *ml_tile;
+  unsigned *arrived;               // few-row class: per (slot, key head) runs of a group that have arrived, then groups of a tile; zero between calls
 };
 
 struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs; };
@@ -343,22 +403,48 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v, bool* any) {
   return v;
 }
 
-// Writes one quad of an output row, or of a partial result.
-__device__ __forceinline__ void store_row_quad(const PagedAttn& p, const Item& it, int head, int row, int d4, floatx4 o, float m, float l, float* part, float* ml,
-                                               int part_rows, int tile_row) {
-  if (it.runs == 1) {
-    const int token = row / p.g.G, hq = head * p.g.G + row - token * p.g.G;
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;    // a row that sees nothing is zero
-    bf16x4 v;
+// One quad of an output row.
+__device__ __forceinline__ void store_out(const PagedAttn& p, const Item& it, int head, int row, int d4, floatx4 o, float m, float l) {
+  const int token = row / p.g.G, hq = head * p.g.G + row - token * p.g.G;
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;    // a row that sees nothing is zero
+  bf16x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; e++) v[e] = (bf16_t)(o[e] * inv);
-    *(bf16x4*)(p.o + (long)(it.q0 + token) * p.o_stride + (long)hq * kPagedD + d4) = v;
-    if (p.lse && d4 == 0) p.lse[(long)(it.q0 + token) * p.g.Hq + hq] = l == 0.f ? -INFINITY : (m * p.scale_log2e + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  } else {
-    const long s = ((long)(it.slot + it.run) * p.g.Hk + head) * part_rows + tile_row;
-    *(floatx4*)(part + s * kPagedD + d4) = o;
-    if (d4 == 0) { ml[s * 2] = m; ml[s * 2 + 1] = l; }
+  for (int e = 0; e < 4; e++) v[e] = (bf16_t)(o[e] * inv);
+  *(bf16x4*)(p.o + (long)(it.q0 + token) * p.o_stride + (long)hq * kPagedD + d4) = v;
+  if (p.lse && d4 == 0) p.lse[(long)(it.q0 + token) * p.g.Hq + hq] = l == 0.f ? -INFINITY : (m * p.scale_log2e + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// Sum of up to N partial results of one quad of a row, `step` rows apart, in order: all loads in flight together.
+template <int N>
+__device__ __forceinline__ void join_quad(const float* part, const float* ml, long at, long step, int count, int d4, float scale_log2e, floatx4* o, float* m, float* l) {
+  floatx4 v[N];
+  float mm[N], ll[N];
+#pragma unroll
+  for (int s = 0; s < N; s++) {
+    mm[s] = -INFINITY; ll[s] = 0.f;
+    v[s] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (s < count) {
+      mm[s] = ml[(at + s * step) * 2];
+      ll[s] = ml[(at + s * step) * 2 + 1];
+      v[s] = *(const floatx4*)(part + (at + s * step) * kPagedD + d4);
+    }
   }
+  float top = *m;
+#pragma unroll
+  for (int s = 0; s < N; s++) top = fmaxf(top, mm[s]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  const float f0 = __builtin_amdgcn_exp2f((*m - ref) * scale_log2e);
+  *l *= f0;
+#pragma unroll
+  for (int e = 0; e < 4; e++) (*o)[e] *= f0;
+#pragma unroll
+  for (int s = 0; s < N; s++) {
+    const float f = __builtin_amdgcn_exp2f((mm[s] - ref) * scale_log2e);
+    *l += ll[s] * f;
+#pragma unroll
+    for (int e = 0; e < 4; e++) (*o)[e] += v[s][e] * f;
+  }
+  *m = top;
 }
 
 // --------------------------------------------------------------------------------------
@@ -373,13 +459,11 @@ __device__ __forceinline__ void store_row_quad(const PagedAttn& p, const Item& i
 constexpr int kUnit = 32;
 constexpr int kUnitBytes = 2 * kUnit * kPagedD * 2;      // K rows, V rows: 16 KiB
 
+constexpr int kJoin = 16;                                // runs that one workgroup joins at a time
+
 template <int RT, int NW>
-__global__ void __launch_bounds__(NW * 64) paged_few_rows_kernel(const PagedAttn p) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
+__device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it, int head, char* smem) {
   const PagedGeom& g = p.g;
-  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
-  if (p.schedule[0] != (int)g.key || idx >= p.schedule[1]) return;
-  const Item it = load_item(p.schedule + kSchedHeader + (long)idx * kItemInts);
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, gr = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_rows = it.n * g.G;
@@ -640,7 +724,59 @@ __global__ void __launch_bounds__(NW * 64) paged_few_rows_kernel(const PagedAttn
 #pragma unroll
       for (int e = 0; e < 4; e++) o[e] += v[e];
     }
-    store_row_quad(p, it, head, row, d4, o, m, l, p.part_few, p.ml_few, g.rows_few, row);
+    if (it.runs == 1) store_out(p, it, head, row, d4, o, m, l);
+    else {
+      const long at = ((long)(it.slot + it.run) * g.Hk + head) * g.rows_few + row;
+      store16_device_scope(p.part_few + at * kPagedD + d4, __builtin_bit_cast(u32x4, o));
+      if (d4 == 0) {
+        __hip_atomic_store(p.ml_few + at * 2, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p.ml_few + at * 2 + 1, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+  }
+  if (it.runs == 1) return;
+  // ---- join the runs: the last of every kJoin runs to arrive joins them into the first one's place, the last group to arrive
+  // joins the groups (of one group: into the output).  Always in the order of the runs, so the result does not depend on who is last.
+  int* s_last = (int*)(s_ml + NW * ROWS * 2);
+  const int groups = (it.runs + kJoin - 1) / kJoin;
+#pragma unroll
+  for (int level = 0; level < 2; level++) {
+    const int first = level == 0 ? it.run & ~(kJoin - 1) : 0, stride = level == 0 ? 1 : kJoin;
+    const int count = level == 0 ? min(kJoin, it.runs - first) : groups;
+    unsigned* cnt = p.arrived + ((long)(it.slot + first) * g.Hk + head) * 2 + level;
+    wait_all_vmem();                                // this wave's part is where every die sees it
+    __syncthreads();
+    if (tid == 0) {
+      const unsigned before = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *s_last = before + 1 == (unsigned)count;
+      if (*s_last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!*s_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    const bool whole = level == 1 || groups == 1;
+    const long step = (long)g.Hk * g.rows_few * stride;
+    for (int i = tid; i < (n_rows * 32 + NW * 64 - 1) / (NW * 64) * (NW * 64); i += NW * 64) {   // (whole rounds: the barrier below)
+      const int row = i >> 5, d4 = (i & 31) * 4;
+      const long at = ((long)(it.slot + first) * g.Hk + head) * g.rows_few + row;
+      floatx4 o = zero4;
+      float m = -INFINITY, l = 0.f;
+      if (row < n_rows)
+        for (int s = 0; s < count; s += kJoin) join_quad<kJoin>(p.part_few, p.ml_few, at + s * step, step, min(count - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
+      if (whole) {
+        if (row < n_rows) store_out(p, it, head, row, d4, o, m, l);
+      } else {
+        __syncthreads();                            // the row's maximum and sum have been read by all its quads
+        if (row < n_rows) {
+          store16_device_scope(p.part_few + at * kPagedD + d4, __builtin_bit_cast(u32x4, o));
+          if (d4 == 0) {
+            __hip_atomic_store(p.ml_few + at * 2, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(p.ml_few + at * 2 + 1, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          }
+        }
+      }
+    }
+    if (whole) return;
   }
 }
 
@@ -695,13 +831,9 @@ constexpr int kStageBytes = kBlk * kPagedD * 2;      // K or V rows of a block: 
 constexpr int kTileLds = 3 * 2 * kStageBytes;
 constexpr int kTileThreads = 512;
 
-__global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAttn p) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
+__device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, int head, char* smem) {
   __shared__ unsigned long long s_odd[8];      // per wave: met values that were not finite
   const PagedGeom& g = p.g;
-  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
-  if (p.schedule[0] != (int)g.key || idx >= p.schedule[2]) return;
-  const Item it = load_item(p.schedule + kSchedHeader + ((long)g.cap_few + idx) * kItemInts);
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int first_pos = it.seq - it.n;
@@ -934,44 +1066,66 @@ __global__ void __launch_bounds__(kTileThreads) paged_tile_kernel(const PagedAtt
 #pragma unroll
       for (int q4 = 0; q4 < 4; q4++) {
         const floatx4 v = {oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
-        store_row_quad(p, it, head, row, dt * 32 + q4 * 8 + h * 4, v, m_run, l, p.part_tile, p.ml_tile, g.rows_tile, wave * 32 + l32);
+        const int d4 = dt * 32 + q4 * 8 + h * 4;
+        if (it.runs == 1) store_out(p, it, head, row, d4, v, m_run, l);
+        else {
+          const long at = ((long)(it.slot + it.run) * g.Hk + head) * g.rows_tile + wave * 32 + l32;
+          *(floatx4*)(p.part_tile + at * kPagedD + d4) = v;
+          if (d4 == 0) { p.ml_tile[at * 2] = m_run; p.ml_tile[at * 2 + 1] = l; }
+        }
       }
   }
 }
 
 // --------------------------------------------------------------------------------------
-// Joins the runs of a tile: run r's workgroup joins a share of the tile's rows.
+// Kernels.  A batch that can only have few rows per request (a decode step) takes the first; else one launch holds the items of both
+// classes, tiles first, so that single tokens run beside the chunks; a few-row item then uses four of the eight waves.
 // --------------------------------------------------------------------------------------
-template <bool FEW>
+constexpr int kFewWaves = 4;
+constexpr int kFewLds = kFewWaves * 2 * kUnitBytes;
+static_assert(kTileLds <= kFewLds, "one launch, one size");
+
+template <int RT>
+__global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const PagedAttn p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
+  if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
+  few_rows_item<RT, kFewWaves>(p, load_item(p.schedule + p.g.sched_few + (long)idx * kItemInts), head, smem);
+}
+
+template <bool FEW>    // FEW: the batch may have few-row items
+__global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAttn p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
+  if (p.schedule[0] != (int)p.g.key) return;
+  const int tiles = p.schedule[2];
+  const int* few = p.schedule + p.g.sched_few;
+  if (idx < tiles) tile_item(p, load_item(few + ((long)p.g.cap_few + idx) * kItemInts), head, smem);
+  else if (FEW && idx - tiles < p.schedule[1] && threadIdx.x < kFewWaves * 64)
+    few_rows_item<2, kFewWaves>(p, load_item(few + (long)(idx - tiles) * kItemInts), head, smem);
+}
+
+// Joins the runs of the cut tiles, 32 rows of a tile and key head at a time (256 KiB of partial results from two runs up: all workgroups share
+// them, where a tile's last run alone would read them at one compute unit's pace).
+constexpr int kJoinRows = 32;
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
   const PagedGeom& g = p.g;
-  const int idx = blockIdx.x / g.Hk, head = blockIdx.x - idx * g.Hk;
-  if (p.schedule[0] != (int)g.key || idx >= p.schedule[FEW ? 1 : 2]) return;
-  const Item it = load_item(p.schedule + kSchedHeader + ((FEW ? 0L : (long)g.cap_few) + idx) * kItemInts);
-  if (it.runs == 1) return;
-  const int rows_max = FEW ? kFewRows : kTileRows, part_rows = FEW ? g.rows_few : g.rows_tile;
-  const float* part = FEW ? p.part_few : p.part_tile;
-  const float* ml = FEW ? p.ml_few : p.ml_tile;
-  const int row0 = it.tile * rows_max, n = min(it.n * g.G - row0, rows_max);
-  const int lo = (int)((long)n * it.run / it.runs), hi = (int)((long)n * (it.run + 1) / it.runs);
-  Item whole = it;
-  whole.runs = 1;
-  for (int i = threadIdx.x + lo * 32; i < hi * 32; i += 256) {
-    const int r = i >> 5, d4 = (i & 31) * 4;
-    const long step = (long)g.Hk * part_rows, at = ((long)it.slot * g.Hk + head) * part_rows + r;
-    float m = -INFINITY;
-    for (int s = 0; s < it.runs; s++) m = fmaxf(m, ml[(at + s * step) * 2]);
-    const float ms = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < it.runs; s++) {
-      const float f = __builtin_amdgcn_exp2f((ml[(at + s * step) * 2] - ms) * p.scale_log2e);
-      l += ml[(at + s * step) * 2 + 1] * f;
-      const floatx4 v = *(const floatx4*)(part + (at + s * step) * kPagedD + d4);
-#pragma unroll
-      for (int e = 0; e < 4; e++) o[e] += v[e] * f;
+  if (p.schedule[0] != (int)g.key) return;
+  const int parts = (g.rows_tile + kJoinRows - 1) / kJoinRows, jobs = p.schedule[3] * g.Hk * parts;
+  for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts, r0 = (rest - head * parts) * kJoinRows;
+    const Item it = load_item(p.schedule + g.sched_few + ((long)g.cap_few + p.schedule[kSchedHeader + cut]) * kItemInts);
+    const int row0 = it.tile * kTileRows, n = min(it.n * g.G - row0, kTileRows);
+    const long step = (long)g.Hk * g.rows_tile;
+    for (int i = threadIdx.x; i < kJoinRows * 32; i += 256) {
+      const int r = r0 + (i >> 5), d4 = (i & 31) * 4;
+      if (r >= n) break;
+      const long at = ((long)it.slot * g.Hk + head) * g.rows_tile + r;
+      floatx4 o = {0.f, 0.f, 0.f, 0.f};
+      float m = -INFINITY, l = 0.f;
+      for (int s = 0; s < it.runs; s += 8) join_quad<8>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, 8), d4, p.scale_log2e, &o, &m, &l);
+      store_out(p, it, head, row0 + r, d4, o, m, l);
     }
-    store_row_quad(p, whole, head, row0 + r, d4, o, m, l, nullptr, nullptr, 0, 0);
   }
 }
 
@@ -1007,17 +1161,17 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   const long most_rows = (long)g->max_new * g->G, all_rows = (long)g->T * g->G;
   g->rt = g->G > kFewRows ? 0 : (most_rows <= 16 ? 1 : 2);
   g->has_tiles = most_rows > (g->rt ? kFewRows : 0);
-  // Runs.  chunk >= work / runs, so a tile of b > chunk blocks is cut into ceil(b / chunk) < 2 b / chunk runs: all cut tiles together
-  // make less than 2 * runs of them, and all tiles together at most tiles + runs items.
-  const int cus = ctx->num_cus;
-  g->run_few = ceil_div(cus, g->Hk);
-  g->run_tile = ceil_div(cus, g->Hk);
+  // Runs.  chunk >= the class's work / runs, so a tile of b > chunk blocks is cut into ceil(b / chunk) < 2 b / chunk runs: all cut tiles
+  // together make less than 2 * runs of them (so there are fewer than `runs`), and all tiles together at most tiles + runs items.
+  const int cus = ctx->num_cus < 1024 ? ctx->num_cus : 1024;
+  g->runs = ceil_div(cus, g->Hk);
+  g->sched_few = kSchedHeader + (g->runs + 3) / 4 * 4;
   const long tiles = all_rows / kTileRows + (g->rt ? (g->B < all_rows / (kFewRows + 1) + 1 ? g->B : all_rows / (kFewRows + 1) + 1) : g->B);
-  g->cap_few = g->rt ? g->B + g->run_few : 0;
-  g->cap_tile = g->has_tiles ? (int)(tiles + g->run_tile) : 0;
+  g->cap_few = g->rt ? g->B + g->runs : 0;
+  g->cap_tile = g->has_tiles ? (int)(tiles + g->runs) : 0;
   g->rows_few = g->rt ? (int)(most_rows < kFewRows ? most_rows : kFewRows) : 0;
   g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
-  if ((long)g->cap_tile * g->Hk > 0x7fffffffL || (long)g->cap_few * g->Hk > 0x7fffffffL)
+  if (((long)g->cap_tile + g->cap_few) * g->Hk > 0x7fffffffL)
     return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: too many tiles for one launch");
   unsigned key = 2166136261u;
   const int v[] = {g->B, g->T, g->max_new, g->max_blocks, g->page, g->n_pages, g->Hq, g->Hk, g->window, cus};
@@ -1026,13 +1180,16 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   return TL_OK;
 }
 
+// Two counters per partial slot and key head: 2 * runs * heads_kv slots, runs = ceil(compute units / heads_kv).
+constexpr size_t kArrivedBytes = 2 * (2 * (1024 + 1024)) * 4;
+
 struct PagedSizes { size_t schedule, ws, part_few, ml_few, part_tile, ml_tile; };
 
 static PagedSizes paged_sizes(const PagedGeom& g) {
   PagedSizes s;
-  s.schedule = ((size_t)kSchedHeader + ((size_t)g.cap_few + g.cap_tile) * kItemInts) * 4;
-  const size_t few = (size_t)2 * g.run_few * g.Hk * g.rows_few, tile = (size_t)2 * g.run_tile * g.Hk * g.rows_tile;   // partial rows
-  s.part_few = 256;
+  s.schedule = ((size_t)g.sched_few + ((size_t)g.cap_few + g.cap_tile) * kItemInts) * 4;
+  const size_t few = (size_t)2 * g.runs * g.Hk * g.rows_few, tile = (size_t)2 * g.runs * g.Hk * g.rows_tile;   // partial rows
+  s.part_few = kArrivedBytes;             // (in front: the arrival counters, the same for all dims, so that calls of any may share a workspace)
   s.ml_few = s.part_few + few * kPagedD * 4;
   s.part_tile = s.ml_few + (few * 8 + 255) / 256 * 256;
   s.ml_tile = s.part_tile + tile * kPagedD * 4;
@@ -1053,7 +1210,7 @@ int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims, size_t* schedul
   const PagedSizes s = paged_sizes(g);
   *schedule_bytes = s.schedule;
   *ws_bytes = s.ws;
-  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.run_few, g.run_tile, g.G};
+  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.runs, g.T, g.G};
   memcpy(info, v, sizeof v);
   return TL_OK;
 }
@@ -1092,7 +1249,14 @@ int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims, const int* query_s
   if (schedule_bytes < z.schedule) return fail(TL_ERR_WORKSPACE_TOO_SMALL, "tl_paged_schedule: schedule of %zu bytes, %zu needed", schedule_bytes, z.schedule);
   if (int e = check_paged_launch(ctx, "tl_paged_schedule")) return e;
   const SchedParams p = {query_start, seq_lens, schedule, g};
-  hipLaunchKernelGGL(paged_schedule_kernel, dim3(1), dim3(kSlotThreads), 0, (hipStream_t)stream, p);
+  const long most = g.cap_tile > g.B ? g.cap_tile : g.B;
+  auto launch = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    hipLaunchKernelGGL(paged_schedule_kernel<NT>, dim3(1), dim3(NT), 0, (hipStream_t)stream, p);
+  };
+  if (most <= 128) launch(std::integral_constant<int, 64>{});
+  else if (most <= 512) launch(std::integral_constant<int, 256>{});
+  else launch(std::integral_constant<int, 1024>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -1122,27 +1286,20 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.q_stride = q_stride; p.o_stride = o_stride;
   p.scale_log2e = scale * 1.4426950408889634f;
   char* ws = (char*)workspace;
+  p.arrived = (unsigned*)ws;
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
   p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
   hipStream_t s = (hipStream_t)stream;
-  constexpr int NW = 4, few_lds = NW * 2 * kUnitBytes;
-  if (g.has_tiles) {
-    TL_HIP(hipFuncSetAttribute((const void*)paged_tile_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kTileLds));
-    hipLaunchKernelGGL(paged_tile_kernel, dim3(g.cap_tile * g.Hk), dim3(kTileThreads), kTileLds, s, p);
+  auto launch = [&](auto kernel, int grid, int threads) -> int {
+    TL_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds));
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), kFewLds, s, p);
     TL_HIP(hipGetLastError());
-  }
-  if (g.rt) {
-    auto few = g.rt == 1 ? paged_few_rows_kernel<1, NW> : paged_few_rows_kernel<2, NW>;
-    TL_HIP(hipFuncSetAttribute((const void*)few, hipFuncAttributeMaxDynamicSharedMemorySize, few_lds));
-    hipLaunchKernelGGL(few, dim3(g.cap_few * g.Hk), dim3(NW * 64), few_lds, s, p);
-    TL_HIP(hipGetLastError());
-    hipLaunchKernelGGL(paged_join_kernel<true>, dim3(g.cap_few * g.Hk), dim3(256), 0, s, p);
-    TL_HIP(hipGetLastError());
-  }
-  if (g.has_tiles) {
-    hipLaunchKernelGGL(paged_join_kernel<false>, dim3(g.cap_tile * g.Hk), dim3(256), 0, s, p);
-    TL_HIP(hipGetLastError());
-  }
+    return TL_OK;
+  };
+  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.cap_few * g.Hk, kFewWaves * 64);
+  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads)) return e;
+  hipLaunchKernelGGL(paged_join_kernel, dim3(2 * ctx->num_cus), dim3(256), 0, s, p);
+  TL_HIP(hipGetLastError());
   return TL_OK;
 }
 

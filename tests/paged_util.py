@@ -9,6 +9,7 @@ import paper_2503_20313_amd as tl
 from oracle import paged as ref
 
 D = 128
+COUNTERS = 2 * 2 * 2048          # words in front of the workspace's partial results
 SCALE = D ** -0.5
 HALF_BF16 = torch.finfo(torch.bfloat16).eps / 2       # half a step, relative
 
@@ -79,7 +80,8 @@ class Batch:
     def buffers(self, c):
         z = tl.tl_paged_query(c, self.dims)
         self.ws_bytes, self.sched_bytes = z["ws_bytes"], z["schedule_bytes"]
-        self.ws = torch.full((self.ws_bytes // 4,), float("nan"), device=dev())        # nothing of an earlier call is needed
+        self.ws = torch.zeros(self.ws_bytes // 4, device=dev())
+        self.ws[COUNTERS:] = float("nan")                                   # of the partial results nothing is needed before they are written
         self.schedule = torch.full((self.sched_bytes // 4,), -1, dtype=torch.int32, device=dev())
         self.o = torch.full((self.T, self.o_stride), 7.0, dtype=torch.bfloat16, device=dev())
         self.lse = torch.full((self.T, self.Hq), 7.0, device=dev())
@@ -101,6 +103,7 @@ class Batch:
         self.attention_call(c, s, lse)
         torch.cuda.synchronize()
         tl.tl_ctx_destroy(c)
+        assert not self.ws[:COUNTERS].view(torch.int32).any(), "a counter is not back at zero"
         return self.o, self.lse
 
 
@@ -113,15 +116,15 @@ def check_attention(b, want=None, lse=True):
     o = np64(b.o[:n, :b.Hq * D]).reshape(n, b.Hq, D)
     tol = 1.01 * (HALF_BF16 * np.abs(o_ref[:n]) + (HALF_BF16 + 2.0 ** -12) * size[:n]) + 1e-30
     fin = np.isfinite(o_ref[:n])
-    bad = np.abs(o - o_ref[:n])[fin] > tol[fin]
+    bad = np.abs(o[fin] - o_ref[:n][fin]) > tol[fin]
     assert not np.isnan(o[fin]).any(), f"{np.isnan(o[fin]).sum()} NaN where the result is finite"
-    assert not bad.any(), f"{bad.sum()} of {bad.size} elements off, worst {np.max(np.abs(o - o_ref[:n])[fin] / tol[fin]):.2f} of the tolerance"
+    assert not bad.any(), f"{bad.sum()} of {bad.size} elements off, worst {np.max(np.abs(o[fin] - o_ref[:n][fin]) / tol[fin]):.2f} of the tolerance"
     same = np.where(np.isnan(o_ref[:n]), np.isnan(o), o == o_ref[:n])
     assert same[~fin].all(), "non-finite results differ"
     if lse:
         got, w = np64(b.lse[:n]), lse_ref[:n]
         f = np.isfinite(w)
-        assert (np.abs(got - w)[f] <= 2.0 ** -11 + 2.0 ** -22 * np.abs(w[f])).all(), np.max(np.abs(got - w)[f])
+        assert (np.abs(got[f] - w[f]) <= 2.0 ** -11 + 2.0 ** -22 * np.abs(w[f])).all(), np.max(np.abs(got[f] - w[f]))
         assert (got[~f] == w[~f])[~np.isnan(w[~f])].all()
     # nothing else was written
     assert (b.o[n:] == 7).all() and (b.o[:, b.Hq * D:] == 7).all() and (b.lse[n:] == 7).all()

@@ -47,7 +47,7 @@ def test_page_sizes(page):
     check_attention(b)
 
 
-@pytest.mark.parametrize("heads,cached,new", [((4, 1), [6000], [1]), ((8, 8), [3000, 10], [1, 1]), ((2, 1), [5000], [40]), ((1, 1), [2500, 0], [300, 1])], ids=str)
+@pytest.mark.parametrize("heads,cached,new", [((4, 1), [6000], [1]), ((16, 1), [9000], [1]), ((2, 1), [20000, 300], [1, 3]), ((8, 8), [3000, 10], [1, 1]), ((2, 1), [5000], [40]), ((1, 1), [2500, 0], [300, 1])], ids=str)
 def test_cut_key_axis(heads, cached, new):
     """Few rows and long contexts: the key axis is cut, the runs are joined."""
     b = Batch(cached, new, *heads, page=16, seed=5)
