@@ -10,11 +10,10 @@ constexpr int kBlk = 64;              // keys per block: the unit in which the s
 constexpr int kTileRows = 256;        // query rows (token-major, the query heads of a key head side by side) of a tile
 constexpr int kFewRows = 32;          // requests with at most so many rows per key head go to the few-row kernel, one tile each
 
-// Schedule: a header of 16 ints -- dims key, items of the few-row class, items of the tile class, cut tiles of that class --, the cut
-// tiles' first items, then the items of both classes.
+// Schedule: a header of 16 ints -- dims key, items, cut tiles of the tile class --, the cut tiles' first items, then the items.
 constexpr int kSchedHeader = 16;
 // An item is a tile, or a run of its key blocks: request, first token row, tokens, sequence length, tile, first and end key block,
-// first partial slot of the tile, index of the run, runs of the tile, 0, 0.
+// first partial slot of the tile, index of the run, runs of the tile, 1 for few rows, 0.
 constexpr int kItemInts = 12;
 
 struct PagedGeom {
@@ -23,8 +22,8 @@ struct PagedGeom {
   int rt;                  // row tiles of 16 in the few-row kernel (0: that class is empty)
   int has_tiles;           // requests with more than kFewRows rows may occur
   int cap_few, cap_tile;   // items per key head at most
-  int runs;                // workgroups per key head, for which the key axes are cut
-  int sched_few;           // where the few-row items start in the schedule, in ints; the tile items follow
+  int side;                // items per key head that run side by side: the key axes are cut for so many
+  int sched_items;         // where the items start in the schedule, in ints
   int rows_few, rows_tile; // rows of a partial result
   unsigned key;            // of all of the above: a schedule serves only the dims it was made for
 };

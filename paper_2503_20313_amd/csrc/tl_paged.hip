@@ -155,12 +155,14 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsPa
 // ======================================================================================
 // Schedule: the attention's work table.  A tile is kTileRows query rows of one request (all of a request's rows, if they are at
 // most kFewRows); its keys are the blocks its rows can see.  A tile whose key axis is longer than its class's chunk is cut into
-// runs of equal length, joined afterwards.  The chunk is what every workgroup gets if the work is dealt out evenly -- a block of a tile
-// counts twice a block of few rows: 2.2 us at the matrix products' pace against 1.1 us at the cache's reading --, or up to
-// twice that where it makes all items run side by side.  Tiles of a request stand with the longest first.
+// runs of equal length, joined afterwards.  The chunk is an even share of the work, or up to half as much again where that lets all
+// items run side by side; the items stand in order of their length, the longest first, for the hardware to hand out.
+// Measured with every chunk from a quarter of the share to uncut, the even share is within 3 % of the best in batches that do not fit
+// side by side (64 requests of 500..8000 tokens: 188 us, at a quarter 197; in the requests' order instead of by length 222), and a
+// longer one that makes them fit is worth it up to half (128 requests of 1000..10000: 78 us against 87), not beyond.
 //
-// Bound by latency: one workgroup, a chain of scans.  The lengths are read once, into LDS; small batches take one wave, whose scans
-// need no barriers (B = 1: 14.5 -> 4.1 us against 1024 threads that read the lengths anew for every pass).
+// Bound by latency: one workgroup, a chain of passes over the requests.  The lengths are read once, into LDS; small batches take one
+// wave, whose reductions need no barriers.
 // ======================================================================================
 struct SchedParams {
   const int *query_start, *seq_lens;
@@ -168,9 +170,11 @@ struct SchedParams {
   PagedGeom g;
 };
 
-constexpr int kMinChunkFew = 4, kMinChunkTile = 8;   // blocks of a run at least
-constexpr int kChunks = 8;                            // chunk lengths tried
-constexpr int kTileCost = 2;                          // a tile's block against a few-row block
+// A block of 64 keys costs in a tile kCostTile / kCostFew of what it costs with few rows: 2.0 us against 0.75, the chip at work.
+constexpr int kCostFew = 3, kCostTile = 8;
+constexpr int kChunks = 5;                    // chunk lengths tried: an even share, and 1 .. 4 eighths of it more
+constexpr int kMinChunk = 4;                  // blocks of a run at least
+constexpr int kBuckets = 64;
 
 // Key blocks that rows [tile*rows, +rows) of a request see.
 __device__ __forceinline__ void tile_span(const PagedGeom& g, int n, int seq, int tile, int rows, int* lo, int* hi) {
@@ -181,40 +185,29 @@ __device__ __forceinline__ void tile_span(const PagedGeom& g, int n, int seq, in
   *lo = min(start / kBlk, *hi);
 }
 
+// Over the 64 lanes of a wave, in every lane: rotations inside rows of 16 lanes, then the four rows.
+template <class F>
+__device__ __forceinline__ int wave_reduce(int x, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, true));
+  return f(f(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)), f(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+
 template <int NT>
 __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p) {
   const PagedGeom& g = p.g;
   constexpr int NW = NT / 64;
-  __shared__ int s_wave[NW], s_wave2[NW];
+  __shared__ int s_wave[NW];
   __shared__ int s_q0[kMaxBatch], s_n[kMaxBatch], s_seq[kMaxBatch];
   __shared__ int s_first[kMaxBatch + 1];     // tiles (of the tile class) of the requests before this one
   __shared__ unsigned long long s_work;
-  __shared__ int s_runs[kChunks];
+  __shared__ int s_count[kChunks], s_long;
+  __shared__ int s_bucket[kBuckets], s_slots[2], s_cut;
   const int tid = threadIdx.x, lane = tid & 63;
-  // inclusive scan of two values over the workgroup; totals
-  auto scan2 = [&](int& v, int& w, int* tv, int* tw) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(v, d), u = __shfl_up(w, d);
-      if (lane >= d) { v += o; w += u; }
-    }
-    if constexpr (NW == 1) {
-      *tv = __shfl(v, 63); *tw = __shfl(w, 63);
-    } else {
-      __syncthreads();   // (the previous scan's totals may still be read)
-      if (lane == 63) { s_wave[tid >> 6] = v; s_wave2[tid >> 6] = w; }
-      __syncthreads();
-      int before = 0, before2 = 0;
-      *tv = 0; *tw = 0;
-#pragma unroll
-      for (int i = 0; i < NW; i++) {
-        const int x = s_wave[i], y = s_wave2[i];
-        if (i < (tid >> 6)) { before += x; before2 += y; }
-        *tv += x; *tw += y;
-      }
-      v += before; w += before2;
-    }
-  };
+  auto add = [](int x, int y) { return x + y; };
+  auto top = [](int x, int y) { return max(x, y); };
   bool bad = false;      // row starts that do not ascend inside the rows: no request can be trusted
   for (int b = tid; b < g.B; b += NT) {
     const int lo = p.query_start[b], hi = p.query_start[b + 1];
@@ -224,7 +217,10 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     s_seq[b] = min(max(p.seq_lens[b], 0), g.max_blocks * g.page);
   }
   if (tid == 0) s_work = 0;
-  if (tid < kChunks) s_runs[tid] = 0;
+  if (tid < kChunks) s_count[tid] = 0;
+  if (tid < kBuckets) s_bucket[tid] = 0;
+  if (tid < 2) s_slots[tid] = 0;
+  if (tid == 0) { s_cut = 0; s_long = 0; }
   if (__syncthreads_or(bad)) {
     if (tid < kSchedHeader) p.out[tid] = tid == 0 ? (int)g.key : 0;
     return;
@@ -234,36 +230,52 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   if (g.has_tiles) {
     for (int base = 0; base < g.B; base += NT) {
       const int b = base + tid;
-      int v = b < g.B && !is_few(b) ? (s_n[b] * g.G + kTileRows - 1) / kTileRows : 0, w = 0, tv, tw;
-      const int mine = v;
-      scan2(v, w, &tv, &tw);
+      const int mine = b < g.B && !is_few(b) ? (s_n[b] * g.G + kTileRows - 1) / kTileRows : 0;
+      int v = mine;      // inclusive scan
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+      }
+      int total = __shfl(v, 63);
+      if constexpr (NW > 1) {
+        __syncthreads();
+        if (lane == 63) s_wave[tid >> 6] = v;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < NW; i++) {
+          const int x = s_wave[i];
+          if (i < (tid >> 6)) v += x;
+          total += x;
+        }
+      }
       if (b < g.B) s_first[b] = n_tiles + v - mine;
-      n_tiles += tv;
+      n_tiles += total;
     }
     if (tid == 0) s_first[g.B] = n_tiles;
     __syncthreads();
   }
-  // tile number i of the tile class: a request's tiles from the last to the first
-  auto tile_at = [&](int i, int* b, int* tile, int* lo, int* hi) {
-    *b = last_at_most(s_first, g.B, i);
-    *tile = s_first[*b + 1] - 1 - i;
-    tile_span(g, s_n[*b], s_seq[*b], *tile, kTileRows, lo, hi);
-  };
-  // few-row tile of request b, if it has one
-  auto few_at = [&](int b, int* lo, int* hi) -> bool {
-    if (b >= g.B || s_n[b] == 0 || !is_few(b)) return false;
-    tile_span(g, s_n[b], s_seq[b], 0, kFewRows, lo, hi);
+  // ---- all tiles of both classes: number i is request i's few rows, if it has few, then tile number i - B of the tile class
+  const int n_all = g.B + n_tiles;
+  struct Tile { int b, tile, lo, hi; bool few; };
+  auto tile_at = [&](int i, Tile* t) -> bool {
+    t->few = i < g.B;
+    t->b = i; t->tile = 0;
+    if (t->few) {
+      if (s_n[i] == 0 || !is_few(i)) return false;
+      tile_span(g, s_n[i], s_seq[i], 0, kFewRows, &t->lo, &t->hi);
+    } else {
+      t->b = last_at_most(s_first, g.B, i - g.B);
+      t->tile = s_first[t->b + 1] - 1 - (i - g.B);
+      tile_span(g, s_n[t->b], s_seq[t->b], t->tile, kTileRows, &t->lo, &t->hi);
+    }
     return true;
   };
   unsigned long long work = 0;
-  for (int b = tid; b < g.B; b += NT) {
-    int lo, hi;
-    if (few_at(b, &lo, &hi)) work += (unsigned)(hi - lo);
-  }
-  for (int i = tid; i < n_tiles; i += NT) {
-    int b, tile, lo, hi;
-    tile_at(i, &b, &tile, &lo, &hi);
-    work += (unsigned)(hi - lo) * (unsigned long long)kTileCost;
+  for (int i = tid; i < n_all; i += NT) {
+    Tile t;
+    if (tile_at(i, &t)) work += (unsigned long long)(unsigned)(t.hi - t.lo) * (unsigned)(t.few ? kCostFew : kCostTile);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) work += __shfl_xor(work, d);
@@ -272,98 +284,127 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     __syncthreads();
     work = s_work;
   }
-  const unsigned long long share = (work + g.runs - 1) / g.runs;
-  auto chunk_of = [&](int j, bool few) -> int {      // candidate j of a class
-    const unsigned long long c = (share * (kChunks + j) + kChunks - 1) / kChunks;
-    return max((int)(few ? c : (c + kTileCost - 1) / kTileCost), few ? kMinChunkFew : kMinChunkTile);
-  };
-  int cf[kChunks], ct[kChunks], runs[kChunks];
+  // ---- the chunk lengths, in blocks
+  const unsigned long long share = (work + g.side - 1) / g.side;
+  int chunk_f[kChunks], chunk_t[kChunks], count[kChunks];
 #pragma unroll
-  for (int j = 0; j < kChunks; j++) { cf[j] = chunk_of(j, true); ct[j] = chunk_of(j, false); runs[j] = 0; }
-  for (int b = tid; b < g.B; b += NT) {
-    int lo, hi;
-    if (!few_at(b, &lo, &hi)) continue;
-#pragma unroll
-    for (int j = 0; j < kChunks; j++) runs[j] += max((int)((unsigned)(hi - lo + cf[j] - 1) / (unsigned)cf[j]), 1);
+  for (int j = 0; j < kChunks; j++) {
+    const unsigned long long c = (share * (8 + j) + 7) / 8;
+    chunk_f[j] = max((int)((c + kCostFew - 1) / kCostFew), kMinChunk);
+    chunk_t[j] = max((int)((c + kCostTile - 1) / kCostTile), kMinChunk);
+    count[j] = 0;
   }
-  for (int i = tid; i < n_tiles; i += NT) {
-    int b, tile, lo, hi;
-    tile_at(i, &b, &tile, &lo, &hi);
+  auto runs_of = [&](const Tile& t, int cf, int ct) -> int {
+    const unsigned c = (unsigned)(t.few ? cf : ct);
+    return max((int)(((unsigned)(t.hi - t.lo) + c - 1) / c), 1);
+  };
+  auto item_cost = [&](const Tile& t, int n) -> int { return ((t.hi - t.lo + n - 1) / n) * (t.few ? kCostFew : kCostTile); };   // of the longest run
+  for (int i = tid; i < n_all; i += NT) {
+    Tile t;
+    if (!tile_at(i, &t)) continue;
 #pragma unroll
-    for (int j = 0; j < kChunks; j++) runs[j] += max((int)((unsigned)(hi - lo + ct[j] - 1) / (unsigned)ct[j]), 1);
+    for (int j = 0; j < kChunks; j++) count[j] += runs_of(t, chunk_f[j], chunk_t[j]);
   }
 #pragma unroll
   for (int j = 0; j < kChunks; j++) {
-#pragma unroll
-    for (int d = 32; d >= 1; d /= 2) runs[j] += __shfl_xor(runs[j], d);
+    count[j] = wave_reduce(count[j], add);
     if constexpr (NW > 1) {
-      if (lane == 0) atomicAdd(&s_runs[j], runs[j]);
+      if (lane == 0) atomicAdd(&s_count[j], count[j]);
     }
   }
   if constexpr (NW > 1) {
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kChunks; j++) runs[j] = s_runs[j];
+    for (int j = 0; j < kChunks; j++) count[j] = s_count[j];
   }
-  int chunk_few = cf[0], chunk_tile = ct[0];
+  int chunk_few = chunk_f[0], chunk_tile = chunk_t[0];
 #pragma unroll
   for (int j = kChunks - 1; j >= 0; j--)
-    if (runs[j] <= g.runs) { chunk_few = cf[j]; chunk_tile = ct[j]; }
+    if (count[j] <= g.side) { chunk_few = chunk_f[j]; chunk_tile = chunk_t[j]; }
 
-  // ---- the items of both classes, in order; every wave writes its tiles' runs lane by lane
-  for (int cls = 0; cls < 2; cls++) {
-    const bool few = cls == 0;
-    const int n = few ? (g.rt ? g.B : 0) : n_tiles, chunk = few ? chunk_few : chunk_tile;
-    int* items = p.out + g.sched_few + (few ? 0 : (long)g.cap_few * kItemInts);
-    int n_items = 0, n_slots = 0, n_cut = 0;
-    for (int base = 0; base < n; base += NT) {
-      const int i = base + tid;
-      int b = 0, tile = 0, lo = 0, hi = 0, cnt = 0;
-      if (few) {
-        b = i;
-        if (few_at(i, &lo, &hi)) cnt = max((int)((unsigned)(hi - lo + chunk - 1) / (unsigned)chunk), 1);
-      } else if (i < n) {
-        tile_at(i, &b, &tile, &lo, &hi);
-        cnt = max((int)((unsigned)(hi - lo + chunk - 1) / (unsigned)chunk), 1);
-      }
-      // v: items up to this tile; w: partial slots in the low 20 bits, cut tiles above them (both at most 2 * runs, far below 2^11, 2^20)
-      int v = cnt, w = cnt > 1 ? cnt + (1 << 20) : 0, tv, tw;
-      const int w0 = w;
-      scan2(v, w, &tv, &tw);
-      const int to = n_items + v - cnt, slot = n_slots + ((w - w0) & 0xfffff);
-      if (!few && cnt > 1) p.out[kSchedHeader + n_cut + ((w - w0) >> 20)] = to;
-      // the wave's runs, 64 at a time: run number r of the wave belongs to the last lane whose first run is not after it
-      const int first = v - cnt - __shfl(v - cnt, 0), all = __shfl(first + cnt, 63);
-      for (int r0 = 0; r0 < all; r0 += 64) {
-        const int r = r0 + lane;
-        int own = 0;
+  // ---- the items, by buckets of their cost.  (Places inside a bucket and partial slots go by arrival: they say where and when an item
+  // is computed, not what.)
+  int longest = 0;
+  for (int i = tid; i < n_all; i += NT) {
+    Tile t;
+    if (tile_at(i, &t)) longest = max(longest, item_cost(t, runs_of(t, chunk_few, chunk_tile)));
+  }
+  longest = wave_reduce(longest, top);
+  if constexpr (NW > 1) {
+    if (lane == 0) atomicMax(&s_long, longest);
+    __syncthreads();
+    longest = s_long;
+  }
+  auto bucket_of = [&](const Tile& t, int n) -> int { return kBuckets - 1 - (int)((long)item_cost(t, n) * kBuckets / (longest + 1)); };
+  for (int i = tid; i < n_all; i += NT) {
+    Tile t;
+    if (!tile_at(i, &t)) continue;
+    const int n = runs_of(t, chunk_few, chunk_tile);
+    atomicAdd(&s_bucket[bucket_of(t, n)], n);
+  }
+  __syncthreads();
+  int n_items = 0;
+  if (tid < 64) {
+    static_assert(kBuckets == 64, "one lane each");
+    const int mine = s_bucket[lane];
+    int v = mine;
 #pragma unroll
-        for (int d = 32; d >= 1; d /= 2) {
-          const int f = __shfl(first, own + d > 63 ? 63 : own + d);
-          if (own + d <= 63 && f <= r) own += d;
-        }
-        const int ob = __shfl(b, own), ot = __shfl(tile, own), olo = __shfl(lo, own), ohi = __shfl(hi, own), oc = __shfl(cnt, own), oto = __shfl(to, own);
-        const int oslot = __shfl(slot, own), s = r - __shfl(first, own);
-        if (r < all) {
-          int* rec = items + (long)(oto + s) * kItemInts;       // (oto + s is below the class's cap: see resolve_paged)
-          const u32x4 q0 = {(unsigned)ob, (unsigned)s_q0[ob], (unsigned)s_n[ob], (unsigned)s_seq[ob]};
-          const u32x4 q1 = {(unsigned)ot, (unsigned)(olo + (int)((long)(ohi - olo) * s / oc)), (unsigned)(olo + (int)((long)(ohi - olo) * (s + 1) / oc)), (unsigned)oslot};
-          const u32x4 q2 = {(unsigned)s, (unsigned)oc, 0, 0};
-          *(u32x4*)rec = q0;
-          *(u32x4*)(rec + 4) = q1;
-          *(u32x4*)(rec + 8) = q2;
-        }
-      }
-      n_items += tv;
-      n_slots += tw & 0xfffff;
-      n_cut += tw >> 20;
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(v, d);
+      if (lane >= d) v += o;
     }
-    if (tid == 0) {
-      p.out[1 + cls] = n_items;
-      if (!few) p.out[3] = n_cut;
+    s_bucket[lane] = v - mine;
+    n_items = __shfl(v, 63);
+  }
+  __syncthreads();
+  int* items = p.out + g.sched_items;
+  for (int base = 0; base < n_all; base += NT) {
+    const int i = base + tid;
+    Tile t = {0, 0, 0, 0, false};
+    int n = 0, to = 0, slot = 0;
+    if (i < n_all && tile_at(i, &t)) {
+      n = runs_of(t, chunk_few, chunk_tile);
+      to = atomicAdd(&s_bucket[bucket_of(t, n)], n);
+      if (n > 1) {
+        slot = atomicAdd(&s_slots[t.few ? 0 : 1], n);
+        if (!t.few) p.out[kSchedHeader + atomicAdd(&s_cut, 1)] = to;
+      }
+    }
+    // the wave's runs, 64 at a time: run number r of the wave belongs to the last lane whose first run is not after it
+    int v = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(v, d);
+      if (lane >= d) v += o;
+    }
+    const int first = v - n, all = __shfl(v, 63);
+    for (int r0 = 0; r0 < all; r0 += 64) {
+      const int r = r0 + lane;
+      int own = 0;
+#pragma unroll
+      for (int d = 32; d >= 1; d /= 2) {
+        const int f = __shfl(first, own + d > 63 ? 63 : own + d);
+        if (own + d <= 63 && f <= r) own += d;
+      }
+      const int ob = __shfl(t.b, own), ot = __shfl(t.tile, own), olo = __shfl(t.lo, own), ohi = __shfl(t.hi, own), oc = __shfl(n, own), oto = __shfl(to, own);
+      const int oslot = __shfl(slot, own), of = __shfl(t.few ? 1 : 0, own), s = r - __shfl(first, own);
+      if (r < all) {
+        int* rec = items + (long)(oto + s) * kItemInts;       // (below the number of items there is room for: see resolve_paged)
+        const u32x4 q0 = {(unsigned)ob, (unsigned)s_q0[ob], (unsigned)s_n[ob], (unsigned)s_seq[ob]};
+        const u32x4 q1 = {(unsigned)ot, (unsigned)(olo + (int)((long)(ohi - olo) * s / oc)), (unsigned)(olo + (int)((long)(ohi - olo) * (s + 1) / oc)), (unsigned)oslot};
+        const u32x4 q2 = {(unsigned)s, (unsigned)oc, (unsigned)of, 0};
+        *(u32x4*)rec = q0;
+        *(u32x4*)(rec + 4) = q1;
+        *(u32x4*)(rec + 8) = q2;
+      }
     }
   }
-  if (tid == 0) p.out[0] = (int)g.key;
+  __syncthreads();
+  if (tid == 0) {
+    p.out[0] = (int)g.key;
+    p.out[1] = n_items;
+    p.out[2] = s_cut;
+  }
 }
 
 // ======================================================================================
@@ -383,11 +424,11 @@ struct PagedAttn {
   unsigned *arrived;               // few-row class: per (slot, key head) runs of a group that have arrived, then groups of a tile; zero between calls
 };
 
-struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs; };
+struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs, few; };
 
 __device__ __forceinline__ Item load_item(const int* rec) {
   Item i;
-  i.b = rec[0]; i.q0 = rec[1]; i.n = rec[2]; i.seq = rec[3]; i.tile = rec[4]; i.k0 = rec[5]; i.k1 = rec[6]; i.slot = rec[7]; i.run = rec[8]; i.runs = rec[9];
+  i.b = rec[0]; i.q0 = rec[1]; i.n = rec[2]; i.seq = rec[3]; i.tile = rec[4]; i.k0 = rec[5]; i.k1 = rec[6]; i.slot = rec[7]; i.run = rec[8]; i.runs = rec[9]; i.few = rec[10];
   return i;
 }
 
@@ -1090,40 +1131,41 @@ __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const Pa
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
   if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
-  few_rows_item<RT, kFewWaves>(p, load_item(p.schedule + p.g.sched_few + (long)idx * kItemInts), head, smem);
+  few_rows_item<RT, kFewWaves>(p, load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts), head, smem);
 }
 
 template <bool FEW>    // FEW: the batch may have few-row items
 __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
-  if (p.schedule[0] != (int)p.g.key) return;
-  const int tiles = p.schedule[2];
-  const int* few = p.schedule + p.g.sched_few;
-  if (idx < tiles) tile_item(p, load_item(few + ((long)p.g.cap_few + idx) * kItemInts), head, smem);
-  else if (FEW && idx - tiles < p.schedule[1] && threadIdx.x < kFewWaves * 64)
-    few_rows_item<2, kFewWaves>(p, load_item(few + (long)(idx - tiles) * kItemInts), head, smem);
+  if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
+  const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);
+  if (!FEW || !it.few) tile_item(p, it, head, smem);
+  else if (threadIdx.x < kFewWaves * 64) few_rows_item<2, kFewWaves>(p, it, head, smem);
 }
 
-// Joins the runs of the cut tiles, 32 rows of a tile and key head at a time (256 KiB of partial results from two runs up: all workgroups share
-// them, where a tile's last run alone would read them at one compute unit's pace).
-constexpr int kJoinRows = 32;
+// Joins the runs of the cut tiles; all workgroups share them, where a tile's last run alone would read its partial results, 128 KiB a
+// run, at one compute unit's pace.  A job is 8 rows of a tile and key head, more where there would be more than two jobs to a workgroup
+// (8 rows against 32: one tile of 32 runs 41 -> 34 us in the whole call; 54 tiles of 2..8 runs 36 -> 41, hence the rule).
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
   const PagedGeom& g = p.g;
   if (p.schedule[0] != (int)g.key) return;
-  const int parts = (g.rows_tile + kJoinRows - 1) / kJoinRows, jobs = p.schedule[3] * g.Hk * parts;
+  const int cuts = p.schedule[2] * g.Hk;
+  int rows = 8;
+  while (rows < 64 && cuts * (kTileRows / rows) > 2 * (int)gridDim.x) rows *= 2;
+  const int parts = (g.rows_tile + rows - 1) / rows, jobs = cuts * parts;
   for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts, r0 = (rest - head * parts) * kJoinRows;
-    const Item it = load_item(p.schedule + g.sched_few + ((long)g.cap_few + p.schedule[kSchedHeader + cut]) * kItemInts);
+    const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts, r0 = (rest - head * parts) * rows;
+    const Item it = load_item(p.schedule + g.sched_items + (long)p.schedule[kSchedHeader + cut] * kItemInts);
     const int row0 = it.tile * kTileRows, n = min(it.n * g.G - row0, kTileRows);
     const long step = (long)g.Hk * g.rows_tile;
-    for (int i = threadIdx.x; i < kJoinRows * 32; i += 256) {
+    for (int i = threadIdx.x; i < rows * 32; i += 256) {
       const int r = r0 + (i >> 5), d4 = (i & 31) * 4;
       if (r >= n) break;
       const long at = ((long)it.slot * g.Hk + head) * g.rows_tile + r;
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
       float m = -INFINITY, l = 0.f;
-      for (int s = 0; s < it.runs; s += 8) join_quad<8>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, 8), d4, p.scale_log2e, &o, &m, &l);
+      for (int s = 0; s < it.runs; s += kJoin) join_quad<kJoin>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
       store_out(p, it, head, row0 + r, d4, o, m, l);
     }
   }
@@ -1161,14 +1203,14 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   const long most_rows = (long)g->max_new * g->G, all_rows = (long)g->T * g->G;
   g->rt = g->G > kFewRows ? 0 : (most_rows <= 16 ? 1 : 2);
   g->has_tiles = most_rows > (g->rt ? kFewRows : 0);
-  // Runs.  chunk >= the class's work / runs, so a tile of b > chunk blocks is cut into ceil(b / chunk) < 2 b / chunk runs: all cut tiles
-  // together make less than 2 * runs of them (so there are fewer than `runs`), and all tiles together at most tiles + runs items.
+  // Runs.  A class's chunk is at least its blocks / side, so a tile of b > chunk blocks is cut into ceil(b / chunk) < 2 b / chunk runs:
+  // all cut tiles together make less than 2 * side of them (there are fewer than `side`), and all tiles at most tiles + side items.
   const int cus = ctx->num_cus < 1024 ? ctx->num_cus : 1024;
-  g->runs = ceil_div(cus, g->Hk);
-  g->sched_few = kSchedHeader + (g->runs + 3) / 4 * 4;
+  g->side = ceil_div(cus, g->Hk);
+  g->sched_items = kSchedHeader + (g->side + 3) / 4 * 4;
   const long tiles = all_rows / kTileRows + (g->rt ? (g->B < all_rows / (kFewRows + 1) + 1 ? g->B : all_rows / (kFewRows + 1) + 1) : g->B);
-  g->cap_few = g->rt ? g->B + g->runs : 0;
-  g->cap_tile = g->has_tiles ? (int)(tiles + g->runs) : 0;
+  g->cap_few = g->rt ? g->B + g->side : 0;
+  g->cap_tile = g->has_tiles ? (int)(tiles + g->side) : 0;
   g->rows_few = g->rt ? (int)(most_rows < kFewRows ? most_rows : kFewRows) : 0;
   g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
   if (((long)g->cap_tile + g->cap_few) * g->Hk > 0x7fffffffL)
@@ -1180,15 +1222,15 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   return TL_OK;
 }
 
-// Two counters per partial slot and key head: 2 * runs * heads_kv slots, runs = ceil(compute units / heads_kv).
+// Two counters per partial slot and key head: 2 * side * heads_kv of those, side = ceil(compute units / heads_kv).
 constexpr size_t kArrivedBytes = 2 * (2 * (1024 + 1024)) * 4;
 
 struct PagedSizes { size_t schedule, ws, part_few, ml_few, part_tile, ml_tile; };
 
 static PagedSizes paged_sizes(const PagedGeom& g) {
   PagedSizes s;
-  s.schedule = ((size_t)g.sched_few + ((size_t)g.cap_few + g.cap_tile) * kItemInts) * 4;
-  const size_t few = (size_t)2 * g.runs * g.Hk * g.rows_few, tile = (size_t)2 * g.runs * g.Hk * g.rows_tile;   // partial rows
+  s.schedule = ((size_t)g.sched_items + ((size_t)g.cap_few + g.cap_tile) * kItemInts) * 4;
+  const size_t few = (size_t)2 * g.side * g.Hk * g.rows_few, tile = (size_t)2 * g.side * g.Hk * g.rows_tile;   // partial rows
   s.part_few = kArrivedBytes;             // (in front: the arrival counters, the same for all dims, so that calls of any may share a workspace)
   s.ml_few = s.part_few + few * kPagedD * 4;
   s.part_tile = s.ml_few + (few * 8 + 255) / 256 * 256;
@@ -1210,7 +1252,7 @@ int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims, size_t* schedul
   const PagedSizes s = paged_sizes(g);
   *schedule_bytes = s.schedule;
   *ws_bytes = s.ws;
-  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.runs, g.T, g.G};
+  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.side, g.T, g.G};
   memcpy(info, v, sizeof v);
   return TL_OK;
 }
@@ -1290,14 +1332,14 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
   p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
   hipStream_t s = (hipStream_t)stream;
-  auto launch = [&](auto kernel, int grid, int threads) -> int {
-    TL_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds));
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), kFewLds, s, p);
+  auto launch = [&](auto kernel, int grid, int threads, int lds) -> int {
+    TL_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), lds, s, p);
     TL_HIP(hipGetLastError());
     return TL_OK;
   };
-  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.cap_few * g.Hk, kFewWaves * 64);
-  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads)) return e;
+  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.cap_few * g.Hk, kFewWaves * 64, kFewWaves * 2 * kUnitBytes);
+  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
   hipLaunchKernelGGL(paged_join_kernel, dim3(2 * ctx->num_cus), dim3(256), 0, s, p);
   TL_HIP(hipGetLastError());
   return TL_OK;

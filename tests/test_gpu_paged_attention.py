@@ -56,8 +56,8 @@ def test_cut_key_axis(heads, cached, new):
     torch.cuda.synchronize()
     hdr = b.schedule[:3].tolist()
     tl.tl_ctx_destroy(c)
-    assert hdr[1] + hdr[2] > len(cached), "this case is meant to cut the key axis"
-    assert hdr[1] <= z["few_items"] and hdr[2] <= z["tile_items"]
+    assert hdr[1] > len(cached), "this case is meant to cut the key axis"
+    assert hdr[1] <= z["few_items"] + z["tile_items"]
     b.run()
     check_attention(b)
 
@@ -171,7 +171,7 @@ def test_lengths_that_make_no_sense_stay_in_bounds():
     b.attention_call(c)
     torch.cuda.synchronize()
     assert (guard[b.schedule.numel():] == -1).all()
-    assert 0 <= int(b.schedule[1]) <= z["few_items"] and 0 <= int(b.schedule[2]) <= z["tile_items"]
+    assert 0 <= int(b.schedule[1]) <= z["few_items"] + z["tile_items"]
     tl.tl_ctx_destroy(c)
 
 
