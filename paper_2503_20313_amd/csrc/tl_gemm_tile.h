@@ -74,6 +74,10 @@ __device__ __forceinline__ void lds_load16(const void* g, char* lds_wave_base) {
 __device__ __forceinline__ void lds_load16_sbase(const char* base, unsigned lane_off, unsigned lds_wave_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_wave_base), "v"(lane_off), "s"(base) : "memory");
 }
+// ... of data that is read once (streaming)
+__device__ __forceinline__ void lds_load16_sbase_nt(const char* base, unsigned lane_off, unsigned lds_wave_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_wave_base), "v"(lane_off), "s"(base) : "memory");
+}
 // ... and with a per-lane 64-bit address, the LDS destination given as a 32-bit LDS address.
 __device__ __forceinline__ void lds_load16_at(const char* g, unsigned lds_wave_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_wave_base), "v"(g) : "memory");

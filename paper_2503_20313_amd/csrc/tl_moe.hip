@@ -6,6 +6,7 @@
 //   (f_S_low, f_S_high, expert, chan_mask_lo, chan_mask_hi, f_R_lo, f_R_hi, 0),
 // over the routed rows sorted by expert (stable: ascending row id = token*topk + slot inside an expert).
 #include "tl_ag_producer.h"
+#include "tl_fast_div.h"
 #include "tl_gemm_tile.h"
 #include "tl_host.h"
 #include "tl_rs_consumer.h"
@@ -92,21 +93,6 @@ __global__ void __launch_bounds__(64) moe_topk_kernel(const float* __restrict__ 
 constexpr int kRouteWaves = kRouteThreads / 64;
 constexpr int kLdsTiles = 2048;  // channel masks are collected in LDS up to this many tiles, else in global memory
 constexpr int kRouteAhead = 8;
-
-// n / d for 0 <= n < 2^31 as a multiplication by a 32-bit reciprocal (the round-up method of Granlund and Montgomery,
-// "Division by Invariant Integers using Multiplication", 1994: m = floor(2^32 (2^l - d) / d) + 1
-// with l = ceil(log2 d), n / d = (mulhi(m, n) + n) >> l).
-struct FastDiv {
-  unsigned mul, shift;
-  __device__ __forceinline__ unsigned div(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
-};
-static FastDiv make_fast_div(unsigned d) {
-  FastDiv f;
-  f.shift = 0;
-  while (f.shift < 31 && (1u << f.shift) < d) f.shift++;
-  f.mul = (unsigned)((((1ull << f.shift) - d) << 32) / d + 1);
-  return f;
-}
 
 __device__ __forceinline__ unsigned long long same_expert_lanes(int e, bool valid, int E) {
   unsigned long long same = __builtin_amdgcn_ballot_w64(valid);

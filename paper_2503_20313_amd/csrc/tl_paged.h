@@ -1,5 +1,6 @@
 // Geometry of the paged-cache operators: what the host resolves from tl_paged_dims and the kernels are given.
 #pragma once
+#include "tl_fast_div.h"
 #include "tl_host.h"
 
 namespace tl {
@@ -25,6 +26,7 @@ struct PagedGeom {
   int side;                // items per key head that run side by side: the key axes are cut for so many
   int sched_items;         // where the items start in the schedule, in ints
   int rows_few, rows_tile; // rows of a partial result
+  FastDiv by_group;        // G: row of a request -> token
   unsigned key;            // of all of the above: a schedule serves only the dims it was made for
 };
 
