@@ -3,6 +3,8 @@
 //
 // Cache: page p, key head h, row r at p * page_stride + (h * page_size + r) * 128 elements, so the rows of a page and head are one
 // contiguous piece (4 KiB for the smallest page) and 16 keys never straddle pages.
+#include <atomic>
+
 #include "tl_gemm_tile.h"
 #include "tl_host.h"
 #include "tl_paged.h"
@@ -14,14 +16,13 @@ typedef short short8_t __attribute__((ext_vector_type(8)));
 
 // ======================================================================================
 // Block tables and slot maps.  Two scans over the requests (tokens, then new pages), done by every workgroup for itself in LDS;
-// then a thread per token finds its request by binary search, and a thread per new page writes its table entry.
-// Where several workgroups share the work, what may be written in place (lengths, the head of the free list) is left to a second
-// launch of one workgroup (PART 2), so that no workgroup's inputs change under it.
+// then a thread per token finds its request by binary search, and a thread per new page writes its table entry.  Where several
+// workgroups share the maps and lengths or the head of the free list are written in place, those are left to a second launch of one
+// workgroup, so that no workgroup's inputs change under it.
+//
+// Bound by latency: lengths, scans, free list, stores, each a few hundred nanoseconds behind the other.  A token to a thread: 64 k tokens of
+// 512 requests 14 -> 7 us against four in a row and a second launch; small steps take one wave, without barriers (6.5 -> 4.4 us).
 // ======================================================================================
-constexpr int kSlotThreads = 1024;
-constexpr int kSlotWaves = kSlotThreads / 64;
-constexpr int kReqPerThread = kMaxBatch / kSlotThreads;
-
 struct SlotsParams {
   const int *ctx_lens, *new_lens, *free_pages, *free_from;
   int n_free;
@@ -30,19 +31,24 @@ struct SlotsParams {
 };
 
 // Inclusive scan over the workgroup's threads; *total = the sum.  All threads call it.
+template <int NT>
 __device__ __forceinline__ int block_scan(int v, int* s_wave, int* total) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const int o = __shfl_up(v, d);
     if (lane >= d) v += o;
+  }
+  if constexpr (NT == 64) {
+    *total = __shfl(v, 63);
+    return v;
   }
   __syncthreads();   // (s_wave may still be read by the previous scan)
   if (lane == 63) s_wave[wave] = v;
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kSlotWaves; w++) {
+  for (int w = 0; w < NT / 64; w++) {
     const int x = s_wave[w];
     if (w < wave) before += x;
     all += x;
@@ -61,17 +67,22 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
   return lo;
 }
 
-template <int PART>  // 0: everything (one workgroup); 1: maps and tables; 2: lengths and counts (one workgroup)
-__global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsParams p) {
-  __shared__ int s_wave[kSlotWaves];
-  __shared__ int s_start[kMaxBatch + 1], s_page[kMaxBatch + 1], s_ctx[kMaxBatch];
+constexpr int kMaps = 1, kLengths = 2;
+
+template <int PARTS, int NT>     // what this launch writes; kLengths: by workgroup 0.  NT = 64: at most 64 requests
+__global__ void __launch_bounds__(NT) paged_slots_kernel(const SlotsParams p) {
+  constexpr int kReq = NT == 64 ? 1 : kMaxBatch / NT;      // requests per thread at most
+  constexpr int kRoom = NT == 64 ? 64 : kMaxBatch;
+  __shared__ int s_wave[NT / 64];
+  __shared__ int s_start[kRoom + 1], s_page[kRoom + 1], s_ctx[kRoom];
   const int tid = threadIdx.x;
-  const int per = (p.B + kSlotThreads - 1) / kSlotThreads, b0 = tid * per;   // a thread's requests: b0 .. b0 + per - 1
+  const int per = (p.B + NT - 1) / NT, b0 = tid * per;     // a thread's requests: b0 .. b0 + per - 1
   const int cap = p.max_blocks * p.page;
-  int len[kReqPerThread];
+  const int from = p.free_from ? max(p.free_from[0], 0) : 0;
+  int len[kReq];
   int sum = 0, asked = 0;
 #pragma unroll
-  for (int i = 0; i < kReqPerThread; i++) {
+  for (int i = 0; i < kReq; i++) {
     len[i] = 0;
     if (i < per && b0 + i < p.B) {
       const int c = min(max(p.ctx_lens[b0 + i], 0), cap), want = min(max(p.new_lens[b0 + i], 0), 1 << 18);
@@ -81,12 +92,12 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsPa
       asked += want - len[i];
     }
   }
-  int all_tokens, all_pages, over;
-  int at = block_scan(sum, s_wave, &all_tokens) - sum;
+  int all_tokens, all_pages, over = 0;
+  int at = block_scan<NT>(sum, s_wave, &all_tokens) - sum;
   // tokens that do not fit the rows are cut off at the end
   int pages = 0;
 #pragma unroll
-  for (int i = 0; i < kReqPerThread; i++)
+  for (int i = 0; i < kReq; i++)
     if (i < per && b0 + i < p.B) {
       const int lo = min(at, p.T), hi = min(at + len[i], p.T);
       asked += len[i] - (hi - lo);
@@ -96,28 +107,29 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsPa
       const int c = s_ctx[b0 + i];
       pages += ((c + len[i] + p.page - 1) >> p.page_shift) - ((c + p.page - 1) >> p.page_shift);
     }
-  int pg = block_scan(pages, s_wave, &all_pages) - pages;
+  int pg = block_scan<NT>(pages, s_wave, &all_pages) - pages;
 #pragma unroll
-  for (int i = 0; i < kReqPerThread; i++)
+  for (int i = 0; i < kReq; i++)
     if (i < per && b0 + i < p.B) {
       const int c = s_ctx[b0 + i];
       s_page[b0 + i] = pg;
       pg += ((c + len[i] + p.page - 1) >> p.page_shift) - ((c + p.page - 1) >> p.page_shift);
     }
   const int n_tokens = min(all_tokens, p.T);
-  const int from = p.free_from ? max(p.free_from[0], 0) : 0;
   const int left = max(p.n_free - from, 0);          // pages that the list still holds
-  if (PART != 1) block_scan(asked, s_wave, &over);
+  const bool lengths = (PARTS & kLengths) && blockIdx.x == 0;
+  if (lengths) block_scan<NT>(asked, s_wave, &over);
   if (tid == 0) { s_start[p.B] = n_tokens; s_page[p.B] = all_pages; }
-  __syncthreads();   // every input that may be written in place has been read
-  if (PART != 2) {
-    const int step = gridDim.x * kSlotThreads;
-    for (int i = blockIdx.x * kSlotThreads + tid; i < all_pages; i += step) {
+  __syncthreads();   // every input that this workgroup may write in place has been read
+  if (PARTS & kMaps) {
+    const int step = gridDim.x * NT;
+    for (int i = blockIdx.x * NT + tid; i < all_pages; i += step) {
+      const int page = i < left ? p.free_pages[from + i] : -1;
       const int b = last_at_most(s_page, p.B, i);
       const int j = ((s_ctx[b] + p.page - 1) >> p.page_shift) + i - s_page[b];
-      p.block_table[(long)b * p.max_blocks + j] = i < left ? p.free_pages[from + i] : -1;
+      p.block_table[(long)b * p.max_blocks + j] = page;
     }
-    for (int t = blockIdx.x * kSlotThreads + tid; t < p.T; t += step) {
+    for (int t = blockIdx.x * NT + tid; t < p.T; t += step) {
       int slot = -1, pos = 0;
       if (t < n_tokens) {
         const int b = last_at_most(s_start, p.B, t);
@@ -136,8 +148,8 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const SlotsPa
       p.positions[t] = pos;
     }
   }
-  if (PART != 1) {
-    for (int b = tid; b <= p.B; b += kSlotThreads) {
+  if (lengths) {
+    for (int b = tid; b <= p.B; b += NT) {
       p.query_start[b] = s_start[b];
       if (b < p.B) p.seq_lens[b] = s_ctx[b] + s_start[b + 1] - s_start[b];
     }
@@ -272,10 +284,18 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     }
     return true;
   };
+  // (every pass below goes over them; a thread's first one stays in registers)
+  Tile mine = {0, 0, 0, 0, false};
+  const bool has = tid < n_all && tile_at(tid, &mine);
+  auto tile_of = [&](int i, Tile* t) -> bool {
+    if (i >= NT) return tile_at(i, t);
+    *t = mine;
+    return has;
+  };
   unsigned long long work = 0;
   for (int i = tid; i < n_all; i += NT) {
     Tile t;
-    if (tile_at(i, &t)) work += (unsigned long long)(unsigned)(t.hi - t.lo) * (unsigned)(t.few ? kCostFew : kCostTile);
+    if (tile_of(i, &t)) work += (unsigned long long)(unsigned)(t.hi - t.lo) * (unsigned)(t.few ? kCostFew : kCostTile);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) work += __shfl_xor(work, d);
@@ -301,7 +321,7 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   auto item_cost = [&](const Tile& t, int n) -> int { return ((t.hi - t.lo + n - 1) / n) * (t.few ? kCostFew : kCostTile); };   // of the longest run
   for (int i = tid; i < n_all; i += NT) {
     Tile t;
-    if (!tile_at(i, &t)) continue;
+    if (!tile_of(i, &t)) continue;
 #pragma unroll
     for (int j = 0; j < kChunks; j++) count[j] += runs_of(t, chunk_f[j], chunk_t[j]);
   }
@@ -327,7 +347,7 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   int longest = 0;
   for (int i = tid; i < n_all; i += NT) {
     Tile t;
-    if (tile_at(i, &t)) longest = max(longest, item_cost(t, runs_of(t, chunk_few, chunk_tile)));
+    if (tile_of(i, &t)) longest = max(longest, item_cost(t, runs_of(t, chunk_few, chunk_tile)));
   }
   longest = wave_reduce(longest, top);
   if constexpr (NW > 1) {
@@ -338,7 +358,7 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   auto bucket_of = [&](const Tile& t, int n) -> int { return kBuckets - 1 - (int)((long)item_cost(t, n) * kBuckets / (longest + 1)); };
   for (int i = tid; i < n_all; i += NT) {
     Tile t;
-    if (!tile_at(i, &t)) continue;
+    if (!tile_of(i, &t)) continue;
     const int n = runs_of(t, chunk_few, chunk_tile);
     atomicAdd(&s_bucket[bucket_of(t, n)], n);
   }
@@ -362,7 +382,7 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     const int i = base + tid;
     Tile t = {0, 0, 0, 0, false};
     int n = 0, to = 0, slot = 0;
-    if (i < n_all && tile_at(i, &t)) {
+    if (i < n_all && tile_of(i, &t)) {
       n = runs_of(t, chunk_few, chunk_tile);
       to = atomicAdd(&s_bucket[bucket_of(t, n)], n);
       if (n > 1) {
@@ -1284,6 +1304,16 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
 // Two counters per partial slot and key head: 2 * side * heads_kv of those, side = ceil(compute units / heads_kv).
 constexpr size_t kArrivedBytes = 2 * (2 * (1024 + 1024)) * 4;
 
+// Lets kernel number `which` of this file use `bytes` of dynamic LDS on `device`; asked of the runtime once (it takes a microsecond a call).
+static int allow_lds(const void* kernel, int which, int device, int bytes) {
+  static std::atomic<unsigned long long> done[4];
+  const unsigned long long bit = 1ull << (device & 63);
+  if (device < 64 && (done[which].load(std::memory_order_acquire) & bit)) return TL_OK;
+  TL_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (device < 64) done[which].fetch_or(bit, std::memory_order_release);
+  return TL_OK;
+}
+
 struct PagedSizes { size_t schedule, ws, part_few, ml_few, part_tile, ml_tile; };
 
 static PagedSizes paged_sizes(const PagedGeom& g) {
@@ -1330,11 +1360,15 @@ int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims, const int* ctx_lens, 
   const SlotsParams p = {ctx_lens, new_lens, free_pages, free_from, n_free, free_to, block_table, query_start, seq_lens, slots, positions, counts,
                          g.B, g.T, g.max_new, g.max_blocks, g.page, g.page_shift, g.n_pages};
   hipStream_t s = (hipStream_t)stream;
-  const int wgs = g.T > 4 * kSlotThreads ? (g.T + 4 * kSlotThreads - 1) / (4 * kSlotThreads) : 1;
-  if (wgs == 1) hipLaunchKernelGGL(paged_slots_kernel<0>, dim3(1), dim3(kSlotThreads), 0, s, p);
+  const bool in_place = seq_lens == ctx_lens || (free_to && free_to == free_from);
+  if (g.B <= 64 && g.T <= 256) hipLaunchKernelGGL((paged_slots_kernel<kMaps | kLengths, 64>), dim3(1), dim3(64), 0, s, p);
   else {
-    hipLaunchKernelGGL(paged_slots_kernel<1>, dim3(wgs), dim3(kSlotThreads), 0, s, p);
-    hipLaunchKernelGGL(paged_slots_kernel<2>, dim3(1), dim3(kSlotThreads), 0, s, p);
+    const int wgs = ceil_div(g.T, 1024);
+    if (wgs == 1 || !in_place) hipLaunchKernelGGL((paged_slots_kernel<kMaps | kLengths, 1024>), dim3(wgs), dim3(1024), 0, s, p);
+    else {
+      hipLaunchKernelGGL((paged_slots_kernel<kMaps, 1024>), dim3(wgs), dim3(1024), 0, s, p);
+      hipLaunchKernelGGL((paged_slots_kernel<kLengths, 1024>), dim3(1), dim3(1024), 0, s, p);
+    }
   }
   TL_HIP(hipGetLastError());
   return TL_OK;
@@ -1391,14 +1425,14 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
   p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
   hipStream_t s = (hipStream_t)stream;
-  auto launch = [&](auto kernel, int grid, int threads, int lds) -> int {
-    TL_HIP(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  auto launch = [&](auto kernel, int which, int grid, int threads, int lds) -> int {
+    if (int e = allow_lds((const void*)kernel, which, ctx->device, lds)) return e;
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), lds, s, p);
     TL_HIP(hipGetLastError());
     return TL_OK;
   };
-  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.cap_few * g.Hk, kFewWaves * 64, kFewWaves * 2 * kUnitBytes);
-  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
+  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, g.cap_few * g.Hk, kFewWaves * 64, kFewWaves * 2 * kUnitBytes);
+  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, g.rt ? 2 : 3, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
   hipLaunchKernelGGL(paged_join_kernel, dim3(2 * ctx->num_cus), dim3(256), 0, s, p);
   TL_HIP(hipGetLastError());
   return TL_OK;

@@ -6,12 +6,15 @@
 //
 // Bound by memory: every element is read once and written once.  16 lanes own a head (8 elements, one 16-byte access, each), so the
 // mean is four lane rotations inside a row of 16 lanes and a pair's partner sits in the same row; a row of lanes takes kHeads heads
-// of one token, whose loads are in flight together and which share the token's angles.
+// of one token, which share the token's angles.  4096 rows of 32 + 32 heads (136 MB moved): kHeads 1, 2, 3, 4: 27.8, 24.4, 25.4, 25.2 us;
+// 8001 rows of 32 + 8 + 8 heads into pages in random order (199 MB): 47.2, 38.8, 38.8, 39.3.
+// Results larger than the dies' L2s together are stored as streaming, as they would not stay there: 33.1 -> 25.2 and 44.3 -> 39.3 us (kHeads 4).
+// Smaller ones, a decode step's, are left for the attention that reads them next.
 #include "tl_paged.h"
 
 namespace tl {
 
-constexpr int kHeads = 4;      // heads of a token that a row of 16 lanes takes
+constexpr int kHeads = 2;      // heads of a token that a row of 16 lanes takes
 
 struct RopeParams {
   const bf16_t *q, *k, *v;
@@ -44,7 +47,7 @@ __device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
   }
 }
 
-template <bool CACHE>
+template <bool CACHE, bool STREAM>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
   const long task = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int t = (int)(task / p.groups), h0 = (int)(task - (long)t * p.groups) * kHeads;
@@ -130,7 +133,7 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
       }
       res = pack_bf16x8(x);
     }
-    *(u32x4*)(dst + l * 8) = res;
+    if constexpr (STREAM) __builtin_nontemporal_store(res, (u32x4*)(dst + l * 8)); else *(u32x4*)(dst + l * 8) = res;
   }
 }
 
@@ -169,10 +172,14 @@ static RopeParams rope_params(const void* q, long long q_stride, const void* k, 
   return p;
 }
 
-static int launch_rope(void (*kernel)(const RopeParams), const RopeParams& p, void* stream) {
+constexpr long kL2Bytes = 32L << 20;      // of the eight dies
+
+template <bool CACHE>
+static int launch_rope(const RopeParams& p, void* stream) {
   const long wgs = ((long)p.T * p.groups + 15) / 16;
   if (wgs > 0x7fffffffL) return fail(TL_ERR_UNSUPPORTED_SHAPE, "too many rows and heads for one launch");
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, p);
+  const bool stream_out = (long)p.T * p.heads * kPagedD * 2 > kL2Bytes;
+  hipLaunchKernelGGL((stream_out ? qk_norm_rope_kernel<CACHE, true> : qk_norm_rope_kernel<CACHE, false>), dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -199,7 +206,7 @@ int tl_qk_norm_rope(tl_ctx* ctx, const void* q, long long q_stride, const void* 
   RopeParams p = rope_params(q, q_stride, k, k_stride, q_out, q_out_stride, T, heads_q, heads_kv, heads_q + heads_kv, q_weight, k_weight, eps, positions,
                              cos_sin, max_position, rot_dim, interleaved);
   p.k_out = (bf16_t*)k_out; p.ko_stride = k_out_stride;
-  return launch_rope(qk_norm_rope_kernel<false>, p, stream);
+  return launch_rope<false>(p, stream);
 }
 
 int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, long long q_stride, const void* k, long long k_stride, const void* v,
@@ -224,7 +231,7 @@ int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims, const void* q,
   p.k_cache = (bf16_t*)k_cache; p.v_cache = (bf16_t*)v_cache;
   p.slots = slots;
   p.page = g.page; p.page_shift = g.page_shift; p.n_slots = g.n_pages * g.page; p.page_stride = g.page_stride;
-  return launch_rope(qk_norm_rope_kernel<true>, p, stream);
+  return launch_rope<true>(p, stream);
 }
 
 }  // extern "C"

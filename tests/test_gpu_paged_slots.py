@@ -81,7 +81,7 @@ def test_tokens_that_do_not_fit():
     run([0] * 3, [3000] * 3, T=8000)
 
 
-@pytest.mark.parametrize("lens", [[1, 1, 1], [3000, 2000, 1]], ids=str)
+@pytest.mark.parametrize("lens", [[1, 1, 1], [100, 100, 100], [3000, 2000, 1]], ids=str)
 def test_in_place(lens):
     run([5, 31, 64], lens, in_place=True, free_from=3)
 

@@ -83,6 +83,24 @@ def test_in_place_and_rows_without_a_position():
     tl.tl_ctx_destroy(c)
 
 
+def test_results_larger_than_the_caches():
+    """Streaming stores; the first and last rows and some between are compared."""
+    T, Hq, Hk = 9001, 16, 4
+    qkv, (wq, wk), pos = draw(T, Hq, Hk, 8)
+    cs, row = angles(128), qkv.stride(0)
+    qo, ko = torch.zeros(T, Hq * D, dtype=torch.bfloat16, device=dev()), torch.zeros(T, Hk * D, dtype=torch.bfloat16, device=dev())
+    c = ctx()
+    q, k = qkv[:, :Hq * D], qkv[:, Hq * D:(Hq + Hk) * D]
+    tl.tl_qk_norm_rope(c, q, row, k, row, qo, Hq * D, ko, Hk * D, T, Hq, Hk, D, wq, wk, EPS, pos, cs, MAXPOS, 128, False)
+    torch.cuda.synchronize()
+    some = torch.tensor([0, 1, 15, 16, 4000, 8191, 8192, T - 2, T - 1], device=dev())
+    p = pos[some].cpu().numpy()
+    close(qo[some], q[some], Hq, wq, p, cs, 128, False)
+    close(ko[some], k[some], Hk, wk, p, cs, 128, False)
+    assert (qo != 0).any(1).all() and (ko != 0).any(1).all()
+    tl.tl_ctx_destroy(c)
+
+
 def test_zero_rows_and_large_values():
     """A row of zeros is finite (eps); values whose squares leave the range of bf16 but not of fp32 are normed alike."""
     T, Hq, Hk = 3, 2, 1
