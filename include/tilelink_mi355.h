@@ -508,7 +508,7 @@ int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int
  *   q dev [max_tokens rows of heads_q*128] bf16, q_stride elements apart;  o likewise (written; rows behind the last request are
  *     left as they were);  lse dev fp32 [max_tokens, heads_q] (written; NULL: not wanted): log of the sum of exponentials
  *   block_table dev int[batch, max_blocks];  schedule from tl_paged_schedule with the same dims
- *   workspace dev, ws_bytes of tl_paged_query, 16-byte aligned, zeroed once: counters that are zero again after every call, and
+ *   workspace dev, ws_bytes of tl_paged_query, 128-byte aligned, zeroed once: counters that are zero again after every call, and
  *     partial results of cut key axes, of which nothing is kept.  One call at a time: calls and graphs that follow each other may
  *     share it, under any dims it is large enough for
  * Deterministic.  Strides multiples of 8, pointers 16-byte aligned.  Enqueued on `stream`.

@@ -441,7 +441,8 @@ struct PagedAttn {
   float scale_log2e;
   float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, and [slot][key head][row][2]: maximum, sum
   float *ml_few, *ml_tile;
-  unsigned *arrived;               // few-row class: per (slot, key head) runs of a group that have arrived, then groups of a tile; zero between calls
+  float *group_few, *group_ml;     // few-row class: what the runs of a group were joined to, at the group's first run's place
+  unsigned *arrived;               // few-row class: per (slot, key head) runs of a group that have arrived, groups of a tile that have; zero between calls
 };
 
 struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs, few; };
@@ -489,8 +490,16 @@ __device__ __forceinline__ void store_out(const PagedAttn& p, const Item& it, in
   if (p.lse && d4 == 0) p.lse[(long)(it.q0 + token) * p.g.Hq + hq] = log_sum(m, l, p.scale_log2e);
 }
 
-// Sum of up to N partial results of one quad of a row, `step` rows apart, in order: all loads in flight together.
-template <int N>
+// A row's maximum and sum, in memory as one 8-byte word; written and read past the die's L2, where another die's part of the same
+// cache line may be older.
+__device__ __forceinline__ void store_ml(float* ml, long at, float m, float l) {
+  const unsigned long long w = (unsigned long long)__builtin_bit_cast(unsigned, m) | ((unsigned long long)__builtin_bit_cast(unsigned, l) << 32);
+  __hip_atomic_store((unsigned long long*)ml + at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Sum of up to N partial results of one quad of a row, `step` rows apart, in order: all loads in flight together.  SAME_LAUNCH: the
+// parts were written by this launch.
+template <int N, bool SAME_LAUNCH>
 __device__ __forceinline__ void join_quad(const float* part, const float* ml, long at, long step, int count, int d4, float scale_log2e, floatx4* o, float* m, float* l) {
   floatx4 v[N];
   float mm[N], ll[N];
@@ -499,8 +508,10 @@ __device__ __forceinline__ void join_quad(const float* part, const float* ml, lo
     mm[s] = -INFINITY; ll[s] = 0.f;
     v[s] = floatx4{0.f, 0.f, 0.f, 0.f};
     if (s < count) {
-      mm[s] = ml[(at + s * step) * 2];
-      ll[s] = ml[(at + s * step) * 2 + 1];
+      const unsigned long long* w = (const unsigned long long*)ml + at + s * step;
+      const unsigned long long x = SAME_LAUNCH ? __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *w;
+      mm[s] = __builtin_bit_cast(float, (unsigned)x);
+      ll[s] = __builtin_bit_cast(float, (unsigned)(x >> 32));
       v[s] = *(const floatx4*)(part + (at + s * step) * kPagedD + d4);
     }
   }
@@ -523,9 +534,10 @@ __device__ __forceinline__ void join_quad(const float* part, const float* ml, lo
 }
 
 // --------------------------------------------------------------------------------------
-// Few rows (single tokens, a handful of speculated ones): bound by reading K and V once.  A workgroup takes an item; its NW waves
-// take units of 32 keys in turn, each with an LDS ring of its own (two units of K and V, filled by direct-to-LDS loads), so a wave
-// never waits for another.  Per unit and tile of 16 rows:
+// Few rows (single tokens, a handful of speculated ones): bound by reading K and V once.  A workgroup takes an item; its 8 waves
+// take units of 32 keys in turn, each into a place of its own in LDS (K and V of a unit, filled by direct-to-LDS loads), so a wave
+// never waits for another and a compute unit has up to 128 KiB in flight.  (4 waves with two units each have as much: 256 requests of
+// 1000 tokens 182 us against 178, and beside tiles, whose workgroups have 8 waves, a mixed batch 105 against 98.)  Per unit and tile of 16 rows:
 //   S^T[keys, q] = K . Q^T   (16x16x32 matrix instructions; a lane owns one query row and holds 4 keys of each half unit)
 //   online softmax           (over the lane's 8 keys and the 4 lane groups)
 //   O^T[d, q] += V^T . P^T   (P^T straight from the score registers; V^T by transposing LDS reads in the same key order)
@@ -533,13 +545,16 @@ __device__ __forceinline__ void join_quad(const float* part, const float* ml, lo
 // The loads are marked as streaming: every line is read once per call, and kept out of the caches' way 64 requests of 500..8000 tokens
 // (1.05 GB) take 167 us against 188, one of 130000 90 against 101 (6.3 and 5.9 TB/s).
 // --------------------------------------------------------------------------------------
+constexpr int kFewWaves = 8;
 constexpr int kUnit = 32;
 constexpr int kUnitBytes = 2 * kUnit * kPagedD * 2;      // K rows, V rows: 16 KiB
 
+constexpr int kFewLds = kFewWaves * kUnitBytes;
 constexpr int kJoin = 16;                                // runs that one workgroup joins at a time
 
-template <int RT, int NW>
+template <int RT>      // row tiles of 16
 __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it, int head, char* smem) {
+  constexpr int NW = kFewWaves;
   const PagedGeom& g = p.g;
   const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, gr = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -578,8 +593,8 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     pos[u] = first_pos + token;
   }
   const unsigned smem_u = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
-  char* ring = smem + wave * (2 * kUnitBytes);
-  const unsigned ring_u = smem_u + wave * (2 * kUnitBytes);
+  char* st = smem + wave * kUnitBytes;
+  const unsigned st_u = smem_u + wave * kUnitBytes;
   // LDS slot (row, pc) holds 16-byte chunk pc ^ (row % 16) of a K row, pc ^ ((row % 4) << 2) of a V row: conflict-free fragment reads
   const int lr = lane >> 4;
   unsigned koff[4];
@@ -592,7 +607,7 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     return (const char*)uniform64((unsigned long long)(cache + (long)pg * g.page_stride + ((long)head * g.page + row) * kPagedD));
   };
   auto issue = [&](const bf16_t* cache, int i, bool is_k) __attribute__((always_inline)) {
-    const unsigned dst = ring_u + (i & 1) * kUnitBytes + (is_k ? 0 : kUnitBytes / 2);
+    const unsigned dst = st_u + (is_k ? 0 : kUnitBytes / 2);
 #pragma unroll
     for (int half = 0; half < 2; half++) {
       const char* base = half_base(cache, i, half);
@@ -623,24 +638,19 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     for (int dt = 0; dt < 8; dt++) oacc[u][dt] = zero4;
   }
 
-  int valid[2] = {0, 0};
+  // K and V of the next unit are requested as soon as this unit's fragments have left their place, so that behind K of a unit, when it
+  // is needed, its V is on its way, and behind V the next K: 8 loads each
+  int ok = 0, ok_next = 0;       // halves of the unit that have a page
   if (n > 0) {
-    valid[0] = halves_valid(0);
+    ok_next = halves_valid(0);
     issue(p.k_cache, 0, true);
     issue(p.v_cache, 0, false);
-    if (n > 1) {
-      valid[1] = halves_valid(1);
-      issue(p.k_cache, 1, true);
-      issue(p.v_cache, 1, false);
-    }
   }
   for (int i = 0; i < n; i++) {
-    const bool more = i + 2 < n;
-    const char* st = ring + (i & 1) * kUnitBytes;
-    const int v2 = (i & 1) ? valid[1] : valid[0];
+    const bool more = i + 1 < n;
     const int key0 = key_of(i);
-    // K of unit i has landed: newer are V of it, and K and V of the next (8 loads each)
-    if (more) wait_vmcnt<24>(); else wait_vmcnt<0>();
+    ok = ok_next;
+    wait_vmcnt<8>();
     floatx4 c[RT][2];
 #pragma unroll
     for (int hf = 0; hf < 2; hf++)
@@ -651,13 +661,12 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
         for (int u = 0; u < RT; u++) c[u][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[u][s], s == 0 ? zero4 : c[u][hf], 0, 0, 0);
       }
     if (more) {
-      if (((i + 2) & 31) == 0) load_pages(i + 2);
-      const int v = halves_valid(i + 2);
-      if (i & 1) valid[1] = v; else valid[0] = v;
+      if (((i + 1) & 31) == 0) load_pages(i + 1);
+      ok_next = halves_valid(i + 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: their place may be filled again
-      issue(p.k_cache, i + 2, true);
+      issue(p.k_cache, i + 1, true);
     }
-    const bool masked = key0 < clean_lo || key0 + kUnit > clean_hi || v2 != 3;
+    const bool masked = key0 < clean_lo || key0 + kUnit > clean_hi || ok != 3;
     bf16x8 pf[RT];
     float alpha[RT];
     bool rescale = false;
@@ -669,7 +678,7 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
 #pragma unroll
           for (int e = 0; e < 4; e++) {
             const int key = key0 + hf * 16 + gr * 4 + e;
-            if (key > pos[u] || key <= pos[u] - reach || !((v2 >> hf) & 1)) c[u][hf][e] = -INFINITY;
+            if (key > pos[u] || key <= pos[u] - reach || !((ok >> hf) & 1)) c[u][hf][e] = -INFINITY;
           }
       }
       float m = m_run[u];
@@ -701,14 +710,14 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
 #pragma unroll
           for (int e = 0; e < 4; e++) oacc[u][dt][e] *= alpha[u];
     }
-    if (more) wait_vmcnt<24>(); else wait_vmcnt<0>();     // V of unit i
+    if (more) wait_vmcnt<8>(); else wait_vmcnt<0>();     // V of unit i
     // Where some row does not see some key of the unit: rows of V that nobody sees become zero, whatever they hold, and non-finite
     // values of the others are taken out of the product (a zero weight times infinity is not zero) and added below where they are seen.
     unsigned long long odd = 0;
     if (masked) {
       const int row = lane >> 1, key = key0 + row;
-      const bool seen = key < min(it.seq, key_end) && key > first_pos - reach && ((v2 >> (row >> 4)) & 1);
-      char* at = (char*)st + kUnitBytes / 2 + row * 256 + (lane & 1) * 128;
+      const bool seen = key < min(it.seq, key_end) && key > first_pos - reach && ((ok >> (row >> 4)) & 1);
+      char* at = st + kUnitBytes / 2 + row * 256 + (lane & 1) * 128;
       bool any = false;
 #pragma unroll
       for (int c16 = 0; c16 < 8; c16++) {
@@ -753,16 +762,16 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     }
     if (more) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      issue(p.v_cache, i + 2, false);
+      issue(p.v_cache, i + 1, false);
     }
   }
 
   // ---- join the waves: row maxima, then scaled rows, then their sums
-  constexpr int ROWS = RT * 16, PITCH = kPagedD + 4;
-  float* s_o = (float*)smem;                        // [NW][ROWS][PITCH]
-  float* s_ml = s_o + NW * ROWS * PITCH;            // [NW][ROWS][2]
-  static_assert((NW * ROWS * PITCH + NW * ROWS * 2) * 4 <= NW * 2 * kUnitBytes, "the join fits the rings");
-  __syncthreads();                                  // the rings are no longer read
+  constexpr int ROWS = RT * 16, PITCH = kPagedD + 4, NP = NW / 2;      // half of the waves' rows at a time
+  float* s_o = (float*)smem;                        // [NP][ROWS][PITCH]
+  float* s_ml = s_o + NP * ROWS * PITCH;            // [NW][ROWS][2]
+  static_assert((NP * ROWS * PITCH + NW * ROWS * 2 + 1) * 4 <= NW * kUnitBytes, "the join fits");
+  __syncthreads();                                  // the units' places are no longer read
 #pragma unroll
   for (int u = 0; u < RT; u++) {
     l_run[u] += __shfl_xor(l_run[u], 16);
@@ -781,13 +790,25 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     for (int w = 0; w < NW; w++) m = fmaxf(m, s_ml[(w * ROWS + row) * 2]);
     const float f = __builtin_amdgcn_exp2f((m_run[u] - (m == -INFINITY ? 0.f : m)) * p.scale_log2e);
 #pragma unroll
-    for (int dt = 0; dt < 8; dt++) {
-      floatx4 v = oacc[u][dt];
+    for (int dt = 0; dt < 8; dt++)
 #pragma unroll
-      for (int e = 0; e < 4; e++) v[e] *= f;
-      *(floatx4*)(s_o + (wave * ROWS + row) * PITCH + dt * 16 + gr * 4) = v;
-    }
+      for (int e = 0; e < 4; e++) oacc[u][dt][e] *= f;
   }
+  auto each_quad = [&](auto f) {                    // this wave's rows in LDS and in registers
+#pragma unroll
+    for (int u = 0; u < RT; u++)
+#pragma unroll
+      for (int dt = 0; dt < 8; dt++) f((floatx4*)(s_o + ((wave % NP) * ROWS + u * 16 + l15) * PITCH + dt * 16 + gr * 4), oacc[u][dt]);
+  };
+  if (wave >= NP) each_quad([](floatx4* at, floatx4& v) { *at = v; });      // the upper waves' rows, then onto the lower ones'
+  __syncthreads();
+  if (wave < NP)
+    each_quad([](floatx4* at, floatx4& v) {
+      const floatx4 o = *at;
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] += o[e];
+      *at = v;
+    });
   __syncthreads();
   for (int i = tid; i < n_rows * 32; i += NW * 64) {
     const int row = i >> 5, d4 = (i & 31) * 4;
@@ -797,8 +818,9 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     const float ms = m == -INFINITY ? 0.f : m;
     floatx4 o = zero4;
 #pragma unroll
-    for (int w = 0; w < NW; w++) {
-      l += s_ml[(w * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f((s_ml[(w * ROWS + row) * 2] - ms) * p.scale_log2e);
+    for (int w = 0; w < NW; w++) l += s_ml[(w * ROWS + row) * 2 + 1] * __builtin_amdgcn_exp2f((s_ml[(w * ROWS + row) * 2] - ms) * p.scale_log2e);
+#pragma unroll
+    for (int w = 0; w < NP; w++) {
       const floatx4 v = *(const floatx4*)(s_o + (w * ROWS + row) * PITCH + d4);
 #pragma unroll
       for (int e = 0; e < 4; e++) o[e] += v[e];
@@ -807,21 +829,23 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     else {
       const long at = ((long)(it.slot + it.run) * g.Hk + head) * g.rows_few + row;
       store16_device_scope(p.part_few + at * kPagedD + d4, __builtin_bit_cast(u32x4, o));
-      if (d4 == 0) {
-        __hip_atomic_store(p.ml_few + at * 2, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(p.ml_few + at * 2 + 1, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
+      if (d4 == 0) store_ml(p.ml_few, at, m, l);
     }
   }
   if (it.runs == 1) return;
-  // ---- join the runs: the last of every kJoin runs to arrive joins them into the first one's place, the last group to arrive
-  // joins the groups (of one group: into the output).  Always in the order of the runs, so the result does not depend on who is last.
+  // ---- join the runs: the last of every kJoin runs to arrive joins them, the last group to arrive joins the groups (of one group: the
+  // runs go into the output at once).  Always in the order of the runs, so the result does not depend on who is last.
+  // No acquire at device scope, which drops the whole L2 of the die under everybody's loads (32 requests of 2000 tokens in 8 runs each:
+  // 28 us, 15 without).  It is not needed: parts and groups are written through, once a launch, to places of their own in whole cache
+  // lines, and read after their arrival only, so no die can hold an older line of them; maxima and sums, which share lines, are read
+  // past the L2.
   int* s_last = (int*)(s_ml + NW * ROWS * 2);
   const int groups = (it.runs + kJoin - 1) / kJoin;
 #pragma unroll
   for (int level = 0; level < 2; level++) {
     const int first = level == 0 ? it.run & ~(kJoin - 1) : 0, stride = level == 0 ? 1 : kJoin;
     const int count = level == 0 ? min(kJoin, it.runs - first) : groups;
+    const float *part = level == 0 ? p.part_few : p.group_few, *ml = level == 0 ? p.ml_few : p.group_ml;
     unsigned* cnt = p.arrived + ((long)(it.slot + first) * g.Hk + head) * 2 + level;
     wait_all_vmem();                                // this wave's part is where every die sees it
     __syncthreads();
@@ -832,27 +856,19 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     }
     __syncthreads();
     if (!*s_last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
     const bool whole = level == 1 || groups == 1;
     const long step = (long)g.Hk * g.rows_few * stride;
-    for (int i = tid; i < (n_rows * 32 + NW * 64 - 1) / (NW * 64) * (NW * 64); i += NW * 64) {   // (whole rounds: the barrier below)
+    for (int i = tid; i < n_rows * 32; i += NW * 64) {
       const int row = i >> 5, d4 = (i & 31) * 4;
       const long at = ((long)(it.slot + first) * g.Hk + head) * g.rows_few + row;
       floatx4 o = zero4;
       float m = -INFINITY, l = 0.f;
-      if (row < n_rows)
-        for (int s = 0; s < count; s += kJoin) join_quad<kJoin>(p.part_few, p.ml_few, at + s * step, step, min(count - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
-      if (whole) {
-        if (row < n_rows) store_out(p, it, head, row, d4, o, m, l);
-      } else {
-        __syncthreads();                            // the row's maximum and sum have been read by all its quads
-        if (row < n_rows) {
-          store16_device_scope(p.part_few + at * kPagedD + d4, __builtin_bit_cast(u32x4, o));
-          if (d4 == 0) {
-            __hip_atomic_store(p.ml_few + at * 2, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(p.ml_few + at * 2 + 1, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          }
-        }
+      for (int s = 0; s < count; s += kJoin) join_quad<kJoin, true>(part, ml, at + s * step, step, min(count - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
+      if (whole) store_out(p, it, head, row, d4, o, m, l);
+      else {
+        store16_device_scope(p.group_few + at * kPagedD + d4, __builtin_bit_cast(u32x4, o));
+        if (d4 == 0) store_ml(p.group_ml, at, m, l);
       }
     }
     if (whole) return;
@@ -1197,10 +1213,8 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
 
 // --------------------------------------------------------------------------------------
 // Kernels.  A batch that can only have few rows per request (a decode step) takes the first; else one launch holds the items of both
-// classes, tiles first, so that single tokens run beside the chunks; a few-row item then uses four of the eight waves.
+// classes, so that single tokens run beside the chunks.
 // --------------------------------------------------------------------------------------
-constexpr int kFewWaves = 4;
-constexpr int kFewLds = kFewWaves * 2 * kUnitBytes;
 static_assert(kTileLds <= kFewLds && 2 * 2 * kStageBytes + kTileRows * kPagedD * 2 <= kFewLds && kTileRows * kPagedD * 4 <= kFewLds, "one launch, one size");
 
 template <int RT>
@@ -1209,7 +1223,7 @@ __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const Pa
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
   const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);     // (there is room for every idx of the launch)
   if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
-  few_rows_item<RT, kFewWaves>(p, it, head, smem);
+  few_rows_item<RT>(p, it, head, smem);
 }
 
 template <bool FEW>    // FEW: the batch may have few-row items
@@ -1219,7 +1233,7 @@ __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAt
   const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);
   if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
   if (!FEW || !it.few) tile_item(p, it, head, smem);
-  else if (threadIdx.x < kFewWaves * 64) few_rows_item<2, kFewWaves>(p, it, head, smem);
+  else few_rows_item<2>(p, it, head, smem);
 }
 
 // Joins the runs of the cut tiles; all workgroups share them, where a tile's last run alone would read its partial results, 128 KiB a
@@ -1243,7 +1257,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
       const long at = ((long)it.slot * g.Hk + head) * g.rows_tile + r;
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
       float m = -INFINITY, l = 0.f;
-      for (int s = 0; s < it.runs; s += kJoin) join_quad<kJoin>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
+      for (int s = 0; s < it.runs; s += kJoin) join_quad<kJoin, false>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
       store_out(p, it, head, row0 + r, d4, o, m, l);
     }
   }
@@ -1314,7 +1328,7 @@ static int allow_lds(const void* kernel, int which, int device, int bytes) {
   return TL_OK;
 }
 
-struct PagedSizes { size_t schedule, ws, part_few, ml_few, part_tile, ml_tile; };
+struct PagedSizes { size_t schedule, ws, part_few, ml_few, group_few, group_ml, part_tile, ml_tile; };
 
 static PagedSizes paged_sizes(const PagedGeom& g) {
   PagedSizes s;
@@ -1322,7 +1336,9 @@ static PagedSizes paged_sizes(const PagedGeom& g) {
   const size_t few = (size_t)2 * g.side * g.Hk * g.rows_few, tile = (size_t)2 * g.side * g.Hk * g.rows_tile;   // partial rows
   s.part_few = kArrivedBytes;             // (in front: the arrival counters, the same for all dims, so that calls of any may share a workspace)
   s.ml_few = s.part_few + few * kPagedD * 4;
-  s.part_tile = s.ml_few + (few * 8 + 255) / 256 * 256;
+  s.group_few = s.ml_few + (few * 8 + 255) / 256 * 256;
+  s.group_ml = s.group_few + few * kPagedD * 4;
+  s.part_tile = s.group_ml + (few * 8 + 255) / 256 * 256;
   s.ml_tile = s.part_tile + tile * kPagedD * 4;
   s.ws = s.ml_tile + (tile * 8 + 255) / 256 * 256;
   return s;
@@ -1406,8 +1422,9 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   if (q_stride < (long long)g.Hq * kPagedD || o_stride < (long long)g.Hq * kPagedD)
     return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: a row stride is shorter than the row's heads");
   if (q_stride % 8 || o_stride % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_attention: row strides must be multiples of 8 elements");
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) || !aligned16(schedule) || !aligned16(workspace))
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) || !aligned16(schedule))
     return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: device pointers must be 16-byte aligned");
+  if (!aligned128(workspace)) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: workspace must be 128-byte aligned");
   if (!aligned4(block_table) || !aligned4(lse)) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: block_table and lse must be 4-byte aligned");
   const PagedSizes z = paged_sizes(g);
   if (ws_bytes < z.ws) return fail(TL_ERR_WORKSPACE_TOO_SMALL, "tl_paged_attention: workspace of %zu bytes, %zu needed", ws_bytes, z.ws);
@@ -1423,6 +1440,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   char* ws = (char*)workspace;
   p.arrived = (unsigned*)ws;
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
+  p.group_few = (float*)(ws + z.group_few); p.group_ml = (float*)(ws + z.group_ml);
   p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
   hipStream_t s = (hipStream_t)stream;
   auto launch = [&](auto kernel, int which, int grid, int threads, int lds) -> int {
@@ -1431,7 +1449,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
     TL_HIP(hipGetLastError());
     return TL_OK;
   };
-  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, g.cap_few * g.Hk, kFewWaves * 64, kFewWaves * 2 * kUnitBytes);
+  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, g.cap_few * g.Hk, kFewWaves * 64, kFewLds);
   if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, g.rt ? 2 : 3, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
   hipLaunchKernelGGL(paged_join_kernel, dim3(2 * ctx->num_cus), dim3(256), 0, s, p);
   TL_HIP(hipGetLastError());

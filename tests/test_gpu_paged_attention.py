@@ -141,6 +141,30 @@ def test_same_bits_again_and_lse_is_optional():
     assert torch.equal(o.view(torch.int16), o3.view(torch.int16)) and (lse3 == 7).all()
 
 
+def test_many_runs_again_and_again():
+    """Long key axes in so many runs that groups of them are joined first, other queries every time, nothing cleared in between: the
+    joined parts are this call's."""
+    b = Batch([20000, 15000, 900], [1, 1, 1], 4, 1, page=64, seed=18)
+    c = ctx()
+    b.buffers(c)
+    b.schedule_call(c)
+    torch.cuda.synchronize()
+    assert int(b.schedule[1]) > 34
+    for i in range(12):
+        b.qkv[:b.rows] = torch.randn(b.rows, b.q_stride, generator=b.g, device=dev()).to(torch.bfloat16)
+        want = b.reference() if i in (0, 5, 11) else None
+        got = []
+        for _ in range(8):
+            b.o.fill_(7)
+            b.attention_call(c)
+            got.append(b.o.clone())
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.int16), got[0].view(torch.int16)) for x in got)
+        if want is not None:
+            check_attention(b, want)
+    tl.tl_ctx_destroy(c)
+
+
 def test_a_schedule_of_other_dims_is_not_used():
     b = Batch([100, 3], [2, 1], 4, 2, seed=13)
     c = ctx()

@@ -92,7 +92,7 @@ def test_null_and_misaligned_pointers(ctx, name, arg):
     ("slots", ARG, "n_free", dict(n_free=-1)),
     ("schedule", SMALL, "needed", dict(schedule_bytes=64)),
     ("attention", SMALL, "needed", dict(ws_bytes=256)),
-    ("attention", ARG, "scale", dict(scale=0.0)), ("attention", ARG, "scale", dict(scale=float("nan"))), ("attention", ARG, "scale", dict(scale=float("inf"))),
+    ("attention", ARG, "128-byte", dict(workspace=P + 64)), ("attention", ARG, "scale", dict(scale=0.0)), ("attention", ARG, "scale", dict(scale=float("nan"))), ("attention", ARG, "scale", dict(scale=float("inf"))),
     ("attention", ARG, "stride", dict(q_stride=1023)), ("attention", SHAPE, "multiples of 8", dict(o_stride=1028)),
     ("rope", ARG, "positive", dict(T=0)), ("rope", SHAPE, "head_dim", dict(head_dim=64)), ("rope", SHAPE, "rot_dim", dict(rot_dim=24)),
     ("rope", SHAPE, "rot_dim", dict(rot_dim=144)), ("rope", ARG, "eps", dict(eps=-1.0)), ("rope", ARG, "eps", dict(eps=float("nan"))),
