@@ -220,13 +220,13 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   const int tid = threadIdx.x, lane = tid & 63;
   auto add = [](int x, int y) { return x + y; };
   auto top = [](int x, int y) { return max(x, y); };
-  bool bad = false;      // row starts that do not ascend inside the rows: no request can be trusted
+  bool bad = false;      // row starts that do not ascend inside the rows, lengths outside the dims: no request can be trusted
   for (int b = tid; b < g.B; b += NT) {
-    const int lo = p.query_start[b], hi = p.query_start[b + 1];
-    bad |= lo < 0 || hi < lo || hi > g.T;
+    const int lo = p.query_start[b], hi = p.query_start[b + 1], seq = p.seq_lens[b];
+    bad |= lo < 0 || hi < lo || hi > g.T || hi - lo > g.max_new || seq < 0 || seq > g.max_blocks * g.page;
     s_q0[b] = lo;
-    s_n[b] = min(max(hi - lo, 0), g.max_new);
-    s_seq[b] = min(max(p.seq_lens[b], 0), g.max_blocks * g.page);
+    s_n[b] = hi - lo;
+    s_seq[b] = seq;
   }
   if (tid == 0) s_work = 0;
   if (tid < kChunks) s_count[tid] = 0;
@@ -310,8 +310,9 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
 #pragma unroll
   for (int j = 0; j < kChunks; j++) {
     const unsigned long long c = (share * (8 + j) + 7) / 8;
-    chunk_f[j] = max((int)((c + kCostFew - 1) / kCostFew), kMinChunk);
-    chunk_t[j] = max((int)((c + kCostTile - 1) / kCostTile), kMinChunk);
+    const unsigned long long most = 1ull << 24;      // (a key axis has at most 2^22 blocks)
+    chunk_f[j] = max((int)min((c + kCostFew - 1) / kCostFew, most), kMinChunk);
+    chunk_t[j] = max((int)min((c + kCostTile - 1) / kCostTile, most), kMinChunk);
     count[j] = 0;
   }
   auto runs_of = [&](const Tile& t, int cf, int ct) -> int {
@@ -1237,29 +1238,27 @@ __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAt
 }
 
 // Joins the runs of the cut tiles; all workgroups share them, where a tile's last run alone would read its partial results, 128 KiB a
-// run, at one compute unit's pace.  A job is 8 rows of a tile and key head, more where there would be more than two jobs to a workgroup
-// (8 rows against 32: one tile of 32 runs 41 -> 34 us in the whole call; 54 tiles of 2..8 runs 36 -> 41, hence the rule).
+// run, at one compute unit's pace.  A job is 8 rows of a tile and key head, a thread has one quad, and four runs at a time keep the
+// registers few enough for eight workgroups a compute unit: a mixed batch with 23 cut tiles 95 us in the whole call with 16 runs at a time
+// and up to 64 rows a job, 90 like this.
+constexpr int kTileJoin = 4, kJoinRows = 8;
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
   const PagedGeom& g = p.g;
   if (p.schedule[0] != (int)g.key) return;
-  const int cuts = p.schedule[2] * g.Hk;
-  int rows = 8;
-  while (rows < 64 && cuts * (kTileRows / rows) > 2 * (int)gridDim.x) rows *= 2;
-  const int parts = (g.rows_tile + rows - 1) / rows, jobs = cuts * parts;
+  const int parts = (g.rows_tile + kJoinRows - 1) / kJoinRows, jobs = p.schedule[2] * g.Hk * parts;
+  const long step = (long)g.Hk * g.rows_tile;
   for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts, r0 = (rest - head * parts) * rows;
+    const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts;
     const Item it = load_item(p.schedule + g.sched_items + (long)p.schedule[kSchedHeader + cut] * kItemInts);
     const int row0 = it.tile * kTileRows, n = min(it.n * g.G - row0, kTileRows);
-    const long step = (long)g.Hk * g.rows_tile;
-    for (int i = threadIdx.x; i < rows * 32; i += 256) {
-      const int r = r0 + (i >> 5), d4 = (i & 31) * 4;
-      if (r >= n) break;
-      const long at = ((long)it.slot * g.Hk + head) * g.rows_tile + r;
-      floatx4 o = {0.f, 0.f, 0.f, 0.f};
-      float m = -INFINITY, l = 0.f;
-      for (int s = 0; s < it.runs; s += kJoin) join_quad<kJoin, false>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, kJoin), d4, p.scale_log2e, &o, &m, &l);
-      store_out(p, it, head, row0 + r, d4, o, m, l);
-    }
+    const int r = (rest - head * parts) * kJoinRows + (threadIdx.x >> 5), d4 = (threadIdx.x & 31) * 4;
+    if (r >= n) continue;
+    const long at = ((long)it.slot * g.Hk + head) * g.rows_tile + r;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    for (int s = 0; s < it.runs; s += kTileJoin)
+      join_quad<kTileJoin, false>(p.part_tile, p.ml_tile, at + s * step, step, min(it.runs - s, kTileJoin), d4, p.scale_log2e, &o, &m, &l);
+    store_out(p, it, head, row0 + r, d4, o, m, l);
   }
 }
 
@@ -1400,13 +1399,15 @@ int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims, const int* query_s
   if (schedule_bytes < z.schedule) return fail(TL_ERR_WORKSPACE_TOO_SMALL, "tl_paged_schedule: schedule of %zu bytes, %zu needed", schedule_bytes, z.schedule);
   if (int e = check_paged_launch(ctx, "tl_paged_schedule")) return e;
   const SchedParams p = {query_start, seq_lens, schedule, g};
-  const long most = g.cap_tile > g.B ? g.cap_tile : g.B;
+  // tiles of both classes at most: up to 64 in one wave (B = 64: 6.3 us against 7.3 with four), up to 256 in four (8 prompt chunks and 40 single tokens:
+  // 8.6 against 12.2 with one and 9.7 with sixteen), more in sixteen (1000 requests: 10.9 against 16.1 with four)
+  const int most = g.B + (g.has_tiles ? g.cap_tile - g.side : 0);
   auto launch = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
     hipLaunchKernelGGL(paged_schedule_kernel<NT>, dim3(1), dim3(NT), 0, (hipStream_t)stream, p);
   };
-  if (most <= 128) launch(std::integral_constant<int, 64>{});
-  else if (most <= 512) launch(std::integral_constant<int, 256>{});
+  if (most <= 64) launch(std::integral_constant<int, 64>{});
+  else if (most <= 256) launch(std::integral_constant<int, 256>{});
   else launch(std::integral_constant<int, 1024>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
@@ -1418,7 +1419,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   PagedGeom g;
   if (int e = resolve_paged(ctx, dims, &g)) return e;
   if (!q || !k_cache || !v_cache || !block_table || !schedule || !o || !workspace) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: null pointer argument");
-  if (!(scale > 0.f) || scale > 3.0e38f) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: scale must be positive and finite");
+  if (!(scale > 0.f) || !(scale * 1.4426950408889634f < __builtin_inff())) return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: scale must be positive and finite");
   if (q_stride < (long long)g.Hq * kPagedD || o_stride < (long long)g.Hq * kPagedD)
     return fail(TL_ERR_INVALID_ARG, "tl_paged_attention: a row stride is shorter than the row's heads");
   if (q_stride % 8 || o_stride % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_attention: row strides must be multiples of 8 elements");
@@ -1451,7 +1452,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   };
   if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, g.cap_few * g.Hk, kFewWaves * 64, kFewLds);
   if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, g.rt ? 2 : 3, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
-  hipLaunchKernelGGL(paged_join_kernel, dim3(2 * ctx->num_cus), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(paged_join_kernel, dim3(8 * ctx->num_cus), dim3(256), 0, s, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }

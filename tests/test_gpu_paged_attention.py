@@ -181,22 +181,63 @@ def test_a_schedule_of_other_dims_is_not_used():
     tl.tl_ctx_destroy(c)
 
 
-def test_lengths_that_make_no_sense_stay_in_bounds():
-    """Row starts that do not ascend and lengths outside the table: the schedule keeps to its room and to the rows."""
-    b = Batch([100, 3, 50], [2, 1, 40], 4, 2, seed=14, max_new=0)
+@pytest.mark.parametrize("what", ["below zero", "beyond the rows", "not ascending", "more than max_new", "seq below zero", "seq beyond the table"])
+def test_lengths_that_make_no_sense_make_an_empty_table(what):
+    b = Batch([100, 3, 50], [2, 1, 40], 4, 2, seed=14)
     c = ctx()
-    z = b.buffers(c)
-    b.start_d = ints([-5, b.T + 50, 0, 2 ** 31 - 1])
-    b.seq_d = ints([2 ** 31 - 1, -7, 50])
-    b.table_d.clamp_(max=b.n_pages - 1)
+    b.buffers(c)
     guard = torch.full((b.schedule.numel() + 4096,), -1, dtype=torch.int32, device=dev())
     b.schedule = guard[:b.schedule.numel()]
+    change = {"below zero": (b.start_d, 0, -1), "beyond the rows": (b.start_d, 3, b.T + 1), "not ascending": (b.start_d, 1, 10), "more than max_new": (b.start_d, 2, 2),
+              "seq below zero": (b.seq_d, 2, -1), "seq beyond the table": (b.seq_d, 0, b.width * b.page + 1)}[what]
+    change[0][change[1]] = change[2]
     b.schedule_call(c)
     b.attention_call(c)
     torch.cuda.synchronize()
-    assert (guard[b.schedule.numel():] == -1).all()
-    assert 0 <= int(b.schedule[1]) <= z["few_items"] + z["tile_items"]
+    assert (guard[16:] == -1).all() and int(guard[1]) == 0
+    assert (b.o == 7).all() and (b.lse == 7).all()
     tl.tl_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("B,n", [(1000, 1), (3, 5000), (300, 20)])
+def test_schedules_of_every_size(B, n):
+    """Every tile's keys are covered once, runs of a tile in order and of one tile together, longest items first, inside the room."""
+    rng = np.random.default_rng(B)
+    new = [int(x) for x in rng.integers(1, n + 1, B)]
+    seq = [int(x) + m for x, m in zip(rng.integers(0, 9000, B), new)]
+    start = np.concatenate([[0], np.cumsum(new)])
+    c = ctx()
+    G, page, width = 4, 64, 256
+    d = tl.tl_paged_dims(batch=B, max_tokens=int(start[-1]), max_new=max(new), max_blocks=width, page_size=page, n_pages=1000, heads_q=4 * G, heads_kv=4, head_dim=D)
+    z = tl.tl_paged_query(c, d)
+    out = torch.full((z["schedule_bytes"] // 4 + 64,), -1, dtype=torch.int32, device=dev())
+    tl.tl_paged_schedule(c, d, ints(start), ints(seq), out, z["schedule_bytes"])
+    torch.cuda.synchronize()
+    tl.tl_ctx_destroy(c)
+    out = out.cpu().numpy()
+    assert (out[z["schedule_bytes"] // 4:] == -1).all()
+    items, cuts = out[1], out[2]
+    assert 0 < items <= z["few_items"] + z["tile_items"]
+    first = 16 + -(-z["side_by_side"] // 4) * 4
+    rec = out[first:first + 12 * items].reshape(items, 12)
+    seen, lengths = {}, []
+    for b, q0, m, s, tile, k0, k1, slot, run, runs, few, _ in rec:
+        assert (q0, m, s) == (start[b], new[b], seq[b]) and few == (m * G <= 32) and (not few or tile == 0)
+        seen.setdefault((b, tile), []).append((run, runs, k0, k1, slot))
+        lengths.append((k1 - k0) * (3 if few else 8))
+    for b in range(B):
+        for tile in range(-(-new[b] * G // 256) if new[b] * G > 32 else 1):
+            r = sorted(seen.pop((b, tile)))
+            last = min((tile * 256 + 255) // G, new[b] - 1) if new[b] * G > 32 else new[b] - 1
+            assert [x[0] for x in r] == list(range(r[0][1])) and len({x[4] for x in r}) == 1
+            assert r[0][2] == 0 and r[-1][3] == -(-(seq[b] - new[b] + last + 1) // 64) and all(x[3] == y[2] for x, y in zip(r, r[1:]))
+    assert not seen
+    step = max(lengths) / 64 + 9                       # a bucket and the rounding of runs of one tile
+    assert all(x >= y - step for x, y in zip(lengths, lengths[1:]))
+    cut_tiles = {(b, t) for b, _, _, _, t, _, _, _, _, runs, few, _ in rec if runs > 1 and not few}
+    assert cuts == len(cut_tiles) and {tuple(rec[i][[0, 4]]) for i in out[16:16 + cuts]} == cut_tiles
+    slots = [(few, slot + run) for _, _, _, _, _, _, _, slot, run, runs, few, _ in rec if runs > 1]
+    assert len(set(slots)) == len(slots) and all(x < 2 * z["side_by_side"] for _, x in slots)
 
 
 def test_captured_and_replayed_with_other_lengths():
