@@ -53,10 +53,9 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
   const int t = (int)(task / p.groups), h0 = (int)(task - (long)t * p.groups) * kHeads;
   if (t >= p.T) return;   // (whole rows of lanes)
   const int l = threadIdx.x & 15;
+  // (position, slot and heads are on their way together; a row that is left out has been read for nothing)
   const int pos = p.rot ? p.positions[t] : 0;
   const int slot = CACHE ? p.slots[t] : 0;
-  if (p.rot && (unsigned)pos >= (unsigned)p.max_position) return;
-  if (CACHE && (unsigned)slot >= (unsigned)p.n_slots) return;
   u32x4 raw[kHeads];
 #pragma unroll
   for (int i = 0; i < kHeads; i++) {
@@ -67,6 +66,8 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
                                           : p.v + t * p.v_stride + (long)(h - p.Hq - p.Hk) * kPagedD;
     raw[i] = *(const u32x4*)(src + l * 8);
   }
+  if (p.rot && (unsigned)pos >= (unsigned)p.max_position) return;
+  if (CACHE && (unsigned)slot >= (unsigned)p.n_slots) return;
   // the lane's angles.  Halves: elements l*8.. of the first half meet those of lane l + rot/16; neighbours: pairs l*4..
   const int half = p.rot >> 1, hl = p.rot >> 4;
   const bool turns = l * 8 < p.rot;
