@@ -440,6 +440,7 @@ struct PagedAttn {
   float* lse;               // [T, Hq] or null
   long q_stride, o_stride;
   float scale_log2e;
+  float lazy;               // tiles: how far, in scores, a row's maximum may leave the exponents' reference: 2^8 in weights
   float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, and [slot][key head][row][2]: maximum, sum
   float *ml_few, *ml_tile;
   float *group_few, *group_ml;     // few-row class: what the runs of a group were joined to, at the group's first run's place
@@ -1013,7 +1014,7 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
   floatx16 oacc[4];
 #pragma unroll
   for (int dt = 0; dt < 4; dt++) oacc[dt] = zero16;
-  float m_run = -INFINITY, l_run = 0.f, m_blk;
+  float m_run = -INFINITY, l_run = 0.f, mc = 0.f, m_blk;
 
   auto block_max = [&](const floatx16 (&sc)[2]) __attribute__((always_inline)) -> float {
     float m = -INFINITY;
@@ -1078,19 +1079,23 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
           }
         m_blk = block_max(c);
       }
+      // The exponents' reference m_run follows the row's maximum only where that has left it by more than 2^8: up to there weights stay
+      // below 256, which fp32 sums and bf16 weights hold as exactly as those below 1, and O needs no rescaling.  (It follows at once
+      // from -inf, and the comparison is false for NaN.)
       const float m_new = fmaxf(m_run, m_blk);
-      const float ms = m_new == -INFINITY ? 0.f : m_new;     // nothing seen so far: every exponent below is -inf
-      const float alpha = __builtin_amdgcn_exp2f((m_run - ms) * p.scale_log2e);
-      m_run = m_new;
-      const float mc = -ms * p.scale_log2e;
-      if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+      const bool grown = !(m_new - m_run <= p.lazy);
+      if (__builtin_amdgcn_ballot_w64(grown)) {
+        const float ms = m_new == -INFINITY ? 0.f : m_new;     // nothing seen so far: every exponent below is -inf
+        const float alpha = grown ? __builtin_amdgcn_exp2f((m_run - ms) * p.scale_log2e) : 1.f;
+        if (grown) { m_run = m_new; mc = -ms * p.scale_log2e; }
+        l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; dt++)
 #pragma unroll
           for (int e = 0; e < 16; e++) oacc[dt][e] *= alpha;
       }
       bf16x8 pf[4];
-      float psum = 0.f, m_part = -INFINITY, m_next = -INFINITY;
+      float m_part = -INFINITY, m_next = -INFINITY;
       static_for<0, 32>([&](auto s_c) {
         constexpr int f = decltype(s_c)::value;
         if constexpr (f + RD < 16) fr[(f + RD) % RN] = kread(kb, f + RD);
@@ -1114,12 +1119,11 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
             constexpr int gq = y / 8, i = y % 8;
             const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(c[gq >> 1][(gq & 1) * 8 + i], p.scale_log2e, mc));
             pf[gq][i] = (bf16_t)pv;
-            psum += pv;
+            l_run += pv;
           }
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      l_run = l_run * alpha + psum;
       m_blk = m_next;
     }
     const int st_free = st_cur;
@@ -1438,6 +1442,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.o = (bf16_t*)o; p.lse = lse;
   p.q_stride = q_stride; p.o_stride = o_stride;
   p.scale_log2e = scale * 1.4426950408889634f;
+  p.lazy = 8.f / p.scale_log2e < 3.0e38f ? 8.f / p.scale_log2e : 3.0e38f;
   char* ws = (char*)workspace;
   p.arrived = (unsigned*)ws;
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
