@@ -631,11 +631,11 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
 
   floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
   floatx4 oacc[RT][8];
-  float m_run[RT], l_run[RT];
+  float m_run[RT], l_run[RT], mc[RT];
 #pragma unroll
   for (int u = 0; u < RT; u++) {
     m_run[u] = -INFINITY;
-    l_run[u] = 0.f;
+    l_run[u] = mc[u] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < 8; dt++) oacc[u][dt] = zero4;
   }
@@ -670,8 +670,8 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
     }
     const bool masked = key0 < clean_lo || key0 + kUnit > clean_hi || ok != 3;
     bf16x8 pf[RT];
-    float alpha[RT];
-    bool rescale = false;
+    bool grown = false;
+    float top[RT];                 // of this lane's 8 scores
 #pragma unroll
     for (int u = 0; u < RT; u++) {
       if (masked) {
@@ -683,35 +683,38 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
             if (key > pos[u] || key <= pos[u] - reach || !((ok >> hf) & 1)) c[u][hf][e] = -INFINITY;
           }
       }
-      float m = m_run[u];
+      top[u] = fmaxf(c[u][0][0], c[u][1][0]);
 #pragma unroll
-      for (int e = 0; e < 4; e++) m = fmaxf(fmaxf(m, c[u][0][e]), c[u][1][e]);
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      const float ms = m == -INFINITY ? 0.f : m;         // nothing seen so far: every exponent below is -inf
-      alpha[u] = __builtin_amdgcn_exp2f((m_run[u] - ms) * p.scale_log2e);
-      rescale |= alpha[u] != 1.f;
-      m_run[u] = m;
-      const float mc = -ms * p.scale_log2e;
-      float sum = 0.f;
+      for (int e = 1; e < 4; e++) top[u] = fmaxf(fmaxf(top[u], c[u][0][e]), c[u][1][e]);
+      grown |= !(top[u] - m_run[u] <= p.lazy);
+    }
+    if (__builtin_amdgcn_ballot_w64(grown)) {
+      // some row's maximum has left its exponents' reference by more than 2^8 (see the tiles): the row's four lanes follow together
+#pragma unroll
+      for (int u = 0; u < RT; u++) {
+        float m = fmaxf(top[u], __shfl_xor(top[u], 16));
+        m = fmaxf(m_run[u], fmaxf(m, __shfl_xor(m, 32)));
+        const bool row = !(m - m_run[u] <= p.lazy);
+        const float ms = m == -INFINITY ? 0.f : m;         // nothing seen so far: every exponent below is -inf
+        const float alpha = row ? __builtin_amdgcn_exp2f((m_run[u] - ms) * p.scale_log2e) : 1.f;
+        if (row) { m_run[u] = m; mc[u] = -ms * p.scale_log2e; }
+        l_run[u] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 8; dt++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) oacc[u][dt][e] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < RT; u++)
 #pragma unroll
       for (int hf = 0; hf < 2; hf++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(c[u][hf][e], p.scale_log2e, mc));
+          const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(c[u][hf][e], p.scale_log2e, mc[u]));
           pf[u][hf * 4 + e] = (bf16_t)pv;
-          sum += pv;
+          l_run[u] += pv;
         }
-      l_run[u] = l_run[u] * alpha[u] + sum;
-    }
-    if (__builtin_amdgcn_ballot_w64(rescale)) {
-#pragma unroll
-      for (int u = 0; u < RT; u++)
-#pragma unroll
-        for (int dt = 0; dt < 8; dt++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) oacc[u][dt][e] *= alpha[u];
-    }
     if (more) wait_vmcnt<8>(); else wait_vmcnt<0>();     // V of unit i
     // Where some row does not see some key of the unit: rows of V that nobody sees become zero, whatever they hold, and non-finite
     // values of the others are taken out of the product (a zero weight times infinity is not zero) and added below where they are seen.
@@ -1020,7 +1023,7 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
     float m = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; e++) m = raw_max(raw_max(m, sc[0][e]), sc[1][e]);
-    return halves_max(m);
+    return m;
   };
   auto sees = [&](int key) __attribute__((always_inline)) -> bool { return key <= q_pos && key > q_pos - reach; };
 
@@ -1082,9 +1085,9 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
       // The exponents' reference m_run follows the row's maximum only where that has left it by more than 2^8: up to there weights stay
       // below 256, which fp32 sums and bf16 weights hold as exactly as those below 1, and O needs no rescaling.  (It follows at once
       // from -inf, and the comparison is false for NaN.)
-      const float m_new = fmaxf(m_run, m_blk);
-      const bool grown = !(m_new - m_run <= p.lazy);
-      if (__builtin_amdgcn_ballot_w64(grown)) {
+      if (__builtin_amdgcn_ballot_w64(!(m_blk - m_run <= p.lazy))) {
+        const float m_new = fmaxf(m_run, halves_max(m_blk));   // (m_blk: of the lane's own half of the keys)
+        const bool grown = !(m_new - m_run <= p.lazy);
         const float ms = m_new == -INFINITY ? 0.f : m_new;     // nothing seen so far: every exponent below is -inf
         const float alpha = grown ? __builtin_amdgcn_exp2f((m_run - ms) * p.scale_log2e) : 1.f;
         if (grown) { m_run = m_new; mc = -ms * p.scale_log2e; }
@@ -1095,7 +1098,7 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
           for (int e = 0; e < 16; e++) oacc[dt][e] *= alpha;
       }
       bf16x8 pf[4];
-      float m_part = -INFINITY, m_next = -INFINITY;
+      float m_next = -INFINITY;
       static_for<0, 32>([&](auto s_c) {
         constexpr int f = decltype(s_c)::value;
         if constexpr (f + RD < 16) fr[(f + RD) % RN] = kread(kb, f + RD);
@@ -1110,9 +1113,8 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
         if constexpr (f >= 18 && f < 22) {
           constexpr int q = f - 18;
 #pragma unroll
-          for (int e = q * 4; e < q * 4 + 4; e++) m_part = raw_max3(m_part, n[0][e], n[1][e]);
+          for (int e = q * 4; e < q * 4 + 4; e++) m_next = raw_max3(m_next, n[0][e], n[1][e]);
         }
-        if constexpr (f == 23) m_next = halves_max(m_part);
         static_for<0, 32>([&](auto y_c) {
           constexpr int y = decltype(y_c)::value;
           if constexpr (y * 7 / 8 == f) {
