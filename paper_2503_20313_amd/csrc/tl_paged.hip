@@ -305,7 +305,9 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     work = s_work;
   }
   // ---- the chunk lengths, in blocks
-  const unsigned long long share = (work + g.side - 1) / g.side;
+  // (divisions are 32 bits wide wherever the numbers are: together 0.3 us)
+  const unsigned long long up = work + (unsigned)(g.side - 1);
+  const unsigned long long share = (up >> 32) ? up / (unsigned)g.side : (unsigned)up / (unsigned)g.side;
   int chunk_f[kChunks], chunk_t[kChunks], count[kChunks];
 #pragma unroll
   for (int j = 0; j < kChunks; j++) {
@@ -356,7 +358,8 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
     __syncthreads();
     longest = s_long;
   }
-  auto bucket_of = [&](const Tile& t, int n) -> int { return kBuckets - 1 - (int)((long)item_cost(t, n) * kBuckets / (longest + 1)); };
+  const float per_cost = (float)kBuckets / ((float)longest + 1.f);
+  auto bucket_of = [&](const Tile& t, int n) -> int { return kBuckets - 1 - min((int)((float)item_cost(t, n) * per_cost), kBuckets - 1); };
   for (int i = tid; i < n_all; i += NT) {
     Tile t;
     if (!tile_of(i, &t)) continue;
@@ -412,7 +415,8 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
       if (r < all) {
         int* rec = items + (long)(oto + s) * kItemInts;       // (below the number of items there is room for: see resolve_paged)
         const u32x4 q0 = {(unsigned)ob, (unsigned)s_q0[ob], (unsigned)s_n[ob], (unsigned)s_seq[ob]};
-        const u32x4 q1 = {(unsigned)ot, (unsigned)(olo + (int)((long)(ohi - olo) * s / oc)), (unsigned)(olo + (int)((long)(ohi - olo) * (s + 1) / oc)), (unsigned)oslot};
+        const unsigned len = (unsigned)(ohi - olo);                 // (at most 2^22 blocks, in fewer than 2^10 runs)
+        const u32x4 q1 = {(unsigned)ot, (unsigned)olo + len * (unsigned)s / (unsigned)oc, (unsigned)olo + len * (unsigned)(s + 1) / (unsigned)oc, (unsigned)oslot};
         const u32x4 q2 = {(unsigned)s, (unsigned)oc, (unsigned)of, 0};
         *(u32x4*)rec = q0;
         *(u32x4*)(rec + 4) = q1;
