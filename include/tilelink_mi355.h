@@ -442,7 +442,7 @@ typedef struct tl_paged_dims {
 
 /* Sizes for `dims` (host call): bytes of `schedule` and of the attention's workspace; info[0..7] = query rows of a tile, rows up to
  * which a request counts as few, keys per block, items of the few-row class and of the tile class per key head at most, items
- * per key head that run side by side, max_tokens, query heads per key head. */
+ * per key head that run side by side, blocks of a cut key axis's run at least, query heads per key head. */
 int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims /*host*/, size_t* schedule_bytes /*host*/, size_t* ws_bytes /*host*/,
                    int* info /*host, 8 ints*/);
 

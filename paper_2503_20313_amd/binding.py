@@ -298,7 +298,7 @@ def _paged(dims):
 def tl_paged_query(ctx, dims):
     sched, ws, info = _sz(), _sz(), (_i * 8)()
     _check(_lib.tl_paged_query(ctx, _paged(dims), ctypes.byref(sched), ctypes.byref(ws), info))
-    keys = ("tile_rows", "few_rows", "block_keys", "few_items", "tile_items", "side_by_side", "max_tokens", "group")
+    keys = ("tile_rows", "few_rows", "block_keys", "few_items", "tile_items", "side_by_side", "run_blocks", "group")
     return dict(zip(keys, list(info)), schedule_bytes=sched.value, ws_bytes=ws.value)
 
 

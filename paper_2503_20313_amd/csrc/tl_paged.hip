@@ -1366,7 +1366,7 @@ int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims, size_t* schedul
   const PagedSizes s = paged_sizes(g);
   *schedule_bytes = s.schedule;
   *ws_bytes = s.ws;
-  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.side, g.T, g.G};
+  const int v[8] = {kTileRows, g.rt ? kFewRows : 0, kBlk, g.cap_few, g.cap_tile, g.side, kMinChunk, g.G};
   memcpy(info, v, sizeof v);
   return TL_OK;
 }

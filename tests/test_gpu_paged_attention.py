@@ -62,6 +62,34 @@ def test_cut_key_axis(heads, cached, new):
     check_attention(b)
 
 
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_cut_key_axis_in_a_window(new):
+    b = Batch([9000, 100], [new, 1], 4, 1, page=16, window=5000, seed=19)
+    b.run()
+    check_attention(b)
+
+
+def test_largest_batch():
+    """4096 requests, the most there can be, of one token each."""
+    rng = np.random.default_rng(20)
+    b = Batch([int(x) for x in rng.integers(0, 40, 4096)], [1] * 4096, 2, 1, page=16, seed=20)
+    b.run()
+    check_attention(b)
+
+
+def test_many_heads():
+    b = Batch([70, 5, 200], [1, 2, 40], 384, 128, page=16, seed=21)
+    b.run()
+    check_attention(b)
+
+
+def test_very_long_request():
+    """300000 keys: runs of hundreds of blocks, tables of thousands of pages, pages looked up again and again."""
+    b = Batch([300000], [2], 2, 1, page=16, seed=22)
+    b.run()
+    check_attention(b)
+
+
 def test_tokens_without_any_key():
     """More new tokens than the sequence has: the first ones have no position and see nothing."""
     b = Batch([0, 0, 0], [3, 40, 1], 4, 2, seq_lens=[1, 17, 0], seed=6)
