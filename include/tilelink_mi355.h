@@ -471,7 +471,7 @@ int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* c
  *   y = x / sqrt(mean(x^2) + eps) * weight  per head;  then for every pair (i, j) of the first rot_dim elements
  *   (y_i, y_j) -> (y_i cos - y_j sin, y_j cos + y_i sin),  (i, j) = (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0.
  *   q dev [T rows of heads_q*128], k dev [T rows of heads_kv*128] bf16, rows q_stride / k_stride elements apart (a packed
- *     projection's rows can be taken where they lie); q_out, k_out likewise (written; may be q and k themselves)
+ *     projection's rows can be taken where they lie); q_out, k_out likewise (written; may be q and k themselves, with their strides)
  *   q_weight, k_weight dev bf16[128], both or neither (NULL: no norm);  positions dev int[T]
  *   cos_sin dev fp32 [max_position, rot_dim]: cosines of the rot_dim/2 angles of a position, then their sines
  *   rot_dim a multiple of 16 up to 128; 0 = no rotation (positions and cos_sin may be NULL)
@@ -485,7 +485,7 @@ int tl_qk_norm_rope(tl_ctx* ctx, const void* q /*dev*/, long long q_stride, cons
 
 /* The same for the max_tokens rows of a step, with keys, and values as they are, stored in the cache at slots[row] (dev int
  * [max_tokens], from tl_paged_slots).  A row whose slot is outside [0, n_pages*page_size), such as -1, is padding: nothing of it
- * is written, q_out included.  Two rows with one slot leave either's key and value there. */
+ * is written, q_out included.  Of two rows with one slot either's key and value, or parts of both, may be there afterwards. */
 int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const void* q /*dev*/, long long q_stride, const void* k /*dev*/,
                           long long k_stride, const void* v /*dev*/, long long v_stride, void* q_out /*dev*/, long long q_out_stride, void* k_cache /*dev*/,
                           void* v_cache /*dev*/, const int* slots /*dev*/, const void* q_weight /*dev*/, const void* k_weight /*dev*/, float eps,

@@ -138,6 +138,12 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
   }
 }
 
+// In place every row lies where it lay: with another stride a row would be written over one that is still to be read.
+static int check_in_place(const char* what, const char* name, const void* in, long long in_stride, const void* out, long long out_stride, int T) {
+  if (in == out && in_stride != out_stride && T > 1) return fail(TL_ERR_INVALID_ARG, "%s: %s in place has one row stride, not two", what, name);
+  return TL_OK;
+}
+
 static int check_rope(const char* what, const void* q, long long q_stride, const void* k, long long k_stride, const void* q_out, long long qo_stride, int T,
                       int Hq, int Hk, int head_dim, const void* wq, const void* wk, float eps, const int* positions, const float* cos_sin, int max_position,
                       int rot_dim) {
@@ -155,7 +161,7 @@ static int check_rope(const char* what, const void* q, long long q_stride, const
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(wq) || !aligned16(wk) || !aligned16(cos_sin))
     return fail(TL_ERR_INVALID_ARG, "%s: device pointers must be 16-byte aligned", what);
   if (!aligned4(positions)) return fail(TL_ERR_INVALID_ARG, "%s: positions must be 4-byte aligned", what);
-  return TL_OK;
+  return check_in_place(what, "q", q, q_stride, q_out, qo_stride, T);
 }
 
 static RopeParams rope_params(const void* q, long long q_stride, const void* k, long long k_stride, void* q_out, long long qo_stride, int T, int Hq, int Hk,
@@ -203,6 +209,7 @@ int tl_qk_norm_rope(tl_ctx* ctx, const void* q, long long q_stride, const void* 
   if (k_out_stride < (long long)heads_kv * kPagedD) return fail(TL_ERR_INVALID_ARG, "%s: a row stride is shorter than the row's heads", what);
   if (k_out_stride % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: row strides must be multiples of 8 elements", what);
   if (!aligned16(k_out)) return fail(TL_ERR_INVALID_ARG, "%s: device pointers must be 16-byte aligned", what);
+  if (int e = check_in_place(what, "k", k, k_stride, k_out, k_out_stride, T)) return e;
   if (int e = check_paged_launch(ctx, what)) return e;
   RopeParams p = rope_params(q, q_stride, k, k_stride, q_out, q_out_stride, T, heads_q, heads_kv, heads_q + heads_kv, q_weight, k_weight, eps, positions,
                              cos_sin, max_position, rot_dim, interleaved);

@@ -110,6 +110,17 @@ def test_no_rotation_and_no_norm_are_right_calls(ctx):
     refused(ARG, "tl_ctx_create_host", slots_call(free_pages=None, n_free=0), ctx)
 
 
+def test_in_place_has_one_stride(ctx):
+    """Another stride in place would write rows over rows that are still to be read; a single row has none."""
+    for call in (rope_call, cache_call):
+        refused(ARG, "in place", call(q_stride=2048), ctx)
+        refused(ARG, "in place", call(q_out_stride=1032), ctx)
+        refused(ARG, "tl_ctx_create_host", call(q_stride=2048, q_out_stride=2048), ctx)
+        refused(ARG, "tl_ctx_create_host", call(q_stride=2048, q_out=2 * P), ctx)
+    refused(ARG, "in place", rope_call(k_out_stride=512), ctx)
+    refused(ARG, "tl_ctx_create_host", rope_call(q_stride=2048, k_stride=512, T=1), ctx)
+
+
 def test_sizes(ctx):
     """What the query asks for is what the calls accept, and grows with the batch; a decode step needs no room for tiles."""
     for kw in (dict(), dict(max_new=1), dict(heads_q=64, heads_kv=1), dict(batch=4096, max_tokens=1 << 18, max_new=0), dict(heads_q=1024, heads_kv=1024),
