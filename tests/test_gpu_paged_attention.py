@@ -110,6 +110,16 @@ def test_missing_pages(new):
     assert (b.o[new[0]:new[0] + new[1], :8 * D] == 0).all()
 
 
+@pytest.mark.parametrize("window", [0, 90])
+def test_pages_in_several_places(window):
+    """Requests with a common beginning list the same pages, and one page stands twice in a table: tables are only read."""
+    b = Batch([160, 160, 160, 96], [1, 40, 3, 40], 8, 2, page=32, window=window, seed=31)
+    b.table[1, :5] = b.table[2, :5] = b.table[0, :5]
+    b.table[3, 2] = b.table[3, 1]
+    b.run()
+    check_attention(b)
+
+
 def test_strides():
     """Pages that lie apart, as where the caches of several layers share a buffer."""
     b = Batch([90, 31], [20, 1], 4, 2, page=32, page_stride=2 * 32 * D * 3 + 64, seed=8)
