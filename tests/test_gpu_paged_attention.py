@@ -110,6 +110,15 @@ def test_missing_pages(new):
     assert (b.o[new[0]:new[0] + new[1], :8 * D] == 0).all()
 
 
+@pytest.mark.parametrize("heads,max_new", [((4, 2), 1), ((4, 2), 60), ((40, 1), 1)], ids=str)
+def test_nothing_new(heads, max_new):
+    """A step in which no request has a new token: no item, no row written."""
+    b = Batch([50, 0, 3000], [0, 0, 0], *heads, max_new=max_new, spare_rows=60, seed=32)
+    b.run()
+    assert b.schedule[1:3].tolist() == [0, 0]
+    check_attention(b)
+
+
 @pytest.mark.parametrize("window", [0, 90])
 def test_pages_in_several_places(window):
     """Requests with a common beginning list the same pages, and one page stands twice in a table: tables are only read."""
