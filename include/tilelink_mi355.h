@@ -493,7 +493,7 @@ int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const
 
 /* The work table of tl_paged_attention, from query_start [batch+1] and seq_lens [batch] (dev; as tl_paged_slots writes them): the
  * requests' query tiles, and the runs into which long key axes are cut so that all compute units have work.  It serves every
- * layer of the step that has the same dims; under other dims the attention finds no work in it and writes nothing.  Row starts that
+ * layer of the step that has the same dims (page_stride may differ); under any others the attention finds no work in it and writes nothing.  Row starts that
  * do not ascend inside [0, max_tokens], a request with more than max_new rows, or a length outside [0, max_blocks*page_size] make an
  * empty table, under which nothing is written either.
  *   schedule dev, schedule_bytes of tl_paged_query, 16-byte aligned (written).  Enqueued on `stream`. */

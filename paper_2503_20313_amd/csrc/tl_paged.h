@@ -11,8 +11,8 @@ constexpr int kBlk = 64;              // keys per block: the unit in which the s
 constexpr int kTileRows = 256;        // query rows (token-major, the query heads of a key head side by side) of a tile
 constexpr int kFewRows = 32;          // requests with at most so many rows per key head go to the few-row kernel, one tile each
 
-// Schedule: a header of 16 ints -- dims key, items, cut tiles of the tile class --, the cut tiles' first items, then the items.
-constexpr int kSchedHeader = 16;
+// Schedule: a header of 16 ints -- 0, items, cut tiles of the tile class, 0, what it was made for --, the cut tiles' first items, then the items.
+constexpr int kSchedHeader = 16, kSchedDims = 4;
 // An item is a tile, or a run of its key blocks: request, first token row, tokens, sequence length, tile, first and end key block,
 // first partial slot of the tile, index of the run, runs of the tile, 1 for few rows, 0.
 constexpr int kItemInts = 12;
@@ -27,8 +27,22 @@ struct PagedGeom {
   int sched_items;         // where the items start in the schedule, in ints
   int rows_few, rows_tile; // rows of a partial result
   FastDiv by_group;        // G: row of a request -> token
-  unsigned key;            // of all of the above: a schedule serves only the dims it was made for
 };
+
+// Header word i of a schedule for `g`.  Words from kSchedDims on are all that items, and the room for them in schedule, tables, rows and
+// workspace, follow from; the other fields are made of these, and page_stride, which no item depends on, may be another for every layer.
+__host__ __device__ __forceinline__ int sched_header(const PagedGeom& g, int i, int items, int cuts) {
+  const int h[kSchedHeader] = {0, items, cuts, 0, g.B, g.T, g.max_new, g.max_blocks, g.page, g.n_pages, g.Hq, g.Hk, g.window, g.side, 0, 0};
+  return h[i];
+}
+// A schedule serves the dims it was made for and no others: every word is compared (ordinary dims share any hash of them).  One that was
+// never made is zero, which no batch is.
+__host__ __device__ __forceinline__ bool sched_made_for(const int* schedule, const PagedGeom& g) {
+  int other = 0;
+#pragma unroll
+  for (int i = kSchedDims; i < kSchedHeader; i++) other |= schedule[i] ^ sched_header(g, i, 0, 0);
+  return other == 0;
+}
 
 int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g);
 

@@ -234,7 +234,10 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   if (tid < 2) s_slots[tid] = 0;
   if (tid == 0) { s_cut = 0; s_long = 0; }
   if (__syncthreads_or(bad)) {
-    if (tid < kSchedHeader) p.out[tid] = tid == 0 ? (int)g.key : 0;
+    if (tid == 0) {
+#pragma unroll
+      for (int i = 0; i < kSchedHeader; i++) p.out[i] = sched_header(g, i, 0, 0);
+    }
     return;
   }
   auto is_few = [&](int b) { return g.rt > 0 && s_n[b] * g.G <= kFewRows; };   // (at most 2^28)
@@ -426,9 +429,8 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
   }
   __syncthreads();
   if (tid == 0) {
-    p.out[0] = (int)g.key;
-    p.out[1] = n_items;
-    p.out[2] = s_cut;
+#pragma unroll
+    for (int i = 0; i < kSchedHeader; i++) p.out[i] = sched_header(g, i, n_items, s_cut);
   }
 }
 
@@ -1233,7 +1235,7 @@ __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const Pa
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
   const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);     // (there is room for every idx of the launch)
-  if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
+  if (!sched_made_for(p.schedule, p.g) || idx >= p.schedule[1]) return;
   few_rows_item<RT>(p, it, head, smem);
 }
 
@@ -1242,7 +1244,7 @@ __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAt
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
   const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);
-  if (p.schedule[0] != (int)p.g.key || idx >= p.schedule[1]) return;
+  if (!sched_made_for(p.schedule, p.g) || idx >= p.schedule[1]) return;
   if (!FEW || !it.few) tile_item(p, it, head, smem);
   else few_rows_item<2>(p, it, head, smem);
 }
@@ -1254,7 +1256,7 @@ __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAt
 constexpr int kTileJoin = 4, kJoinRows = 8;
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
   const PagedGeom& g = p.g;
-  if (p.schedule[0] != (int)g.key) return;
+  if (!sched_made_for(p.schedule, g)) return;
   const int parts = (g.rows_tile + kJoinRows - 1) / kJoinRows, jobs = p.schedule[2] * g.Hk * parts;
   const long step = (long)g.Hk * g.rows_tile;
   for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
@@ -1317,10 +1319,6 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
   if (((long)g->cap_tile + g->cap_few) * g->Hk > 0x7fffffffL)
     return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: too many tiles for one launch");
-  unsigned key = 2166136261u;
-  const int v[] = {g->B, g->T, g->max_new, g->max_blocks, g->page, g->n_pages, g->Hq, g->Hk, g->window, cus};
-  for (int x : v) key = (key ^ (unsigned)x) * 16777619u;
-  g->key = key | 1u;                                    // a schedule that was never made is zero
   return TL_OK;
 }
 
