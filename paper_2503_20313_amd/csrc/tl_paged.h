@@ -44,6 +44,22 @@ __host__ __device__ __forceinline__ bool sched_made_for(const int* schedule, con
   return other == 0;
 }
 
+struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs, few; };
+
+__host__ __device__ __forceinline__ Item load_item(const int* schedule, const PagedGeom& g, int idx) {
+  const int* rec = schedule + g.sched_items + (long)idx * kItemInts;
+  Item i;
+  i.b = rec[0]; i.q0 = rec[1]; i.n = rec[2]; i.seq = rec[3]; i.tile = rec[4]; i.k0 = rec[5]; i.k1 = rec[6]; i.slot = rec[7]; i.run = rec[8]; i.runs = rec[9]; i.few = rec[10];
+  return i;
+}
+// Item `idx` of a launch, if the schedule has it.  Before that is known nothing behind the header is read: the schedule of smaller dims
+// ends anywhere behind it.
+__host__ __device__ __forceinline__ bool sched_item(const int* schedule, const PagedGeom& g, int idx, Item* it) {
+  if (!sched_made_for(schedule, g) || idx >= schedule[1]) return false;
+  *it = load_item(schedule, g, idx);
+  return true;
+}
+
 int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g);
 
 // Last check before a launch: a real context, and its device is the current one (the stream belongs to that device).

@@ -453,14 +453,6 @@ struct PagedAttn {
   unsigned *arrived;               // few-row class: per (slot, key head) runs of a group that have arrived, groups of a tile that have; zero between calls
 };
 
-struct Item { int b, q0, n, seq, tile, k0, k1, slot, run, runs, few; };
-
-__device__ __forceinline__ Item load_item(const int* rec) {
-  Item i;
-  i.b = rec[0]; i.q0 = rec[1]; i.n = rec[2]; i.seq = rec[3]; i.tile = rec[4]; i.k0 = rec[5]; i.k1 = rec[6]; i.slot = rec[7]; i.run = rec[8]; i.runs = rec[9]; i.few = rec[10];
-  return i;
-}
-
 __device__ __forceinline__ bool not_finite(unsigned bits16) { return (bits16 & 0x7f80u) == 0x7f80u; }
 
 // 16 bytes of a value row whose non-finite elements became zeros; any = there were some.
@@ -1234,8 +1226,8 @@ template <int RT>
 __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
-  const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);     // (there is room for every idx of the launch)
-  if (!sched_made_for(p.schedule, p.g) || idx >= p.schedule[1]) return;
+  Item it;
+  if (!sched_item(p.schedule, p.g, idx, &it)) return;
   few_rows_item<RT>(p, it, head, smem);
 }
 
@@ -1243,8 +1235,8 @@ template <bool FEW>    // FEW: the batch may have few-row items
 __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
-  const Item it = load_item(p.schedule + p.g.sched_items + (long)idx * kItemInts);
-  if (!sched_made_for(p.schedule, p.g) || idx >= p.schedule[1]) return;
+  Item it;
+  if (!sched_item(p.schedule, p.g, idx, &it)) return;
   if (!FEW || !it.few) tile_item(p, it, head, smem);
   else few_rows_item<2>(p, it, head, smem);
 }
@@ -1261,7 +1253,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn p) {
   const long step = (long)g.Hk * g.rows_tile;
   for (int job = blockIdx.x; job < jobs; job += gridDim.x) {
     const int cut = job / (g.Hk * parts), rest = job - cut * g.Hk * parts, head = rest / parts;
-    const Item it = load_item(p.schedule + g.sched_items + (long)p.schedule[kSchedHeader + cut] * kItemInts);
+    const Item it = load_item(p.schedule, g, p.schedule[kSchedHeader + cut]);
     const int row0 = it.tile * kTileRows, n = min(it.n * g.G - row0, kTileRows);
     const int r = (rest - head * parts) * kJoinRows + (threadIdx.x >> 5), d4 = (threadIdx.x & 31) * 4;
     if (r >= n) continue;

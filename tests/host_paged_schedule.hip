@@ -1,4 +1,4 @@
-// The check that stands in front of every use of a schedule, on the host: geometries as the library resolves them (a context made by
+// The checks that stand in front of every use of a schedule, on the host: geometries as the library resolves them (a context made by
 // tl_ctx_create_host, 256 compute units), headers as the schedule kernel writes them, in buffers of exactly a schedule's size.
 // Prints "host_paged_schedule ok <checks>".
 #include <stdio.h>
@@ -70,6 +70,22 @@ int main() {
   EXPECT(!serves(s1, one));
   free(s1);
   free(s2);
+
+  // Items are looked for over the launch of the call's own dims, far beyond the end of a schedule of smaller ones: none is found, and
+  // nothing behind the header is read.
+  const tl_paged_dims least = dims(1, 1, 1, 1), most = dims(4096, 8192, 512, 64);
+  int* sl = schedule_for(least);
+  PagedGeom gl, gm;
+  Item it;
+  EXPECT(resolve_paged(ctx, &least, &gl) == TL_OK && resolve_paged(ctx, &most, &gm) == TL_OK && gm.cap_few + gm.cap_tile > 100 * gl.cap_few);
+  for (int idx = 0; idx < gm.cap_few + gm.cap_tile; idx++) EXPECT(!sched_item(sl, gm, idx, &it));
+  // under its own dims: the items that it has, every one inside the room
+  EXPECT(sched_item(sl, gl, 0, &it) && !sched_item(sl, gl, 1, &it));
+  for (int i = 0; i < kSchedHeader; i++) sl[i] = sched_header(gl, i, gl.cap_few, 0);
+  for (int idx = 0; idx < gl.cap_few; idx++) EXPECT(sched_item(sl, gl, idx, &it) && it.few == 0x11111111);
+  EXPECT(!sched_item(sl, gl, gl.cap_few, &it));
+  free(sl);
+
   // another number of compute units: items side by side, and with them room and layout, are others
   tl_ctx* small = nullptr;
   EXPECT(tl_ctx_create_host(&cfg, 64, &small) == TL_OK);

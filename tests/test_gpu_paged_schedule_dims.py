@@ -51,6 +51,18 @@ def test_dims_that_hash_alike():
     tl.tl_ctx_destroy(c)
 
 
+@pytest.mark.parametrize("max_new", [1, 512])
+def test_a_schedule_of_smaller_dims_that_ends_early(max_new):
+    """The buffer of one request's schedule, under the dims of a large batch.  What lies behind its end looks like items."""
+    c = ctx()
+    small, large = paged_dims(1, 1, 1, 64), paged_dims(4096, 8192, max_new, 64)
+    z = tl.tl_paged_query(c, large)
+    s = made_schedule(c, small, [1], [100], behind=z["schedule_bytes"] // 4)
+    s[tl.tl_paged_query(c, small)["schedule_bytes"] // 4:] = 1
+    assert not attend(c, large, s)
+    tl.tl_ctx_destroy(c)
+
+
 def test_one_schedule_for_layers_whose_pages_lie_differently():
     c = ctx()
     s = made_schedule(c, paged_dims(128, 1024, 13, 64), [1], [20])
