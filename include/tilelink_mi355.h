@@ -457,7 +457,7 @@ int tl_paged_query(const tl_ctx* ctx, const tl_paged_dims* dims /*host*/, size_t
  *   query_start         dev int[batch+1] (written): first row of every request's new tokens, then their number
  *   seq_lens            dev int[batch] (written): tokens of the request after the step
  *   slots, positions    dev int[max_tokens] (written): slot and position of every new token; -1 and 0 in the rows behind the last
- *   counts              dev int[4] (written): new tokens, pages taken, pages that the list lacked, tokens that did not fit
+ *   counts              dev int[4] (written): new tokens, pages taken, pages that the list lacked, tokens that did not fit (2^31-1 if more)
  * A request gets at most max_new tokens and as many as its table has room for; tokens beyond max_tokens rows are cut off at the
  * end.  A page that the list lacks has entry and slots -1: such a token is neither stored nor attended to (counts[2] tells).
  * In place: seq_lens may be ctx_lens, and free_to may be free_from (a captured step then feeds itself); nothing else may overlap.

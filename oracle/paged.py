@@ -15,7 +15,7 @@ def slots(ctx_lens, new_lens, free_pages, free_from, block_table, T, max_new, pa
     start, seq = [0], []
     used, lacking, over, row = 0, 0, 0, 0
     for b, (c, n) in enumerate(zip(ctx_lens, new_lens)):
-        c, want = min(max(int(c), 0), cap), min(max(int(n), 0), 1 << 18)
+        c, want = min(max(int(c), 0), cap), max(int(n), 0)
         n = min(want, max_new, cap - c, T - row)
         over += want - n
         for j in range(-(-c // page), -(-(c + n) // page)):
@@ -34,7 +34,7 @@ def slots(ctx_lens, new_lens, free_pages, free_from, block_table, T, max_new, pa
         start.append(row)
         seq.append(c + n)
     return dict(table=table, query_start=np.array(start), seq_lens=np.array(seq), slots=out_slots, positions=positions, free_to=free_from + used,
-                counts=np.array([row, used, lacking, over]))
+                counts=np.array([row, used, lacking, min(over, 2 ** 31 - 1)]))
 
 
 def norm_rope(x, weight, eps, positions, cos_sin, rot, interleaved):

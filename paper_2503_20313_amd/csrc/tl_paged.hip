@@ -57,6 +57,16 @@ __device__ __forceinline__ int block_scan(int v, int* s_wave, int* total) {
   return v + before;
 }
 
+// Over the 64 lanes of a wave, in every lane: rotations inside rows of 16 lanes, then the four rows.
+template <class F>
+__device__ __forceinline__ int wave_reduce(int x, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, true));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, true));
+  return f(f(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)), f(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+
 // The largest i in [0, n) with a[i] <= x, for a[0] <= x and ascending a: of equal entries the last, so empty requests are passed over.
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
   int lo = 0, hi = n;
@@ -80,19 +90,21 @@ __global__ void __launch_bounds__(NT) paged_slots_kernel(const SlotsParams p) {
   const int cap = p.max_blocks * p.page;
   const int from = p.free_from ? max(p.free_from[0], 0) : 0;
   int len[kReq];
-  int sum = 0, asked = 0;
+  int sum = 0, over = 0;
+  // Tokens that do not fit: requests may ask for 2^43 together, so their sum stays at the largest int where it gets there.
+  auto add_over = [](int x, int y) { return (int)min((unsigned)x + (unsigned)y, 0x7fffffffu); };
 #pragma unroll
   for (int i = 0; i < kReq; i++) {
     len[i] = 0;
     if (i < per && b0 + i < p.B) {
-      const int c = min(max(p.ctx_lens[b0 + i], 0), cap), want = min(max(p.new_lens[b0 + i], 0), 1 << 18);
+      const int c = min(max(p.ctx_lens[b0 + i], 0), cap), want = max(p.new_lens[b0 + i], 0);
       s_ctx[b0 + i] = c;
       len[i] = min(min(want, p.max_new), cap - c);
-      sum += len[i];             // (at most 2^12 * 2^18: the sums fit)
-      asked += want - len[i];
+      sum += len[i];             // (max_new is at most 2^18: 2^12 * 2^18, the sums fit)
+      over = add_over(over, want - len[i]);
     }
   }
-  int all_tokens, all_pages, over = 0;
+  int all_tokens, all_pages;
   int at = block_scan<NT>(sum, s_wave, &all_tokens) - sum;
   // tokens that do not fit the rows are cut off at the end
   int pages = 0;
@@ -100,7 +112,7 @@ __global__ void __launch_bounds__(NT) paged_slots_kernel(const SlotsParams p) {
   for (int i = 0; i < kReq; i++)
     if (i < per && b0 + i < p.B) {
       const int lo = min(at, p.T), hi = min(at + len[i], p.T);
-      asked += len[i] - (hi - lo);
+      over = add_over(over, len[i] - (hi - lo));
       at += len[i];
       s_start[b0 + i] = lo;
       len[i] = hi - lo;
@@ -118,7 +130,17 @@ __global__ void __launch_bounds__(NT) paged_slots_kernel(const SlotsParams p) {
   const int n_tokens = min(all_tokens, p.T);
   const int left = max(p.n_free - from, 0);          // pages that the list still holds
   const bool lengths = (PARTS & kLengths) && blockIdx.x == 0;
-  if (lengths) block_scan<NT>(asked, s_wave, &over);
+  if (lengths) {
+    over = wave_reduce(over, add_over);
+    if constexpr (NT > 64) {
+      __syncthreads();   // (s_wave may still be read by the scan)
+      if ((tid & 63) == 0) s_wave[tid >> 6] = over;
+      __syncthreads();
+      over = 0;
+#pragma unroll
+      for (int w = 0; w < NT / 64; w++) over = add_over(over, s_wave[w]);
+    }
+  }
   if (tid == 0) { s_start[p.B] = n_tokens; s_page[p.B] = all_pages; }
   __syncthreads();   // every input that this workgroup may write in place has been read
   if (PARTS & kMaps) {
@@ -195,16 +217,6 @@ __device__ __forceinline__ void tile_span(const PagedGeom& g, int n, int seq, in
   const int start = g.window ? max(seq - n + t0 - g.window + 1, 0) : 0;
   *hi = (end + kBlk - 1) / kBlk;
   *lo = min(start / kBlk, *hi);
-}
-
-// Over the 64 lanes of a wave, in every lane: rotations inside rows of 16 lanes, then the four rows.
-template <class F>
-__device__ __forceinline__ int wave_reduce(int x, F f) {
-  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true));
-  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, true));
-  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, true));
-  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, true));
-  return f(f(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)), f(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
 }
 
 template <int NT>
