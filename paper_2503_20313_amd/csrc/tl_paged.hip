@@ -449,6 +449,12 @@ __global__ void __launch_bounds__(NT) paged_schedule_kernel(const SchedParams p)
 // ======================================================================================
 // Attention.
 // ======================================================================================
+// The exponents' reference of a row follows the row's maximum only where that has left it by more than kLazy (in exponents of two), so that
+// sums and O need no rescaling in nearly every block.  Every weight is 2^-kLazy times exp2 of what lies above the reference: in (0, 1], as
+// with a reference that is the maximum itself, so whatever a sum of such weights holds is finite here too (weights up to 2^kLazy would let
+// values above 2^120 overflow).  At the other end, weights below 2^(kLazy - 126) of the largest are zero.
+constexpr float kLazy = 8.f;
+
 struct PagedAttn {
   PagedGeom g;
   const bf16_t* q;
@@ -458,7 +464,7 @@ struct PagedAttn {
   float* lse;               // [T, Hq] or null
   long q_stride, o_stride;
   float scale_log2e;
-  float lazy;               // tiles: how far, in scores, a row's maximum may leave the exponents' reference: 2^8 in weights
+  float lazy;               // how far, in scores, a row's maximum may leave the exponents' reference: kLazy in exponents
   float *part_few, *part_tile;     // partial results: [slot][key head][row][128], unnormalised, and [slot][key head][row][2]: maximum, sum
   float *ml_few, *ml_tile;
   float *group_few, *group_ml;     // few-row class: what the runs of a group were joined to, at the group's first run's place
@@ -485,7 +491,7 @@ __device__ __forceinline__ int token_of(const PagedGeom& g, int row, int head, i
 }
 
 __device__ __forceinline__ float log_sum(float m, float l, float scale_log2e) {
-  return l == 0.f ? -INFINITY : (m * scale_log2e + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  return l == 0.f ? -INFINITY : (__builtin_fmaf(m, scale_log2e, kLazy) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 // What a row's sum is multiplied by: a row that sees nothing is zero.
 __device__ __forceinline__ float row_scale(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
@@ -699,7 +705,7 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
       grown |= !(top[u] - m_run[u] <= p.lazy);
     }
     if (__builtin_amdgcn_ballot_w64(grown)) {
-      // some row's maximum has left its exponents' reference by more than 2^8 (see the tiles): the row's four lanes follow together
+      // some row's maximum has left its exponents' reference by more than kLazy: the row's four lanes follow together
 #pragma unroll
       for (int u = 0; u < RT; u++) {
         float m = fmaxf(top[u], __shfl_xor(top[u], 16));
@@ -707,7 +713,7 @@ __device__ __forceinline__ void few_rows_item(const PagedAttn& p, const Item& it
         const bool row = !(m - m_run[u] <= p.lazy);
         const float ms = m == -INFINITY ? 0.f : m;         // nothing seen so far: every exponent below is -inf
         const float alpha = row ? __builtin_amdgcn_exp2f((m_run[u] - ms) * p.scale_log2e) : 1.f;
-        if (row) { m_run[u] = m; mc[u] = -ms * p.scale_log2e; }
+        if (row) { m_run[u] = m; mc[u] = __builtin_fmaf(-ms, p.scale_log2e, -kLazy); }
         l_run[u] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 8; dt++)
@@ -1092,15 +1098,14 @@ __device__ __forceinline__ void tile_item(const PagedAttn& p, const Item& it, in
           }
         m_blk = block_max(c);
       }
-      // The exponents' reference m_run follows the row's maximum only where that has left it by more than 2^8: up to there weights stay
-      // below 256, which fp32 sums and bf16 weights hold as exactly as those below 1, and O needs no rescaling.  (It follows at once
-      // from -inf, and the comparison is false for NaN.)
+      // The exponents' reference m_run follows the row's maximum only where that has left it by more than kLazy.  (It follows at once from
+      // -inf, and the comparison is false for NaN.)
       if (__builtin_amdgcn_ballot_w64(!(m_blk - m_run <= p.lazy))) {
         const float m_new = fmaxf(m_run, halves_max(m_blk));   // (m_blk: of the lane's own half of the keys)
         const bool grown = !(m_new - m_run <= p.lazy);
         const float ms = m_new == -INFINITY ? 0.f : m_new;     // nothing seen so far: every exponent below is -inf
         const float alpha = grown ? __builtin_amdgcn_exp2f((m_run - ms) * p.scale_log2e) : 1.f;
-        if (grown) { m_run = m_new; mc = -ms * p.scale_log2e; }
+        if (grown) { m_run = m_new; mc = __builtin_fmaf(-ms, p.scale_log2e, -kLazy); }
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; dt++)
@@ -1450,7 +1455,7 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.o = (bf16_t*)o; p.lse = lse;
   p.q_stride = q_stride; p.o_stride = o_stride;
   p.scale_log2e = scale * 1.4426950408889634f;
-  p.lazy = 8.f / p.scale_log2e < 3.0e38f ? 8.f / p.scale_log2e : 3.0e38f;
+  p.lazy = kLazy / p.scale_log2e < 3.0e38f ? kLazy / p.scale_log2e : 3.0e38f;
   char* ws = (char*)workspace;
   p.arrived = (unsigned*)ws;
   p.part_few = (float*)(ws + z.part_few); p.ml_few = (float*)(ws + z.ml_few);
