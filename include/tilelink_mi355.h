@@ -504,7 +504,8 @@ int tl_paged_schedule(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int
  * Attention of every request's new tokens over its keys in the cache, the new ones included (they are stored first):
  *   o[t,i,:] = bf16( sum_j softmax_j( scale * q[t,i,:] . K[j,h,:] ) V[j,h,:] ),  h = i / (heads_q/heads_kv),  j the positions that
  *   the token sees: not after its own, inside the window, on pages that exist (entries of block_table outside [0, n_pages) do not).
- * fp32 scores, statistics and accumulation, probabilities rounded to bf16 before they multiply V.  A token that sees nothing has
+ * fp32 scores, statistics and accumulation.  Probabilities multiply V with 16 bits in requests that count as few rows (info[1] of
+ * tl_paged_query; every single token with at most 32 query heads per key head), rounded to bf16 in larger ones.  A token that sees nothing has
  * o = 0 and lse = -inf.  A key or value that a token does not see has no influence on it, infinities and NaN included.
  *   q dev [max_tokens rows of heads_q*128] bf16, q_stride elements apart;  o likewise (written; rows behind the last request are
  *     left as they were);  lse dev fp32 [max_tokens, heads_q] (written; NULL: not wanted): log of the sum of exponentials
