@@ -424,8 +424,9 @@ int tl_attn_query(const tl_ctx* ctx, int S, int heads, int head_dim, int causal,
  * No call reads a length on the host: a step can be captured into a HIP graph and replayed with other lengths.
  *
  * Cache: k_cache and v_cache hold n_pages pages of page_size tokens, bf16; the row of token r of page p and key head h starts at
- * element p*page_stride + (h*page_size + r)*head_dim.  A token's slot is p*page_size + r.  Nothing is read from a page that no
- * table lists, and what lies behind a request's last token has no influence on any result, whatever it holds.
+ * element p*page_stride + (h*page_size + r)*head_dim.  A token's slot is p*page_size + r.  Of pages that no table lists only page 0
+ * is ever read, in the place of keys that have no page; neither it nor what lies behind a request's last token has any influence on a
+ * result, whatever it holds.
  */
 typedef struct tl_paged_dims {
   int batch;                 /* requests: rows of block_table, at most 4096 */
