@@ -71,6 +71,9 @@ inline int check_paged_launch(const tl_ctx* ctx, const char* what) {
   return TL_OK;
 }
 
+// A launch's work items are counted in 32 bits, and a larger grid is cut off at its end without an error.
+inline bool fits_one_launch(long workgroups, long threads) { return workgroups * threads <= 0xffffffffL; }
+
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 }  // namespace tl

@@ -1337,7 +1337,8 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   g->cap_tile = g->has_tiles ? (int)(tiles + g->side) : 0;
   g->rows_few = g->rt ? (int)(most_rows < kFewRows ? most_rows : kFewRows) : 0;
   g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
-  if (((long)g->cap_tile + g->cap_few) * g->Hk > 0x7fffffffL)
+  static_assert(kTileThreads == kFewWaves * 64, "one bound for both");
+  if (!fits_one_launch(((long)g->cap_tile + g->cap_few) * g->Hk, kTileThreads))
     return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: too many tiles for one launch");
   return TL_OK;
 }

@@ -144,13 +144,16 @@ static int check_in_place(const char* what, const char* name, const void* in, lo
   return TL_OK;
 }
 
+static long rope_workgroups(int T, int heads) { return ((long)T * ceil_div(heads, kHeads) + 15) / 16; }
+
 static int check_rope(const char* what, const void* q, long long q_stride, const void* k, long long k_stride, const void* q_out, long long qo_stride, int T,
-                      int Hq, int Hk, int head_dim, const void* wq, const void* wk, float eps, const int* positions, const float* cos_sin, int max_position,
+                      int Hq, int Hk, int heads, int head_dim, const void* wq, const void* wk, float eps, const int* positions, const float* cos_sin, int max_position,
                       int rot_dim) {
   if (!q || !k || !q_out) return fail(TL_ERR_INVALID_ARG, "%s: null pointer argument", what);
   if (T <= 0 || Hq <= 0 || Hk <= 0) return fail(TL_ERR_INVALID_ARG, "%s: rows and heads must be positive", what);
   if (head_dim != kPagedD) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: head_dim %d is not supported (128 only)", what, head_dim);
   if (Hq > 1024 || Hk > 1024) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: at most 1024 heads", what);
+  if (!fits_one_launch(rope_workgroups(T, heads), 256)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and heads for one launch", what);
   if (!!wq != !!wk) return fail(TL_ERR_INVALID_ARG, "%s: q_weight and k_weight are given together or not at all", what);
   if (wq && !(eps >= 0.f)) return fail(TL_ERR_INVALID_ARG, "%s: eps must not be negative", what);
   if (rot_dim < 0 || rot_dim > kPagedD || rot_dim % 16) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: rot_dim %d is not a multiple of 16 up to 128", what, rot_dim);
@@ -183,8 +186,7 @@ constexpr long kL2Bytes = 32L << 20;      // of the eight dies
 
 template <bool CACHE>
 static int launch_rope(const RopeParams& p, void* stream) {
-  const long wgs = ((long)p.T * p.groups + 15) / 16;
-  if (wgs > 0x7fffffffL) return fail(TL_ERR_UNSUPPORTED_SHAPE, "too many rows and heads for one launch");
+  const long wgs = rope_workgroups(p.T, p.heads);
   const bool stream_out = (long)p.T * p.heads * kPagedD * 2 > kL2Bytes;
   hipLaunchKernelGGL((stream_out ? qk_norm_rope_kernel<CACHE, true> : qk_norm_rope_kernel<CACHE, false>), dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
@@ -202,8 +204,8 @@ int tl_qk_norm_rope(tl_ctx* ctx, const void* q, long long q_stride, const void* 
                     const int* positions, const float* cos_sin, int max_position, int rot_dim, int interleaved, void* stream) {
   const char* what = "tl_qk_norm_rope";
   if (int e = check_ctx(ctx)) return e;
-  if (int e = check_rope(what, q, q_stride, k, k_stride, q_out, q_out_stride, T, heads_q, heads_kv, head_dim, q_weight, k_weight, eps, positions, cos_sin,
-                         max_position, rot_dim))
+  if (int e = check_rope(what, q, q_stride, k, k_stride, q_out, q_out_stride, T, heads_q, heads_kv, heads_q + heads_kv, head_dim, q_weight, k_weight, eps,
+                         positions, cos_sin, max_position, rot_dim))
     return e;
   if (!k_out) return fail(TL_ERR_INVALID_ARG, "%s: null pointer argument", what);
   if (k_out_stride < (long long)heads_kv * kPagedD) return fail(TL_ERR_INVALID_ARG, "%s: a row stride is shorter than the row's heads", what);
@@ -224,8 +226,8 @@ int tl_qk_norm_rope_cache(tl_ctx* ctx, const tl_paged_dims* dims, const void* q,
   const char* what = "tl_qk_norm_rope_cache";
   PagedGeom g;
   if (int e = resolve_paged(ctx, dims, &g)) return e;
-  if (int e = check_rope(what, q, q_stride, k, k_stride, q_out, q_out_stride, g.T, g.Hq, g.Hk, kPagedD, q_weight, k_weight, eps, positions, cos_sin,
-                         max_position, rot_dim))
+  if (int e = check_rope(what, q, q_stride, k, k_stride, q_out, q_out_stride, g.T, g.Hq, g.Hk, g.Hq + 2 * g.Hk, kPagedD, q_weight, k_weight, eps, positions,
+                         cos_sin, max_position, rot_dim))
     return e;
   if (!v || !k_cache || !v_cache || !slots) return fail(TL_ERR_INVALID_ARG, "%s: null pointer argument", what);
   if (v_stride < (long long)g.Hk * kPagedD) return fail(TL_ERR_INVALID_ARG, "%s: a row stride is shorter than the row's heads", what);
