@@ -440,8 +440,6 @@ typedef struct tl_paged_dims {
   int window;                /* 0: a token sees every earlier one of its request and itself; w > 0: itself and the w-1 before it */
   long long page_stride;     /* elements from a page to the next, in k_cache and in v_cache; 0 = heads_kv*page_size*head_dim */
 } tl_paged_dims;
-/* Dims under which there may be 2^23 items of all key heads together (info[3] + info[4] below, times heads_kv) do not fit one launch and
- * are refused. */
 
 /* Sizes for `dims` (host call): bytes of `schedule` and of the attention's workspace; info[0..7] = query rows of a tile, rows up to
  * which a request counts as few, keys per block, items of the few-row class and of the tile class per key head at most, items
@@ -478,8 +476,7 @@ int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* c
  *   q_weight, k_weight dev bf16[128], both or neither (NULL: no norm);  positions dev int[T]
  *   cos_sin dev fp32 [max_position, rot_dim]: cosines of the rot_dim/2 angles of a position, then their sines
  *   rot_dim a multiple of 16 up to 128; 0 = no rotation (positions and cos_sin may be NULL)
- * A row whose position is outside [0, max_position) is left as it was.  Strides multiples of 8, pointers 16-byte aligned; at most
- * 2^28 pairs of heads in all rows together (one launch).
+ * A row whose position is outside [0, max_position) is left as it was.  Strides multiples of 8, pointers 16-byte aligned.
  * Before tl_sp_ag_attention: on the local query and key shards.
  */
 int tl_qk_norm_rope(tl_ctx* ctx, const void* q /*dev*/, long long q_stride, const void* k /*dev*/, long long k_stride, void* q_out /*dev*/,

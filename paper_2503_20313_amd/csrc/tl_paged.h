@@ -71,8 +71,14 @@ inline int check_paged_launch(const tl_ctx* ctx, const char* what) {
   return TL_OK;
 }
 
-// A launch's work items are counted in 32 bits, and a larger grid is cut off at its end without an error.
-inline bool fits_one_launch(long workgroups, long threads) { return workgroups * threads <= 0xffffffffL; }
+// A grid's work items are counted in 32 bits a dimension, and a larger one is cut off at its end without an error: workgroups beyond kGridX
+// go into rows of a second dimension, of which the last may reach beyond `workgroups`.
+constexpr unsigned kGridX = 1u << 16;
+constexpr long kMostWorkgroups = 65535L * kGridX;
+inline dim3 grid_of(long workgroups) {
+  return workgroups <= (long)kGridX ? dim3((unsigned)workgroups) : dim3(kGridX, (unsigned)((workgroups + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ unsigned workgroup_index() { return blockIdx.y * kGridX + blockIdx.x; }
 
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 

@@ -1253,7 +1253,8 @@ static_assert(kTileLds <= kFewLds && 2 * 2 * kStageBytes + kTileRows * kPagedD *
 template <int RT>
 __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
+  const unsigned wg = workgroup_index();
+  const int idx = wg / (unsigned)p.g.Hk, head = wg - idx * p.g.Hk;
   Item it;
   if (!sched_item(p.schedule, p.g, idx, &it)) return;
   few_rows_item<RT>(p, it, head, smem);
@@ -1262,7 +1263,8 @@ __global__ void __launch_bounds__(kFewWaves * 64) paged_few_rows_kernel(const Pa
 template <bool FEW>    // FEW: the batch may have few-row items
 __global__ void __launch_bounds__(kTileThreads) paged_mixed_kernel(const PagedAttn p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int idx = blockIdx.x / p.g.Hk, head = blockIdx.x - idx * p.g.Hk;
+  const unsigned wg = workgroup_index();
+  const int idx = wg / (unsigned)p.g.Hk, head = wg - idx * p.g.Hk;
   Item it;
   if (!sched_item(p.schedule, p.g, idx, &it)) return;
   if (!FEW || !it.few) tile_item(p, it, head, smem);
@@ -1337,8 +1339,7 @@ int resolve_paged(const tl_ctx* ctx, const tl_paged_dims* d, PagedGeom* g) {
   g->cap_tile = g->has_tiles ? (int)(tiles + g->side) : 0;
   g->rows_few = g->rt ? (int)(most_rows < kFewRows ? most_rows : kFewRows) : 0;
   g->rows_tile = g->has_tiles ? (int)(most_rows < kTileRows ? most_rows : kTileRows) : 0;
-  static_assert(kTileThreads == kFewWaves * 64, "one bound for both");
-  if (!fits_one_launch(((long)g->cap_tile + g->cap_few) * g->Hk, kTileThreads))
+  if (((long)g->cap_tile + g->cap_few) * g->Hk > 0x7fffffffL)
     return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_paged_dims: too many tiles for one launch");
   return TL_OK;
 }
@@ -1474,14 +1475,14 @@ int tl_paged_attention(tl_ctx* ctx, const tl_paged_dims* dims, const void* q, lo
   p.group_few = (float*)(ws + z.group_few); p.group_ml = (float*)(ws + z.group_ml);
   p.part_tile = (float*)(ws + z.part_tile); p.ml_tile = (float*)(ws + z.ml_tile);
   hipStream_t s = (hipStream_t)stream;
-  auto launch = [&](auto kernel, int which, int grid, int threads, int lds) -> int {
+  auto launch = [&](auto kernel, int which, long grid, int threads, int lds) -> int {
     if (int e = allow_lds((const void*)kernel, which, ctx->device, lds)) return e;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), lds, s, p);
+    hipLaunchKernelGGL(kernel, grid_of(grid), dim3(threads), lds, s, p);
     TL_HIP(hipGetLastError());
     return TL_OK;
   };
-  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, g.cap_few * g.Hk, kFewWaves * 64, kFewLds);
-  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, g.rt ? 2 : 3, (g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
+  if (!g.has_tiles) return launch(g.rt == 1 ? paged_few_rows_kernel<1> : paged_few_rows_kernel<2>, g.rt == 1 ? 0 : 1, (long)g.cap_few * g.Hk, kFewWaves * 64, kFewLds);
+  if (int e = launch(g.rt ? paged_mixed_kernel<true> : paged_mixed_kernel<false>, g.rt ? 2 : 3, ((long)g.cap_tile + g.cap_few) * g.Hk, kTileThreads, kFewLds)) return e;
   hipLaunchKernelGGL(paged_join_kernel, dim3(8 * ctx->num_cus), dim3(256), 0, s, p);
   TL_HIP(hipGetLastError());
   return TL_OK;

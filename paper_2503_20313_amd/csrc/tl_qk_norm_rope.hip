@@ -49,7 +49,7 @@ __device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
 
 template <bool CACHE, bool STREAM>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const RopeParams p) {
-  const long task = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const long task = (long)workgroup_index() * 16 + (threadIdx.x >> 4);
   const int t = (int)(task / p.groups), h0 = (int)(task - (long)t * p.groups) * kHeads;
   if (t >= p.T) return;   // (whole rows of lanes)
   const int l = threadIdx.x & 15;
@@ -153,7 +153,7 @@ static int check_rope(const char* what, const void* q, long long q_stride, const
   if (T <= 0 || Hq <= 0 || Hk <= 0) return fail(TL_ERR_INVALID_ARG, "%s: rows and heads must be positive", what);
   if (head_dim != kPagedD) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: head_dim %d is not supported (128 only)", what, head_dim);
   if (Hq > 1024 || Hk > 1024) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: at most 1024 heads", what);
-  if (!fits_one_launch(rope_workgroups(T, heads), 256)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and heads for one launch", what);
+  if (rope_workgroups(T, heads) > kMostWorkgroups) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: too many rows and heads for one launch", what);
   if (!!wq != !!wk) return fail(TL_ERR_INVALID_ARG, "%s: q_weight and k_weight are given together or not at all", what);
   if (wq && !(eps >= 0.f)) return fail(TL_ERR_INVALID_ARG, "%s: eps must not be negative", what);
   if (rot_dim < 0 || rot_dim > kPagedD || rot_dim % 16) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: rot_dim %d is not a multiple of 16 up to 128", what, rot_dim);
@@ -186,9 +186,8 @@ constexpr long kL2Bytes = 32L << 20;      // of the eight dies
 
 template <bool CACHE>
 static int launch_rope(const RopeParams& p, void* stream) {
-  const long wgs = rope_workgroups(p.T, p.heads);
   const bool stream_out = (long)p.T * p.heads * kPagedD * 2 > kL2Bytes;
-  hipLaunchKernelGGL((stream_out ? qk_norm_rope_kernel<CACHE, true> : qk_norm_rope_kernel<CACHE, false>), dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL((stream_out ? qk_norm_rope_kernel<CACHE, true> : qk_norm_rope_kernel<CACHE, false>), grid_of(rope_workgroups(p.T, p.heads)), dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
