@@ -476,7 +476,8 @@ int tl_paged_slots(tl_ctx* ctx, const tl_paged_dims* dims /*host*/, const int* c
  *   q_weight, k_weight dev bf16[128], both or neither (NULL: no norm);  positions dev int[T]
  *   cos_sin dev fp32 [max_position, rot_dim]: cosines of the rot_dim/2 angles of a position, then their sines
  *   rot_dim a multiple of 16 up to 128; 0 = no rotation (positions and cos_sin may be NULL)
- * A row whose position is outside [0, max_position) is left as it was.  Strides multiples of 8, pointers 16-byte aligned.
+ * A row whose position is outside [0, max_position) is left as it was.  Strides multiples of 8, pointers 16-byte aligned; other than
+ * in place no output may overlap an input.  The sum of a head's squares has to fit fp32 (elements below 2^60).
  * Before tl_sp_ag_attention: on the local query and key shards.
  */
 int tl_qk_norm_rope(tl_ctx* ctx, const void* q /*dev*/, long long q_stride, const void* k /*dev*/, long long k_stride, void* q_out /*dev*/,
