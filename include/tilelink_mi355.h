@@ -382,6 +382,81 @@ int tl_moe_gemm_scatter_rs(tl_ctx* ctx, const void* x2, const void* w2, const in
                            size_t ws_bytes, void* compute_stream, void* comm_stream);
 
 /*
+ * A mixture-of-experts layer in training: its parts one by one, with what a backward pass needs.  tl_moe_route chooses the experts; row (t, j),
+ * number t*topk + j, is token t at its j-th expert.
+ *   tl_moe_sort                                  the rows in the order of their experts, and the place of every row in it
+ *   tl_moe_dispatch, tl_moe_dispatch_grad        token rows into that order, and the gradient back to the tokens
+ *   tl_moe_gemm, _grad_x, _grad_w                every expert's product on its rows, and the gradients of rows and weights
+ *   tl_moe_combine, tl_moe_combine_grad          rows back to their tokens with their weights, and the gradients of rows and weights
+ *   tl_moe_route_grad                            the gradient of the gate's logits from that of the routing weights
+ * Matrices are bf16, products and sums fp32, every result rounded once.  No call reads a number of rows on the host: a step can be
+ * captured into a HIP graph and replayed with another routing.  All results are the same from run to run.
+ *
+ * Sorted matrices hold max_rows rows, T*topk or fewer.  A place (entry of row_pos) outside [0, max_rows) -- an expert of another rank, a
+ * dropped token, a full buffer -- takes no part: it adds nothing to its token, its weight's gradient is zero, its weight may hold
+ * anything.  No two rows that take part may have one place.  Rows of the sorted matrices that nobody's place names are left as they were.
+ * topk <= 32, T*topk < 2^31, H % 8 == 0; matrices 16-byte aligned, numbers 4-byte.  Unless it says so no output may overlap an input.
+ */
+
+/* The rows whose expert lies in [first_expert, first_expert + E) -- this rank's, all of them with 0 and the number of experts --, sorted by expert, ascending
+ * row number inside an expert; with tl_moe_route's ids the order of its sorted_row.
+ *   topk_ids        dev int[T, topk]: any values; a row whose expert is none of ours takes no part
+ *   expert_offsets  dev int[E+1] (written): expert e owns the places [expert_offsets[e], expert_offsets[e+1])
+ *   sorted_row      dev int[T*topk] (the first expert_offsets[E] are written): the row at a place
+ *   row_pos         dev int[T, topk] (written): the place of a row, -1 where it takes no part
+ *   workspace       dev, bytes from tl_moe_sort_query (host call): needs no preparation, nothing of it is kept
+ * E <= 256, T*topk <= 2^20.  Enqueued on `stream`. */
+int tl_moe_sort_query(const tl_ctx* ctx, int T, int topk, int E, size_t* ws_bytes /*host*/);
+int tl_moe_sort(tl_ctx* ctx, const int* topk_ids /*dev*/, int T, int topk, int first_expert, int E, int* expert_offsets /*dev*/, int* sorted_row /*dev*/,
+                int* row_pos /*dev*/, void* workspace /*dev*/, size_t ws_bytes, void* stream);
+
+/* xs[row_pos[t,j], :] = x[t, :].   x dev [T, H], xs dev [max_rows, H] (written). */
+int tl_moe_dispatch(tl_ctx* ctx, const void* x /*dev*/, const int* row_pos /*dev*/, int T, int H, int topk, int max_rows, void* xs /*dev*/, void* stream);
+
+/* dx[t, :] = bf16( sum_j dxs[row_pos[t,j], :] ), in the order of j; zero for a token without rows.   dxs dev [max_rows, H], dx dev [T, H] (written). */
+int tl_moe_dispatch_grad(tl_ctx* ctx, const void* dxs /*dev*/, const int* row_pos /*dev*/, int T, int H, int topk, int max_rows, void* dx /*dev*/, void* stream);
+
+/* out[t, :] = bf16( add[t, :] + sum_j topk_w[t,j] ys[row_pos[t,j], :] ).   ys dev [max_rows, H], topk_w dev fp32 [T, topk], out dev [T, H] (written);
+ * add dev [T, H] (a residual, a shared expert's output) or NULL; out may be add. */
+int tl_moe_combine(tl_ctx* ctx, const void* ys /*dev*/, const float* topk_w /*dev*/, const int* row_pos /*dev*/, int T, int H, int topk, int max_rows,
+                   const void* add /*dev*/, void* out /*dev*/, void* stream);
+
+/* dys[row_pos[t,j], :] = bf16( topk_w[t,j] dout[t, :] ),  dtopk_w[t,j] = sum_h dout[t,h] ys[row_pos[t,j], h].
+ *   dout dev [T, H], ys dev [max_rows, H];  dys dev [max_rows, H] (written; may be ys), dtopk_w dev fp32 [T, topk] (written).
+ * (The gradient of tl_moe_combine's `add` is dout.) */
+int tl_moe_combine_grad(tl_ctx* ctx, const void* dout /*dev*/, const void* ys /*dev*/, const float* topk_w /*dev*/, const int* row_pos /*dev*/, int T, int H,
+                        int topk, int max_rows, void* dys /*dev*/, float* dtopk_w /*dev*/, void* stream);
+
+/* Gradient of tl_moe_route's weights.  With p = softmax over all E logits of a token and e_j its chosen experts:
+ *   renormalize == 0:  w_j = p_{e_j},  dlogits_i = p_i ( sum_{j: e_j = i} dtopk_w_j - sum_k p_{e_k} dtopk_w_k )
+ *   otherwise:         w_j = p_{e_j} / sum_k p_{e_k},  dlogits_i = sum_{j: e_j = i} w_j ( dtopk_w_j - sum_k w_k dtopk_w_k )
+ *   gate_logits dev fp32 [T, E], topk_ids dev int[T, topk], dtopk_w dev fp32 [T, topk];  dlogits dev fp32 [T, E] (written; may be gate_logits)
+ * An id outside [0, E) is no choice: it has no weight, its dtopk_w is not read.  A logit of -inf has a gradient of zero; so have all of a
+ * token whose logits -- whose chosen ones, with renormalize -- are all -inf, which has no weights.  topk <= E <= 256, T <= 2^24. */
+int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits /*dev*/, const int* topk_ids /*dev*/, const float* dtopk_w /*dev*/, int T, int E, int topk,
+                      int renormalize, float* dlogits /*dev*/, void* stream);
+
+/* The experts' products.  X_e are the rows [expert_offsets[e], expert_offsets[e+1]) of x, dY_e those of dy, W_e = w[e]:
+ *   tl_moe_gemm         Y_e = bf16( X_e . W_e )
+ *   tl_moe_gemm_grad_x  dX_e = bf16( dY_e . W_e^T )
+ *   tl_moe_gemm_grad_w  dW_e = bf16( X_e^T . dY_e ), or with dw_f32 != 0 in fp32 and unrounded, added to dw_add[e] where that is not NULL
+ *   x, dx dev [max_rows, K], y, dy dev [max_rows, N], w dev [E, K, N] bf16;  dw dev [E, K, N] bf16, or fp32 with dw_f32;  dw_add dev fp32
+ *     [E, K, N] or NULL (an accumulator over several batches: dw may be dw_add)
+ *   expert_offsets dev int[E+1] ascending, from tl_moe_sort or tl_moe_route; of rows from max_rows on none is read or written
+ * Rows that are no expert's are left as they were.  An expert without rows has dW_e = 0 (+ dw_add[e]).
+ *   workspace dev, 128-byte aligned, bytes from tl_moe_gemm_query (host call; `way` one of TL_MOE_*), zeroed once: zero again where it has
+ *     to be after every call, so that calls and graphs that follow each other may share it, whatever their sizes.  One call at a time.
+ * K % 8 == 0, N % 8 == 0, up to 2^20; E <= 256. */
+enum { TL_MOE_FORWARD = 0, TL_MOE_GRAD_X = 1, TL_MOE_GRAD_W = 2 };
+int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, int E, size_t* ws_bytes /*host*/);
+int tl_moe_gemm(tl_ctx* ctx, const void* x /*dev*/, const void* w /*dev*/, const int* expert_offsets /*dev*/, int max_rows, int K, int N, int E, void* y /*dev*/,
+                void* workspace /*dev*/, size_t ws_bytes, void* stream);
+int tl_moe_gemm_grad_x(tl_ctx* ctx, const void* dy /*dev*/, const void* w /*dev*/, const int* expert_offsets /*dev*/, int max_rows, int K, int N, int E,
+                       void* dx /*dev*/, void* workspace /*dev*/, size_t ws_bytes, void* stream);
+int tl_moe_gemm_grad_w(tl_ctx* ctx, const void* x /*dev*/, const void* dy /*dev*/, const int* expert_offsets /*dev*/, int max_rows, int K, int N, int E,
+                       const float* dw_add /*dev*/, void* dw /*dev*/, int dw_f32, void* workspace /*dev*/, size_t ws_bytes, void* stream);
+
+/*
  * Sequence-parallel attention: AllGather of K and V overlapped with flash attention of the local queries
  * (paper: "Kernel Design", AG KV + self-attention; evaluation, sequence-parallel self-attention).
  *   O[i,hd,:] = bf16( sum_j softmax_j( scale * Q[i,hd,:] . K[j,hd,:] ) V[j,hd,:] ),  fp32 scores, statistics and accumulation,

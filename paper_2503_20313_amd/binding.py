@@ -23,6 +23,7 @@ TL_OK, TL_ERR_INVALID_ARG, TL_ERR_UNSUPPORTED_SHAPE, TL_ERR_WORKSPACE_TOO_SMALL,
 TL_COMM_NONE, TL_COMM_WAVES, TL_COMM_STREAM, TL_COMM_SIDE_KERNEL, TL_COMM_EXTERNAL, TL_COMM_COPY_ENGINE = 0, 1, 2, 3, 4, 5
 TL_ORDER_NATURAL, TL_ORDER_RING, TL_ORDER_OWN_FIRST, TL_ORDER_ARRIVAL = 0, 1, 2, 3
 TL_ACT_SILU_MUL, TL_ACT_GELU_MUL = 1, 2
+TL_MOE_FORWARD, TL_MOE_GRAD_X, TL_MOE_GRAD_W = 0, 1, 2
 TL_OP_AG_GEMM, TL_OP_GEMM_RS, TL_OP_MOE_AG_GATHER_GEMM, TL_OP_MOE_GEMM_SCATTER_RS, TL_OP_SP_AG_ATTENTION = 0, 1, 2, 3, 4
 
 
@@ -79,6 +80,17 @@ _lib.tl_moe_ag_gather_gemm.argtypes = [_vp, ctypes.POINTER(_vp), _vp, _vp, _vp, 
 _lib.tl_moe_ag_gather_gemm_act_mul.argtypes = [_vp, ctypes.POINTER(_vp), _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _u, _vp, _sz, _vp, _vp]
 _lib.tl_moe_gemm_scatter_rs.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp,
                                         _i, _i, _i, _i, _i, _vp, _u, _vp, _sz, _vp, _vp]
+_lib.tl_moe_sort_query.argtypes = [_vp, _i, _i, _i, ctypes.POINTER(_sz)]
+_lib.tl_moe_sort.argtypes = [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.tl_moe_dispatch.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp]
+_lib.tl_moe_dispatch_grad.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp]
+_lib.tl_moe_combine.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]
+_lib.tl_moe_combine_grad.argtypes = [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]
+_lib.tl_moe_route_grad.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp]
+_lib.tl_moe_gemm_query.argtypes = [_vp, _i, _i, _i, _i, _i, ctypes.POINTER(_sz)]
+_lib.tl_moe_gemm.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _sz, _vp]
+_lib.tl_moe_gemm_grad_x.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _sz, _vp]
+_lib.tl_moe_gemm_grad_w.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _sz, _vp]
 _lib.tl_sp_ag_attention.restype = _i
 _lib.tl_sp_ag_attention.argtypes = [_vp, _vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, _vp, _vp, _i, _i, _i, _i, ctypes.c_float, _vp, _u, _vp, _sz,
                                     _vp, _vp]
@@ -275,6 +287,56 @@ def tl_moe_gemm_scatter_rs(ctx, x2, w2, sorted_row, tile_tables, n_tiles, topk_w
     _check(_lib.tl_moe_gemm_scatter_rs(ctx, _ptr(x2), _ptr(w2), _ptr(sorted_row), _ptr(tile_tables), _ptr(n_tiles), _ptr(topk_w), _ptr(scatter_buf),
                                        _ptr(partial), _ptr_array(peer_recv), _ptr_array(peer_push), _ptr(out), T, H, I, E, topk, _ptr(flags), epoch,
                                        _ptr(workspace), ws_bytes, _stream(compute_stream), _stream(comm_stream)))
+
+
+def tl_moe_sort_query(ctx, T, topk, E):
+    ws = _sz()
+    _check(_lib.tl_moe_sort_query(ctx, T, topk, E, ctypes.byref(ws)))
+    return ws.value
+
+
+def tl_moe_sort(ctx, topk_ids, T, topk, first_expert, E, expert_offsets, sorted_row, row_pos, workspace, ws_bytes, stream=None):
+    _check(_lib.tl_moe_sort(ctx, _ptr(topk_ids), T, topk, first_expert, E, _ptr(expert_offsets), _ptr(sorted_row), _ptr(row_pos), _ptr(workspace), ws_bytes,
+                            _stream(stream)))
+
+
+def tl_moe_dispatch(ctx, x, row_pos, T, H, topk, max_rows, xs, stream=None):
+    _check(_lib.tl_moe_dispatch(ctx, _ptr(x), _ptr(row_pos), T, H, topk, max_rows, _ptr(xs), _stream(stream)))
+
+
+def tl_moe_dispatch_grad(ctx, dxs, row_pos, T, H, topk, max_rows, dx, stream=None):
+    _check(_lib.tl_moe_dispatch_grad(ctx, _ptr(dxs), _ptr(row_pos), T, H, topk, max_rows, _ptr(dx), _stream(stream)))
+
+
+def tl_moe_combine(ctx, ys, topk_w, row_pos, T, H, topk, max_rows, add, out, stream=None):
+    _check(_lib.tl_moe_combine(ctx, _ptr(ys), _ptr(topk_w), _ptr(row_pos), T, H, topk, max_rows, _ptr(add), _ptr(out), _stream(stream)))
+
+
+def tl_moe_combine_grad(ctx, dout, ys, topk_w, row_pos, T, H, topk, max_rows, dys, dtopk_w, stream=None):
+    _check(_lib.tl_moe_combine_grad(ctx, _ptr(dout), _ptr(ys), _ptr(topk_w), _ptr(row_pos), T, H, topk, max_rows, _ptr(dys), _ptr(dtopk_w), _stream(stream)))
+
+
+def tl_moe_route_grad(ctx, gate_logits, topk_ids, dtopk_w, T, E, topk, renormalize, dlogits, stream=None):
+    _check(_lib.tl_moe_route_grad(ctx, _ptr(gate_logits), _ptr(topk_ids), _ptr(dtopk_w), T, E, topk, int(renormalize), _ptr(dlogits), _stream(stream)))
+
+
+def tl_moe_gemm_query(ctx, way, max_rows, K, N, E):
+    ws = _sz()
+    _check(_lib.tl_moe_gemm_query(ctx, way, max_rows, K, N, E, ctypes.byref(ws)))
+    return ws.value
+
+
+def tl_moe_gemm(ctx, x, w, expert_offsets, max_rows, K, N, E, y, workspace, ws_bytes, stream=None):
+    _check(_lib.tl_moe_gemm(ctx, _ptr(x), _ptr(w), _ptr(expert_offsets), max_rows, K, N, E, _ptr(y), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def tl_moe_gemm_grad_x(ctx, dy, w, expert_offsets, max_rows, K, N, E, dx, workspace, ws_bytes, stream=None):
+    _check(_lib.tl_moe_gemm_grad_x(ctx, _ptr(dy), _ptr(w), _ptr(expert_offsets), max_rows, K, N, E, _ptr(dx), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def tl_moe_gemm_grad_w(ctx, x, dy, expert_offsets, max_rows, K, N, E, dw_add, dw, dw_f32, workspace, ws_bytes, stream=None):
+    _check(_lib.tl_moe_gemm_grad_w(ctx, _ptr(x), _ptr(dy), _ptr(expert_offsets), max_rows, K, N, E, _ptr(dw_add), _ptr(dw), int(dw_f32), _ptr(workspace), ws_bytes,
+                                   _stream(stream)))
 
 
 def tl_attn_query(ctx, S, heads, head_dim, causal):

@@ -30,9 +30,12 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-template <int BM_, int BN_, int WM_, int WN_, int BK_ = 32, int NS_ = 4>
+// A_KM: A is given as [K, M] (M contiguous), B_NK: B as [N, K] (K contiguous): the operands of the products that transpose one of
+// their matrices.  An operand's tile has the LDS layout of its place in memory, rows of K or K rows, and the reads that go with it.
+template <int BM_, int BN_, int WM_, int WN_, int BK_ = 32, int NS_ = 4, bool A_KM_ = false, bool B_NK_ = false>
 struct TileCfg {
   static constexpr int BM = BM_, BN = BN_, BK = BK_, NS = NS_, WM = WM_, WN = WN_;
+  static constexpr bool A_KM = A_KM_, B_NK = B_NK_;
   static constexpr int NWAVES = WM * WN, NTHREADS = NWAVES * 64;
   static constexpr int WTM = BM / WM, WTN = BN / WN, MT = WTM / 32, NT = WTN / 32;
   static constexpr int SL = BK / 16;              // 16-wide k-slices (one MFMA deep) per stage
@@ -43,6 +46,8 @@ struct TileCfg {
   static constexpr int B_CPR = BN / 8;            // 16-byte chunks per k-row of the B tile
   static constexpr int B_LOADS = BK * B_CPR / 64;
   static constexpr bool B_SWZ = (B_CPR % 16) == 0;
+  static constexpr int AT_CPR = BM / 8;           // the same of an A tile that lies in k-rows
+  static constexpr bool AT_SWZ = (AT_CPR % 16) == 0;
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BK * BN * 2, STAGE_BYTES = A_BYTES + B_BYTES;
   // Epilogue staging: every wave passes its WTM x WTN result through an LDS region of its own, rows padded by 16 bytes.
   static constexpr int EP_PITCH = WTN * 2 + 16;
@@ -216,6 +221,12 @@ struct GatedRows {
   }
 };
 
+// Whether a functor takes the accumulators themselves: Out::F32, out.store4(row, col, v) stores 4 of them (col % 4 == 0).
+template <class Out, class = void>
+struct StoresF32 : std::false_type {};
+template <class Out>
+struct StoresF32<Out, std::void_t<decltype(Out::F32)>> : std::integral_constant<bool, Out::F32> {};
+
 // Computes one output tile.  `a` points at column 0 of the A rows: tile row r is A row r, or A row
 // a_rows[r] / a_div when a_rows is given (row gather: the tile's rows are picked by index; the picked rows must lie
 // within 4 GiB of `a`); `b` points at row 0 of B at the tile's first column; both are the same for every lane.
@@ -230,6 +241,9 @@ struct GatedRows {
 // masked.  K % 8 == 0 (rows of A start on 16-byte boundaries); a last K step shorter than BK is filled up with zeros:
 // the 16-byte pieces of it that lie beyond K are loaded from a block of zeros instead of from the matrices (every lane
 // of a direct-to-LDS load names its own global address), so both operands of the surplus products are zero.
+// Cfg::A_KM: `a` points at k-row 0 of A at the tile's first row (rows % 8 == 0; a_rows is not used); Cfg::B_NK: `b` points at column 0
+// of the row of B^T that is the tile's first column.  With A in k-rows and B in k-rows any K will do: each piece of 16 bytes then
+// belongs to one k.
 // All threads of the workgroup must call it; it ends with all LDS accesses complete.
 //
 // LDS: the NS stages of the A tile, then the NS stages of the B tile.  The K loop is unrolled NS times so that the ring
@@ -257,29 +271,44 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
     int j = wave + i * Cfg::NWAVES;  // wave-load index: LDS slots [64j, 64j+64)
     if (j >= Cfg::A_LOADS) j = Cfg::A_LOADS - 1;
     int slot = j * 64 + lane;
-    int row = slot / Cfg::A_CPR;
-    int chunk = (slot % Cfg::A_CPR) ^ ((row / Cfg::A_RPB) % Cfg::A_CPR);  // logical 16-byte chunk stored at this slot
-    int grow = row < rows ? row : rows - 1;
-    if (a_rows) grow = a_rows[grow] / a_div;
-    a_voff[i] = (unsigned)grow * (unsigned)(lda * 2) + (unsigned)(chunk * 16);
-    if (chunk * 8 < k_tail) tail_ok |= 1u << i;
+    if constexpr (Cfg::A_KM) {
+      const int k = slot / Cfg::AT_CPR, mcp = slot - k * Cfg::AT_CPR;
+      const int mc = Cfg::AT_SWZ ? (mcp ^ ((k & 3) << 2)) : mcp;
+      const int r = mc * 8 < rows ? mc * 8 : rows - 8;
+      a_voff[i] = (unsigned)k * (unsigned)(lda * 2) + (unsigned)(r * 2);
+      if (k < k_tail) tail_ok |= 1u << i;
+    } else {
+      int row = slot / Cfg::A_CPR;
+      int chunk = (slot % Cfg::A_CPR) ^ ((row / Cfg::A_RPB) % Cfg::A_CPR);  // logical 16-byte chunk stored at this slot
+      int grow = row < rows ? row : rows - 1;
+      if (a_rows) grow = a_rows[grow] / a_div;
+      a_voff[i] = (unsigned)grow * (unsigned)(lda * 2) + (unsigned)(chunk * 16);
+      if (chunk * 8 < k_tail) tail_ok |= 1u << i;
+    }
   }
 #pragma unroll
   for (int i = 0; i < Cfg::B_PER_WAVE; i++) {
     int j = wave + i * Cfg::NWAVES;
     if (j >= Cfg::B_LOADS) j = Cfg::B_LOADS - 1;
     int slot = j * 64 + lane;
-    int k = slot / Cfg::B_CPR, ncp = slot - k * Cfg::B_CPR;
-    int nc = Cfg::B_SWZ ? (ncp ^ ((k & 3) << 2)) : ncp;
-    int col = nc * 8 < cols ? nc * 8 : cols - 8;
-    b_voff[i] = (unsigned)k * (unsigned)(ldb * 2) + (unsigned)(col * 2);
-    if (k < k_tail) tail_ok |= 1u << (Cfg::A_PER_WAVE + i);
+    if constexpr (Cfg::B_NK) {
+      const int n = slot / Cfg::A_CPR, chunk = (slot % Cfg::A_CPR) ^ ((n / Cfg::A_RPB) % Cfg::A_CPR);
+      b_voff[i] = (unsigned)(n < cols ? n : cols - 1) * (unsigned)(ldb * 2) + (unsigned)(chunk * 16);
+      if (chunk * 8 < k_tail) tail_ok |= 1u << (Cfg::A_PER_WAVE + i);
+    } else {
+      int k = slot / Cfg::B_CPR, ncp = slot - k * Cfg::B_CPR;
+      int nc = Cfg::B_SWZ ? (ncp ^ ((k & 3) << 2)) : ncp;
+      int col = nc * 8 < cols ? nc * 8 : cols - 8;
+      b_voff[i] = (unsigned)k * (unsigned)(ldb * 2) + (unsigned)(col * 2);
+      if (k < k_tail) tail_ok |= 1u << (Cfg::A_PER_WAVE + i);
+    }
   }
   // scalar registers hold the two bases; they advance by one K step per requested stage
   const char* a_base = (const char*)uniform64((unsigned long long)a);
   const char* b_base = (const char*)uniform64((unsigned long long)b);
   // (made uniform explicitly: inside a function that is not inlined the arguments arrive in vector registers)
-  const long b_step = (long)uniform64((unsigned long long)(ldb * Cfg::BK * 2));  // bytes per K-step
+  const long b_step = Cfg::B_NK ? Cfg::BK * 2 : (long)uniform64((unsigned long long)(ldb * Cfg::BK * 2));  // bytes per K-step
+  const long a_step = Cfg::A_KM ? (long)uniform64((unsigned long long)(lda * Cfg::BK * 2)) : Cfg::BK * 2;
   const unsigned smem_u = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem);
 
   // Load number L (0..LPW-1) of this wave's share of the stage the bases point at, into ring slot `slot`:
@@ -305,7 +334,7 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
   };
   auto issue_stage = [&](int slot, auto tail_c) {
     static_for<0, LPW>([&](auto l_c) { issue_load(slot, l_c, tail_c); });
-    a_base += Cfg::BK * 2;
+    a_base += a_step;
     b_base += b_step;
   };
 
@@ -316,6 +345,17 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
   const char* a_rd[SL];
 #pragma unroll
   for (int sl = 0; sl < SL; sl++) a_rd[sl] = smem + a_row * Cfg::A_PITCH + ((a_x ^ (2 * sl)) << 4);
+  // ... from k-rows (A_KM): the transposing reads of the B fragment below, on the A tile
+  const char* at_rd[Cfg::MT];
+  if constexpr (Cfg::A_KM) {
+    const int k = 8 * (lane >> 5) + ((lane & 15) >> 2), m = wm * Cfg::WTM + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int mt = 0; mt < Cfg::MT; mt++) {
+      int mc = (m + mt * 32) >> 3;
+      if (Cfg::AT_SWZ) mc ^= (k & 3) << 2;
+      at_rd[mt] = smem + (k * Cfg::AT_CPR + mc) * 16 + (m & 4) * 2;
+    }
+  }
   // B fragment (MFMA A operand) via transposing reads: lane supplies the address of k-row
   // 8*(lane/32) + (lane%16)/4 (+4 for the second read), columns 16*((lane/16)%2) + 4*(lane%4)..+3.
   const int b_k = 8 * (lane >> 5) + ((lane & 15) >> 2);
@@ -327,6 +367,13 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
     int nc = n >> 3;
     if (Cfg::B_SWZ) nc ^= (b_k & 3) << 2;
     b_rd[nt] = smem + A_REGION + (b_k * Cfg::B_CPR + nc) * 16 + (n & 4) * 2;
+  }
+  // ... from rows of K (B_NK): the plain reads of the A fragment
+  const char* bn_rd[SL];
+  if constexpr (Cfg::B_NK) {
+    const int row = wn * Cfg::WTN + (lane & 31), x = (lane >> 5) ^ ((row / Cfg::A_RPB) % Cfg::A_CPR);
+#pragma unroll
+    for (int sl = 0; sl < SL; sl++) bn_rd[sl] = smem + A_REGION + row * Cfg::A_PITCH + ((x ^ (2 * sl)) << 4);
   }
 
   floatx16 acc[Cfg::MT][Cfg::NT];
@@ -344,16 +391,26 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
   constexpr int N_MFMA = Cfg::MT * Cfg::NT;
   auto read_frag = [&](int slot, auto sl_c, auto buf_c, auto r_c) {
     constexpr int BUF = decltype(buf_c)::value, R = decltype(r_c)::value, S = decltype(sl_c)::value;
+    typedef short short8_t __attribute__((ext_vector_type(8)));
     if constexpr (R < Cfg::NT) {
-      const char* p = b_rd[R] + slot * Cfg::B_BYTES + S * 16 * Cfg::B_CPR * 16;
-      short4_t lo = lds_read_tr(p);
-      short4_t hi = lds_read_tr(p + 4 * Cfg::B_CPR * 16);
-      typedef short short8_t __attribute__((ext_vector_type(8)));
-      short8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      bfr[BUF][R] = __builtin_bit_cast(bf16x8, v);
+      if constexpr (Cfg::B_NK) {
+        bfr[BUF][R] = *(const bf16x8*)(bn_rd[S] + slot * Cfg::B_BYTES + R * 32 * Cfg::A_PITCH);
+      } else {
+        const char* p = b_rd[R] + slot * Cfg::B_BYTES + S * 16 * Cfg::B_CPR * 16;
+        short4_t lo = lds_read_tr(p);
+        short4_t hi = lds_read_tr(p + 4 * Cfg::B_CPR * 16);
+        short8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        bfr[BUF][R] = __builtin_bit_cast(bf16x8, v);
+      }
     } else {
       constexpr int MTI = R - Cfg::NT;
-      af[BUF][MTI] = *(const bf16x8*)(a_rd[S] + slot * Cfg::A_BYTES + MTI * 32 * Cfg::A_PITCH);
+      if constexpr (Cfg::A_KM) {
+        const char* p = at_rd[MTI] + slot * Cfg::A_BYTES + S * 16 * Cfg::AT_CPR * 16;
+        const short4_t lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * Cfg::AT_CPR * 16);
+        af[BUF][MTI] = __builtin_bit_cast(bf16x8, (short8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      } else {
+        af[BUF][MTI] = *(const bf16x8*)(a_rd[S] + slot * Cfg::A_BYTES + MTI * 32 * Cfg::A_PITCH);
+      }
     }
   };
   using std::integral_constant;
@@ -437,7 +494,7 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
       slice(integral_constant<int, S & 1>{}, integral_constant<int, S + 1>{}, yes{}, nslot, integral_constant<int, S + 1>{}, more_c, tail_c, slot);
     });
     if constexpr (MORE) {
-      a_base += Cfg::BK * 2;
+      a_base += a_step;
       b_base += b_step;
     }
   };
@@ -465,6 +522,21 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
     if (!split.combine(acc)) return;   // (uniform) the workgroup that comes last stores the tile
   }
 
+  if constexpr (StoresF32<Out>::value) {
+    // a lane's four consecutive columns at a time: 32 rows of 32 bytes an instruction, whole lines after four of them
+#pragma unroll
+    for (int mt = 0; mt < Cfg::MT; mt++) {
+      const int row = wm * Cfg::WTM + mt * 32 + (lane & 31);
+#pragma unroll
+      for (int nt = 0; nt < Cfg::NT; nt++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          const int col = wn * Cfg::WTN + nt * 32 + g * 8 + (lane >> 5) * 4;
+          if (row < rows && col < cols) out.store4(row, col, floatx4{acc[mt][nt][g * 4], acc[mt][nt][g * 4 + 1], acc[mt][nt][g * 4 + 2], acc[mt][nt][g * 4 + 3]});
+        }
+    }
+    return;
+  } else {
   // ---- epilogue.  Accumulator register e of lane l holds C[row = l%32][col = (e/4)*8 + (l/32)*4 + e%4] of its 32x32
   // block: stored from there, every store instruction would touch 32 rows with 16 bytes each.  Instead the wave
   // rounds its result to bf16 into an LDS region of its own and reads it back row-wise, so that a store instruction
@@ -518,6 +590,7 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
   }
   // the next tile's loads overwrite the staging regions: all LDS reads must be done; the global stores need not be
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
 }
 
 }  // namespace tl
