@@ -444,9 +444,9 @@ int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits /*dev*/, const int* 
  *     [E, K, N] or NULL (an accumulator over several batches: dw may be dw_add)
  *   expert_offsets dev int[E+1] ascending, from tl_moe_sort or tl_moe_route; of rows from max_rows on none is read or written
  * Rows that are no expert's are left as they were.  An expert without rows has dW_e = 0 (+ dw_add[e]).
- *   workspace dev, 128-byte aligned, bytes from tl_moe_gemm_query (host call; `way` one of TL_MOE_*), zeroed once: zero again where it has
- *     to be after every call, so that calls and graphs that follow each other may share it, whatever their sizes.  One call at a time.
- * K % 8 == 0, N % 8 == 0, up to 2^20; E <= 256. */
+ *   workspace dev, 128-byte aligned, bytes from tl_moe_gemm_query (host call; `way` one of TL_MOE_*): needs no preparation, nothing of it is kept,
+ *     so that calls and graphs that follow each other may share it, whatever their sizes.  One call at a time.
+ * K % 8 == 0, N % 8 == 0, up to 2^20; E <= 256; for dW E*ceil(K/128)*ceil(N/128) < 2^22. */
 enum { TL_MOE_FORWARD = 0, TL_MOE_GRAD_X = 1, TL_MOE_GRAD_W = 2 };
 int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, int E, size_t* ws_bytes /*host*/);
 int tl_moe_gemm(tl_ctx* ctx, const void* x /*dev*/, const void* w /*dev*/, const int* expert_offsets /*dev*/, int max_rows, int K, int N, int E, void* y /*dev*/,

@@ -221,7 +221,7 @@ struct GatedRows {
   }
 };
 
-// Whether a functor takes the accumulators themselves: Out::F32, out.store4(row, col, v) stores 4 of them (col % 4 == 0).
+// Whether a functor takes the sums in fp32: Out::F32, out.store4(row, col, v) stores four of them (col % 4 == 0) with out.load4(row, col) added.
 template <class Out, class = void>
 struct StoresF32 : std::false_type {};
 template <class Out>
@@ -523,18 +523,35 @@ __device__ __forceinline__ void gemm_tile(const bf16_t* __restrict__ a, long lda
   }
 
   if constexpr (StoresF32<Out>::value) {
-    // a lane's four consecutive columns at a time: 32 rows of 32 bytes an instruction, whole lines after four of them
+    // Through LDS as below, in fp32, 32 rows of the wave tile at a time: whole lines leave and, where the functor adds to what it finds
+    // somewhere, arrive.  (A lane's four columns stored from where they are: 64 M sums added into fp32 took 180 us more than 128 MB of bf16.)
+    constexpr int P = Cfg::WTN * 4 + 16, CPR = Cfg::WTN / 4, ITERS = 32 * CPR / 64;
+    static_assert(Cfg::NWAVES * 32 * P <= Cfg::LDS_BYTES, "the staging regions fit");
+    char* ep = smem + wave * (32 * P);
 #pragma unroll
     for (int mt = 0; mt < Cfg::MT; mt++) {
-      const int row = wm * Cfg::WTM + mt * 32 + (lane & 31);
 #pragma unroll
       for (int nt = 0; nt < Cfg::NT; nt++)
 #pragma unroll
-        for (int g = 0; g < 4; g++) {
-          const int col = wn * Cfg::WTN + nt * 32 + g * 8 + (lane >> 5) * 4;
-          if (row < rows && col < cols) out.store4(row, col, floatx4{acc[mt][nt][g * 4], acc[mt][nt][g * 4 + 1], acc[mt][nt][g * 4 + 2], acc[mt][nt][g * 4 + 3]});
+        for (int g = 0; g < 4; g++)
+          *(floatx4*)(ep + (lane & 31) * P + (nt * 32 + g * 8 + (lane >> 5) * 4) * 4) =
+              floatx4{acc[mt][nt][g * 4], acc[mt][nt][g * 4 + 1], acc[mt][nt][g * 4 + 2], acc[mt][nt][g * 4 + 3]};
+      const int r0 = wm * Cfg::WTM + mt * 32 + lane / CPR, c = wn * Cfg::WTN + (lane % CPR) * 4;
+      floatx4 add[ITERS];
+#pragma unroll
+      for (int i = 0; i < ITERS; i++)
+        if (r0 + i * (64 / CPR) < rows && c < cols) add[i] = out.load4(r0 + i * (64 / CPR), c);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < ITERS; i++)
+        if (r0 + i * (64 / CPR) < rows && c < cols) {
+          floatx4 v = *(const floatx4*)(ep + (lane / CPR + i * (64 / CPR)) * P + (lane % CPR) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; e++) v[e] += add[i][e];
+          out.store4(r0 + i * (64 / CPR), c, v);
         }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     return;
   } else {
   // ---- epilogue.  Accumulator register e of lane l holds C[row = l%32][col = (e/4)*8 + (l/32)*4 + e%4] of its 32x32

@@ -18,27 +18,42 @@ struct ProductParams {
   float* out32;
   int max_rows, K, N, E;
   int nbm, nbn;            // column blocks; for dW also row blocks of an expert's K x N
-  int swizzle, group_m;
+  int group_m;
 };
 
-// dW in fp32: (add +) the product.
-struct AddRows32 {
+// Where dW goes: stored as streaming (the layer's weights are larger than the caches, and nobody reads their gradient soon).
+struct GradRows16 {
+  static constexpr bool SCALED = false, GATED = false;
+  bf16_t* c;
+  long ldc;
+  __device__ __forceinline__ bf16_t* row(int r, float& scale) const { return c + (long)r * ldc; }
+  __device__ __forceinline__ void group(int /*r0*/) const {}
+  __device__ __forceinline__ void store(int r, int col, u32x4 v) const { __builtin_nontemporal_store(v, (u32x4*)(c + (long)r * ldc + col)); }
+};
+struct GradRows32 {
   static constexpr bool SCALED = false, GATED = false, F32 = true;
-  const float* add;
+  const float* add;        // or null
   float* c;
   long ldc;
   __device__ __forceinline__ bf16_t* row(int, float&) const { return nullptr; }
   __device__ __forceinline__ void group(int) const {}
   __device__ __forceinline__ void store(int, int, u32x4) const {}
-  __device__ __forceinline__ void store4(int r, int col, floatx4 v) const {
-    const long at = (long)r * ldc + col;
-    if (add) {
-      const floatx4 a = *(const floatx4*)(add + at);
-#pragma unroll
-      for (int e = 0; e < 4; e++) v[e] += a[e];
-    }
-    *(floatx4*)(c + at) = v;
+  __device__ __forceinline__ floatx4 load4(int r, int col) const {
+    return add ? __builtin_nontemporal_load((const floatx4*)(add + (long)r * ldc + col)) : floatx4{0.f, 0.f, 0.f, 0.f};
   }
+  __device__ __forceinline__ void store4(int r, int col, floatx4 v) const { __builtin_nontemporal_store(v, (floatx4*)(c + (long)r * ldc + col)); }
+};
+
+// A part of a cut sum, as it is.
+struct PartRows {
+  static constexpr bool SCALED = false, GATED = false, F32 = true;
+  float* c;
+  long ldc;
+  __device__ __forceinline__ bf16_t* row(int, float&) const { return nullptr; }
+  __device__ __forceinline__ void group(int) const {}
+  __device__ __forceinline__ void store(int, int, u32x4) const {}
+  __device__ __forceinline__ floatx4 load4(int, int) const { return floatx4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void store4(int r, int col, floatx4 v) const { *(floatx4*)(c + (long)r * ldc + col) = v; }
 };
 
 // Rows of expert e, whatever expert_offsets holds: inside [0, max_rows), or none.
@@ -47,98 +62,529 @@ __device__ __forceinline__ void rows_of(const ProductParams& p, int e, int* lo, 
   *n = max(min(max(p.offsets[e + 1], 0), p.max_rows) - *lo, 0);
 }
 
-template <class Cfg, bool GRAD_X>
-__global__ void __launch_bounds__(Cfg::NTHREADS) moe_product_kernel(const ProductParams p) {
+// The number, among ascending starts, of the last start at or before x, for a wave whose lane i holds starts 4i .. 4i + 3.
+__device__ __forceinline__ int last_start(const int (&start)[4], int x) {
+  int c = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(start[i] <= x));
+  return c - 1;
+}
+// Exclusive scan over 256 numbers, lane i has 4i .. 4i + 3; returns their sum.
+__device__ __forceinline__ int scan_starts(const int (&count)[4], int (&start)[4]) {
+  const int lane = threadIdx.x & 63;
+  int v = count[0] + count[1] + count[2] + count[3];
+  const int mine = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  int at = v - mine;
+#pragma unroll
+  for (int i = 0; i < 4; i++) { start[i] = at; at += count[i]; }
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Y and dX.  An expert's rows make tiles of BM rows, and a half one where the rest fits into that (an expert's last tile is half empty in the
+// mean; with whole ones alone 16384 rows of 32 experts cost a fifth more); whole tiles first, in patches that share rows and columns in
+// a die's L2, then the half ones.
+template <class Big, class Half, bool GRAD_X>
+__global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const ProductParams p) {
+  static_assert(Big::NTHREADS == Half::NTHREADS && Big::BN == Half::BN && Big::BM == 2 * Half::BM, "the two shapes share workgroup and columns");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  __shared__ int s_lo[kMaxProductExperts], s_n[kMaxProductExperts], s_first[kMaxProductExperts + 1];
+  __shared__ int s_lo[kMaxProductExperts], s_n[kMaxProductExperts], s_at[kMaxProductExperts];     // an expert's rows, its first whole tile
   const int tid = threadIdx.x, lane = tid & 63;
-  // ---- the row tiles of all experts
-  for (int e = tid; e < kMaxProductExperts; e += Cfg::NTHREADS) {
+  for (int e = tid; e < kMaxProductExperts; e += Big::NTHREADS) {
     int lo = 0, n = 0;
     if (e < p.E) rows_of(p, e, &lo, &n);
     s_lo[e] = lo;
     s_n[e] = n;
   }
   __syncthreads();
+  int big[4], half[4], big_at[4], half_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int n = s_n[lane * 4 + i], rest = n % Big::BM;
+    half[i] = rest > 0 && rest <= Half::BM ? 1 : 0;
+    big[i] = n / Big::BM + (rest > Half::BM ? 1 : 0);
+  }
+  Sched sc;
+  sc.nbm = scan_starts(big, big_at);
+  const int n_half = scan_starts(half, half_at);
   if (tid < 64) {
-    int v = 0, mine[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) { mine[i] = (s_n[lane * 4 + i] + Cfg::BM - 1) / Cfg::BM; v += mine[i]; }
-    int scan = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(scan, d);
-      if (lane >= d) scan += o;
-    }
-    int at = scan - v;
-#pragma unroll
-    for (int i = 0; i < 4; i++) { s_first[lane * 4 + i] = at; at += mine[i]; }
-    if (lane == 63) s_first[kMaxProductExperts] = at;
+    for (int i = 0; i < 4; i++) s_at[lane * 4 + i] = big_at[i];
   }
   __syncthreads();
-  Sched sc;
-  sc.nbm = __builtin_amdgcn_readfirstlane(s_first[kMaxProductExperts]);
   sc.nbn = p.nbn;
   sc.n_tiles = sc.nbm * sc.nbn;
   sc.G = gridDim.x;
   sc.first_block = 0;
-  sc.swizzle = p.swizzle;
+  sc.swizzle = 1;
   sc.group_m = p.group_m < sc.nbm ? p.group_m : (sc.nbm > 0 ? sc.nbm : 1);
+  const int n_all = sc.n_tiles + n_half * sc.nbn;
   const int kdim = GRAD_X ? p.N : p.K, ndim = GRAD_X ? p.K : p.N;
-  for (int pos = blockIdx.x; pos < sc.n_tiles; pos += sc.G) {
-    const int tile = sched_tile(sc, pos), bm = tile / sc.nbn, bn = tile - bm * sc.nbn;
-    int e = 0;    // the last expert whose tiles start at or before bm (one without tiles starts where the next one does)
+  struct Job { bool big; int e, rows, col, cols; long at; };
+  auto job_at = [&](int pos) {
+    Job j;
+    j.big = pos < sc.n_tiles;
+    int bm, bn, r0;
+    if (j.big) {
+      const int tile = sched_tile(sc, pos);
+      bm = tile / sc.nbn;
+      bn = tile - bm * sc.nbn;
+      j.e = last_start(big_at, bm);
+      r0 = (bm - __builtin_amdgcn_readfirstlane(s_at[j.e])) * Big::BM;
+    } else {
+      bm = (pos - sc.n_tiles) / sc.nbn;
+      bn = pos - sc.n_tiles - bm * sc.nbn;
+      j.e = last_start(half_at, bm);
+      r0 = __builtin_amdgcn_readfirstlane(s_n[j.e]) / Big::BM * Big::BM;
+    }
+    j.rows = min(__builtin_amdgcn_readfirstlane(s_n[j.e]) - r0, Big::BM);
+    j.at = __builtin_amdgcn_readfirstlane(s_lo[j.e]) + r0;
+    j.col = bn * Big::BN;
+    j.cols = min(Big::BN, ndim - j.col);
+    return j;
+  };
+  for (int pos = blockIdx.x; pos < n_all; pos += gridDim.x) {
+    const Job j = job_at(pos);
+    const DenseRows out{p.out + j.at * ndim + j.col, ndim};
+    const bf16_t* a = (GRAD_X ? p.dy : p.x) + j.at * kdim;
+    const bf16_t* b = p.w + (long)j.e * p.K * p.N + (GRAD_X ? (long)j.col * p.N : (long)j.col);
+    if (j.big) gemm_tile<Big>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, kdim, smem);
+    else gemm_tile<Half>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, kdim, smem);
+  }
+}
+
+// ======================================================================================
+// Few rows for an expert (single tokens being decoded, a small batch over many experts): bound by reading the weights once.  A unit is up
+// to 64 rows of an expert times a block of output columns; NW waves take its steps along the summed axis in turn, each through a ring of
+// its own in LDS, so that no wave waits for another; their sums are joined at the end, in the order of the waves.  Per step
+//   Y^T[columns, rows] += W^T . X^T   (16x16x32 matrix instructions; a lane owns one row and four columns)
+// W as it lies (forward: 32 k-rows of 64 columns, transposing LDS reads) or along its rows (dX: 32 rows of 64 values, plain reads):
+// either way 4 KiB in pieces of a whole 128-byte line.
+// ======================================================================================
+struct FewUnit {
+  const bf16_t *x, *w;      // first row; W at the unit's first column
+  bf16_t* out;              // first row, first column
+  int ldx, ldw, ldo;
+  int rows, cols, kdim;
+  bool once;                // the weights are this unit's alone: streaming loads
+};
+
+constexpr int kFewRing = 40 * 1024;       // LDS of a wave: four waves a compute unit, with up to 140 KiB in flight together
+constexpr int kFewRows = 64;
+
+template <bool NK, int RT, bool WIDE>     // RT: row tiles of 16
+struct FewShape {
+  static constexpr int CW = (NK ? 32 : 64) * (WIDE ? 2 : 1), BK = NK ? 64 : 32, CT = CW / 16, KH = BK / 32;
+  static constexpr int PITCH = NK ? BK * 2 : CW * 2, RPL = 1024 / PITCH;     // bytes of a row of memory, rows of a load
+  static constexpr int W_LOADS = WIDE ? 8 : 4, X_LOADS = RT * BK / 32, LPS = W_LOADS + X_LOADS, STAGE = LPS * 1024;
+  static constexpr int NS = kFewRing / STAGE;
+  static_assert(NS >= 2 && NS * LPS <= 63, "ring depth, vmcnt range");
+};
+
+template <bool NK, int RT, bool WIDE, int NW>
+__device__ __forceinline__ void few_unit(const FewUnit& f, char* smem) {
+  typedef FewShape<NK, RT, WIDE> S;
+  const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, gr = lane >> 4;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int steps = (f.kdim + S::BK - 1) / S::BK;
+  const int mine = steps > wave ? (steps - wave + NW - 1) / NW : 0;
+  char* ring = smem + wave * kFewRing;
+  const unsigned ring_u = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring);
+  // ---- W: load j covers RPL rows of memory; LDS place (row, c) holds piece c ^ w_twist(row), which keeps the fragment reads apart
+  auto w_twist = [](int row) { return NK ? (row >> 1) & 7 : WIDE ? (row & 3) << 1 | ((row >> 3) & 1) << 3 : ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2; };
+  constexpr int WC = S::PITCH / 16;                 // pieces of a row
+  auto w_variant = [](int j) { return S::RPL == 8 ? j & 1 : (j >> 1) & 1; };      // bit 3 of the load's rows
+  unsigned w_off[2], x_off[S::X_LOADS];
+#pragma unroll
+  for (int j = 0; j < 2; j++) {
+    const int row = lane / WC + 8 * j;
+    w_off[j] = (unsigned)(lane / WC) * (unsigned)(f.ldw * 2) + (unsigned)(((lane % WC) ^ w_twist(row)) << 4);
+  }
+  // ---- X: rows of BK values, 16-byte pieces twisted by their row; rows that are not there repeat the last one
+  constexpr int XC = S::BK / 8;                     // pieces of a row
+  auto x_twist = [](int row) { return NK ? (row >> 1) & 7 : (row >> 2) & 3; };
+  auto x_row = [&](int q) { return q * (64 / XC) + lane / XC; };
+  auto x_piece = [&](int q) { return (lane % XC) ^ x_twist(x_row(q)); };
+#pragma unroll
+  for (int q = 0; q < S::X_LOADS; q++) x_off[q] = (unsigned)min(x_row(q), f.rows - 1) * (unsigned)(f.ldx * 2) + (unsigned)(x_piece(q) << 4);
+  const bool whole_cols = f.cols == S::CW;
+  auto issue = [&](int i, int slot) __attribute__((always_inline)) {
+    const int k0 = (wave + i * NW) * S::BK;
+    const unsigned dst = ring_u + slot * S::STAGE;
+    if (whole_cols && k0 + S::BK <= f.kdim) {
+      const char* wb = (const char*)uniform64((unsigned long long)(f.w + (NK ? (long)k0 : (long)k0 * f.ldw)));
+      const char* xb = (const char*)uniform64((unsigned long long)(f.x + k0));
+      const long w8 = (long)f.ldw * (2 * S::RPL);
+      if (f.once) {
+#pragma unroll
+        for (int j = 0; j < S::W_LOADS; j++) lds_load16_sbase_nt(wb + j * w8, w_off[w_variant(j)], dst + j * 1024);
+      } else {
+#pragma unroll
+        for (int j = 0; j < S::W_LOADS; j++) lds_load16_sbase(wb + j * w8, w_off[w_variant(j)], dst + j * 1024);
+      }
+#pragma unroll
+      for (int q = 0; q < S::X_LOADS; q++) lds_load16_sbase(xb, x_off[q], dst + (S::W_LOADS + q) * 1024);
+      return;
+    }
+    // an edge: columns beyond the last repeat the last ones, values beyond the summed axis are zeros
+#pragma unroll
+    for (int j = 0; j < S::W_LOADS; j++) {
+      const int row = j * S::RPL + lane / WC, piece = (lane % WC) ^ w_twist(row);
+      const int k = k0 + (NK ? piece * 8 : row), c = NK ? min(row, f.cols - 1) : min(piece * 8, f.cols - 8);
+      const bf16_t* src = NK ? f.w + (long)c * f.ldw + k : f.w + (long)k * f.ldw + c;
+      lds_load16_at(k < f.kdim ? (const char*)src : (const char*)g_zero_chunk, dst + j * 1024);
+    }
+#pragma unroll
+    for (int q = 0; q < S::X_LOADS; q++) {
+      const char* src = (const char*)(f.x + k0) + x_off[q];
+      lds_load16_at(k0 + x_piece(q) * 8 < f.kdim ? src : (const char*)g_zero_chunk, dst + (S::W_LOADS + q) * 1024);
+    }
+  };
+  floatx4 acc[RT][S::CT];
+#pragma unroll
+  for (int u = 0; u < RT; u++)
+#pragma unroll
+    for (int c = 0; c < S::CT; c++) acc[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < S::NS; i++)
+    if (i < mine) issue(i, i);
+  // ---- where the lane's fragments lie in a stage
+  const int r = l15 >> 2;
+  const int w_rd = NK ? l15 * 128 : (8 * gr + r) * S::PITCH + (lane & 1) * 8;
+  const int w_x = NK ? w_twist(l15) : w_twist(8 * gr + r);
+  int slot = 0;
+  for (int i = 0; i < mine; i++) {
+    if (i + S::NS <= mine) wait_vmcnt<(S::NS - 1) * S::LPS>(); else wait_vmcnt<0>();
+    const char* st = ring + slot * S::STAGE;
+    bf16x8 wf[S::KH][S::CT], xf[S::KH][RT];
+#pragma unroll
+    for (int h = 0; h < S::KH; h++) {
+#pragma unroll
+      for (int c = 0; c < S::CT; c++) {
+        if constexpr (NK) {
+          wf[h][c] = *(const bf16x8*)(st + w_rd + c * 2048 + (((4 * h + gr) ^ w_x) << 4));
+        } else {
+          typedef short short8_t __attribute__((ext_vector_type(8)));
+          const char* p = st + w_rd + (((2 * c + ((lane & 2) >> 1)) ^ w_x) << 4);
+          const short4_t lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * S::PITCH);
+          wf[h][c] = __builtin_bit_cast(bf16x8, (short8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < RT; u++) {
+        const int row = u * 16 + l15;
+        xf[h][u] = *(const bf16x8*)(st + S::W_LOADS * 1024 + row * (XC * 16) + (((4 * h + gr) ^ x_twist(row)) << 4));
+      }
+    }
+    if (i + S::NS < mine) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the fragments are in registers: their place may be filled again
+      issue(i + S::NS, slot);
+    }
+#pragma unroll
+    for (int h = 0; h < S::KH; h++)
+#pragma unroll
+      for (int c = 0; c < S::CT; c++)
+#pragma unroll
+        for (int u = 0; u < RT; u++) acc[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[h][c], xf[h][u], acc[u][c], 0, 0, 0);
+    slot = slot + 1 == S::NS ? 0 : slot + 1;
+  }
+  // ---- join and store.  Lane (l15, gr): row l15 of a row tile, columns 4 gr .. + 3 of a column tile
+  if constexpr (NW > 1) {
+    constexpr int PITCH = S::CW + 4;
+    static_assert(RT * 16 * PITCH * 4 <= kFewRing, "a wave's sums fit its ring");
+    __syncthreads();
+    float* own = (float*)ring;
+#pragma unroll
+    for (int u = 0; u < RT; u++)
+#pragma unroll
+      for (int c = 0; c < S::CT; c++) *(floatx4*)(own + (u * 16 + l15) * PITCH + c * 16 + gr * 4) = acc[u][c];
+    __syncthreads();
+    for (int i = tid; i < f.rows * (S::CW / 4); i += NW * 64) {
+      const int row = i / (S::CW / 4), col = (i - row * (S::CW / 4)) * 4;
+      if (col >= f.cols) continue;
+      floatx4 v = *(const floatx4*)((const float*)smem + row * PITCH + col);
+#pragma unroll
+      for (int w = 1; w < NW; w++) {
+        const floatx4 o = *(const floatx4*)((const float*)(smem + w * kFewRing) + row * PITCH + col);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] += o[e];
+      }
+      bf16x4 b;
+#pragma unroll
+      for (int e = 0; e < 4; e++) b[e] = (bf16_t)v[e];
+      *(bf16x4*)(f.out + (long)row * f.ldo + col) = b;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < RT; u++)
+#pragma unroll
+      for (int c = 0; c < S::CT; c++) {
+        const int row = u * 16 + l15, col = c * 16 + gr * 4;
+        bf16x4 b;
+#pragma unroll
+        for (int e = 0; e < 4; e++) b[e] = (bf16_t)acc[u][c][e];
+        if (row < f.rows && col < f.cols) *(bf16x4*)(f.out + (long)row * f.ldo + col) = b;
+      }
+  }
+}
+
+// NW waves share a unit, or NC = 2 take one each, side by side.
+template <bool GRAD_X, bool WIDE, int NW, int NC>
+__global__ void __launch_bounds__(NW * NC * 64) moe_few_rows_kernel(const ProductParams p) {
+  static_assert(NW == 1 || NC == 1, "waves share a unit or have one each");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int beside = NC == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  constexpr int CW = FewShape<GRAD_X, 1, WIDE>::CW;
+  const int ndim = GRAD_X ? p.K : p.N, kdim = GRAD_X ? p.N : p.K;
+  // ---- the row tiles of all experts, in every wave: lane i the experts 4i .. 4i + 3
+  int tiles = 0, t4[4], n4[4], lo4[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    lo4[i] = n4[i] = 0;
+    if (lane * 4 + i < p.E) rows_of(p, lane * 4 + i, &lo4[i], &n4[i]);
+    t4[i] = (n4[i] + kFewRows - 1) / kFewRows;
+    tiles += t4[i];
+  }
+  int scan = tiles;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(scan, d);
+    if (lane >= d) scan += o;
+  }
+  // ---- a die takes a run of units
+  const int units = __builtin_amdgcn_readlane(scan, 63) * p.nbn;
+  const int per = (units + kXcds * NC - 1) / (kXcds * NC) * NC, i = blockIdx.x / kXcds * NC + beside, unit = (blockIdx.x % kXcds) * per + i;
+  if (i >= per || unit >= units) return;                // (there are fewer than the grid has room for)
+  const int bm = unit / p.nbn, bn = unit - bm * p.nbn;
+  int at = scan - tiles, e4 = 0, first = 0, n = 0, lo = 0;     // in the lane that has it: which of its four
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if (at <= bm && bm < at + t4[i]) { e4 = i; first = at; n = n4[i]; lo = lo4[i]; }
+    at += t4[i];
+  }
+  const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(scan > bm));
+  const int e = owner * 4 + __builtin_amdgcn_readlane(e4, owner);
+  first = __builtin_amdgcn_readlane(first, owner);
+  n = __builtin_amdgcn_readlane(n, owner);
+  lo = __builtin_amdgcn_readlane(lo, owner);
+  const int r0 = (bm - first) * kFewRows, col = bn * CW;
+  FewUnit f;
+  f.rows = min(n - r0, kFewRows);
+  f.cols = min(CW, ndim - col);
+  f.kdim = kdim;
+  f.once = n <= kFewRows;
+  const bf16_t* w = p.w + (long)e * p.K * p.N;
+  f.w = GRAD_X ? w + (long)col * p.N : w + col;
+  f.ldw = p.N;
+  f.x = (GRAD_X ? p.dy : p.x) + (long)(lo + r0) * kdim;
+  f.ldx = kdim;
+  f.out = p.out + (long)(lo + r0) * ndim + col;
+  f.ldo = ndim;
+  if (f.rows <= 16) few_unit<GRAD_X, 1, WIDE, NW>(f, smem + beside * kFewRing);
+  else if (f.rows <= 32) few_unit<GRAD_X, 2, WIDE, NW>(f, smem + beside * kFewRing);
+  else few_unit<GRAD_X, 4, WIDE, NW>(f, smem + beside * kFewRing);
+}
+
+// ======================================================================================
+// dW.  An expert's tiles sum over its rows, many or few, so the work is laid out by length, by a launch of its own (one workgroup): an even
+// share of all rows x tiles for every compute unit is the longest an item should be, a longer sum is cut into parts, and the items stand
+// in the order of their length, the longest first, for the hardware to hand out.  The parts of a cut sum go to the workspace in fp32,
+// and a third launch adds them up in their order.
+// A workgroup takes one item: it may end while its stores are on their way.  (A persistent one that requests the next item's first stages
+// before it stores this one's result has to wait, a few steps later, for those stores to be complete, as loads and stores are counted
+// together: 32 gradients of 4096 x 1792 over 512 rows each 284 us against 262.)
+// ======================================================================================
+constexpr int kMaxParts = 8;
+constexpr int kMinPart = 256;             // rows
+struct GradWItem {                        // (a 16-byte load)
+  int row, rows;                          // of x and dy
+  unsigned what;                          // expert, parts << 8, place << 12 (of the part's sums)
+  int tile;
+};
+struct CutTile {
+  int e, tile, parts, place;              // the first part's place
+};
+struct GradWPlan {                        // at the front of the workspace; items and cut tiles behind it
+  int n_items, n_cut;
+};
+constexpr int kPlanHeader = 128;
+constexpr int kPlanThreads = 1024;
+
+struct GradWParams {
+  ProductParams p;
+  GradWPlan* plan;
+  GradWItem* items;
+  CutTile* cut;
+  float* partial;          // [places][BM * BN]
+  int places, share_of;    // places of partial sums; compute units that share the work
+  int run;
+};
+
+__global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const GradWParams g) {
+  __shared__ int s_lo[kMaxProductExperts], s_n[kMaxProductExperts], s_expert[kMaxProductExperts], s_first[kMaxProductExperts], s_place[kMaxProductExperts];
+  __shared__ int s_chunk, s_items;
+  const ProductParams& p = g.p;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int per = p.nbm * p.nbn;
+  if (tid < kMaxProductExperts) {
+    int lo = 0, n = -1;
+    if (tid < p.E) rows_of(p, tid, &lo, &n);
+    s_lo[tid] = lo;
+    s_n[tid] = n;
+  }
+  __syncthreads();
+  if (tid < p.E) {     // the experts by their rows, most first
+    const int n = s_n[tid];
+    int rank = 0;
+    for (int o = 0; o < p.E; o++) rank += s_n[o] > n || (s_n[o] == n && o < tid);
+    s_expert[rank] = tid;
+  }
+  if (tid < 64) {      // the longest part there is to be
+    long all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) all += max(s_n[lane * 4 + i], 0);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+    const long share = (all * per + g.share_of - 1) / g.share_of;
+    if (lane == 0) s_chunk = g.places ? (int)max(min(share, 0x7fffffffL), (long)kMinPart) : 0x7fffffff;
+  }
+  __syncthreads();
+  const unsigned chunk = (unsigned)s_chunk;
+  auto parts_of = [&](int n) { return max(min((int)(((unsigned)max(n, 0) + (chunk - 1)) / chunk), kMaxParts), 1); };     // (both below 2^31)
+  if (tid < 64) {
+    int items[4], places[4], at[4], pl[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int r = lane * 4 + i, parts = r < p.E ? parts_of(s_n[s_expert[r]]) : 0;
+      items[i] = parts * per;
+      places[i] = parts > 1 ? items[i] : 0;
+    }
+    const int n_items = scan_starts(items, at), n_places = scan_starts(places, pl);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      s_first[lane * 4 + i] = at[i];
+      s_place[lane * 4 + i] = pl[i];
+    }
+    int cut = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) cut += places[i] ? per : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) cut += __shfl_xor(cut, d);
+    if (lane == 0) {
+      s_items = n_items;
+      g.plan->n_items = n_items;
+      g.plan->n_cut = cut;
+    }
+    (void)n_places;      // (at most g.places: see grad_w_shape)
+  }
+  __syncthreads();
+  const int n_items = s_items;
+  for (int l = tid; l < n_items; l += kPlanThreads) {
+    int r = 0;    // the last of the sorted experts whose items start at or before l
 #pragma unroll
     for (int d = kMaxProductExperts / 2; d >= 1; d /= 2)
-      if (s_first[e + d] <= bm) e += d;
-    e = __builtin_amdgcn_readfirstlane(e);
-    const int r0 = (bm - s_first[e]) * Cfg::BM, rows = __builtin_amdgcn_readfirstlane(min(s_n[e] - r0, Cfg::BM));
-    const long at = __builtin_amdgcn_readfirstlane(s_lo[e] + r0);
-    const int col = bn * Cfg::BN, cols = min(Cfg::BN, ndim - col);
-    const bf16_t* w = p.w + (long)e * p.K * p.N;
-    if constexpr (GRAD_X)
-      gemm_tile<Cfg>(p.dy + at * p.N, p.N, nullptr, 1, w + (long)col * p.N, p.N, DenseRows{p.out + at * p.K + col, p.K}, rows, cols, kdim, smem);
-    else
-      gemm_tile<Cfg>(p.x + at * p.K, p.K, nullptr, 1, w + col, p.N, DenseRows{p.out + at * p.N + col, p.N}, rows, cols, kdim, smem);
+      if (r + d < p.E && s_first[r + d] <= l) r += d;
+    const int e = s_expert[r], n = s_n[e], parts = parts_of(n);
+    const int item = l - s_first[r], part = item / per, tile = item - part * per;
+    const int k0 = n / parts * part + min(part, n % parts), k1 = n / parts * (part + 1) + min(part + 1, n % parts);
+    const int place0 = s_place[r] + tile * parts;
+    g.items[l] = GradWItem{s_lo[e] + k0, k1 - k0, (unsigned)e | (unsigned)parts << 8 | (unsigned)(parts > 1 ? place0 + part : 0) << 12, tile};
+    // (experts with cut sums come first: their tiles are numbers r * per + tile)
+    if (parts > 1 && part == 0) g.cut[r * per + tile] = CutTile{e, tile, parts, place0};
   }
 }
 
 template <class Cfg, class Out>
-__global__ void __launch_bounds__(Cfg::NTHREADS) moe_grad_w_kernel(const ProductParams p) {
+__global__ void __launch_bounds__(Cfg::NTHREADS) moe_grad_w_kernel(const GradWParams g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int per = p.nbm * p.nbn;
-  const int e = blockIdx.x / per, tile = blockIdx.x - e * per;
+  const ProductParams& p = g.p;
+  // runs of g.run items go to one die, which then reads its part of the rows once
+  const int i = blockIdx.x / kXcds, l = ((i / g.run) * kXcds + blockIdx.x % kXcds) * g.run + i % g.run;
+  const u32x4 rec = *(const u32x4*)(g.items + l);       // (whatever it is where there is no such item: there is room for the whole grid)
+  if (l >= g.plan->n_items) return;
+  const int row0 = __builtin_amdgcn_readfirstlane(rec[0]), n = __builtin_amdgcn_readfirstlane(rec[1]), tile = __builtin_amdgcn_readfirstlane(rec[3]);
+  const unsigned what = __builtin_amdgcn_readfirstlane(rec[2]);
+  const int e = what & 255, parts = (what >> 8) & 15, place = what >> 12;
   const int bm = tile / p.nbn, bn = tile - bm * p.nbn;
-  int lo, n;
-  rows_of(p, e, &lo, &n);
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  n = __builtin_amdgcn_readfirstlane(n);
   const int row = bm * Cfg::BM, rows = min(Cfg::BM, p.K - row), col = bn * Cfg::BN, cols = min(Cfg::BN, p.N - col);
   const long at = ((long)e * p.K + row) * p.N + col;
   Out out;
   if constexpr (StoresF32<Out>::value) out = Out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
   else out = Out{p.out + at, p.N};
   if (n == 0) {     // an expert without rows
-    for (int i = threadIdx.x; i < rows * (cols / 8); i += Cfg::NTHREADS) {
-      const int r = i / (cols / 8), c = (i - r * (cols / 8)) * 8;
+    for (int c = threadIdx.x; c < rows * (cols / 8); c += Cfg::NTHREADS) {
+      const int y = c / (cols / 8), x = (c - y * (cols / 8)) * 8;
       if constexpr (StoresF32<Out>::value) {
-        out.store4(r, c, floatx4{0.f, 0.f, 0.f, 0.f});
-        out.store4(r, c + 4, floatx4{0.f, 0.f, 0.f, 0.f});
+        out.store4(y, x, out.load4(y, x));
+        out.store4(y, x + 4, out.load4(y, x + 4));
       } else {
-        out.store(r, c, u32x4{0, 0, 0, 0});
+        out.store(y, x, u32x4{0, 0, 0, 0});
       }
     }
     return;
   }
-  gemm_tile<Cfg, Out>(p.x + (long)lo * p.K + row, p.K, nullptr, 1, p.dy + (long)lo * p.N + col, p.N, out, rows, cols, n, smem);
+  const bf16_t *a = p.x + (long)row0 * p.K + row, *b = p.dy + (long)row0 * p.N + col;
+  if (parts == 1) gemm_tile<Cfg, Out>(a, p.K, nullptr, 1, b, p.N, out, rows, cols, n, smem);
+  else gemm_tile<Cfg, PartRows>(a, p.K, nullptr, 1, b, p.N, PartRows{g.partial + (long)place * (Cfg::BM * Cfg::BN), Cfg::BN}, rows, cols, n, smem);
+}
+
+// The cut sums: eight neighbouring columns to a thread.
+template <int TILE, class Out>
+__global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams g) {
+  const ProductParams& p = g.p;
+  constexpr int kSlices = TILE * TILE / 8 / 256;
+  const int n = g.plan->n_cut * kSlices;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const CutTile t = g.cut[i / kSlices];
+    const int chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (TILE / 8), x = chunk % (TILE / 8) * 8;
+    const int bm = t.tile / p.nbn, bn = t.tile - bm * p.nbn;
+    if (bm * TILE + y >= p.K || bn * TILE + x >= p.N) continue;
+    const float* src = g.partial + (long)t.place * (TILE * TILE) + y * TILE + x;
+    floatx4 v[kMaxParts][2];
+#pragma unroll
+    for (int q = 0; q < kMaxParts; q++) {
+      v[q][0] = v[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (q < t.parts) {
+        v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE)));
+        v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE) + 4));
+      }
+    }
+    float o[8];
+#pragma unroll
+    for (int c = 0; c < 8; c++) o[c] = v[0][c / 4][c % 4];
+#pragma unroll
+    for (int q = 1; q < kMaxParts; q++)
+#pragma unroll
+      for (int c = 0; c < 8; c++) o[c] += v[q][c / 4][c % 4];
+    const long at = ((long)t.e * p.K + bm * TILE) * p.N + bn * TILE;
+    if constexpr (StoresF32<Out>::value) {
+      const Out out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        floatx4 w = out.load4(y, x + 4 * h);
+#pragma unroll
+        for (int c = 0; c < 4; c++) w[c] += o[4 * h + c];
+        out.store4(y, x + 4 * h, w);
+      }
+    } else {
+      Out{p.out + at, p.N}.store(y, x, pack_bf16x8(o));
+    }
+  }
 }
 
 // ======================================================================================
 // Host side
 // ======================================================================================
-typedef TileCfg<256, 256, 2, 4, 32, 4, false, true> CfgX256;      // dX: W along its rows
-typedef TileCfg<128, 128, 2, 2, 64, 4, false, true> CfgX128;
-typedef TileCfg<256, 256, 2, 4, 32, 4, true, false> CfgW256;      // dW: both operands in the rows that are summed over
+template <bool NK> using ProductBig = TileCfg<256, 256, 2, 4, 32, 4, false, NK>;
+template <bool NK> using ProductBigHalf = TileCfg<128, 256, 2, 4, 32, 4, false, NK>;
+template <bool NK> using ProductSmall = TileCfg<128, 128, 2, 2, 64, 4, false, NK>;
+template <bool NK> using ProductSmallHalf = TileCfg<64, 128, 2, 2, 64, 4, false, NK>;
+typedef TileCfg<256, 256, 2, 4, 32, 4, true, false> CfgW256;
 typedef TileCfg<128, 128, 2, 2, 64, 4, true, false> CfgW128;
 
 static int check_product(const char* what, int max_rows, int K, int N, int E) {
@@ -147,6 +593,34 @@ static int check_product(const char* what, int max_rows, int K, int N, int E) {
   if (K % 8 || N % 8) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: K=%d and N=%d must be multiples of 8", what, K, N);
   if (K > (1 << 20) || N > (1 << 20)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: K and N must not exceed 2^20", what);
   return TL_OK;
+}
+
+struct GradWShape {
+  int tile, nbm, nbn, places, run;
+  long grid;                                   // items at most, in whole runs for every die
+  size_t items_at, cut_at, partial_at, ws_bytes;
+};
+static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, int E) {
+  GradWShape s;
+  const int cus = min(ctx->num_cus, 1 << 16);
+  // The large tile, unless even its cut sums would leave compute units without work.
+  const long tiles = (long)E * ceil_div(K, 256) * ceil_div(N, 256), parts = max(min(max_rows / E / kMinPart, kMaxParts), 1);
+  s.tile = tiles * parts < cus ? 128 : 256;
+  s.nbm = ceil_div(K, s.tile);
+  s.nbn = ceil_div(N, s.tile);
+  const long per = (long)s.nbm * s.nbn;
+  // A share is all rows x tiles over the compute units, and no sum is longer than all rows: none is cut where every expert has a tile for every
+  // unit.  A cut one of n rows has fewer than 2 n / share parts in each of its tiles, all together fewer than two for every unit.
+  s.places = per < cus && max_rows > kMinPart ? 2 * cus : 0;
+  s.run = (int)min((per + kXcds - 1) / kXcds, 32L);
+  const long span = (long)s.run * kXcds;
+  s.grid = (E * per + s.places + span - 1) / span * span;
+  auto up = [](size_t b) { return (b + 127) / 128 * 128; };
+  s.items_at = kPlanHeader;
+  s.cut_at = up(s.items_at + s.grid * sizeof(GradWItem));
+  s.partial_at = up(s.cut_at + s.places / 2 * sizeof(CutTile));
+  s.ws_bytes = up(s.partial_at + (size_t)s.places * s.tile * s.tile * sizeof(float));
+  return s;
 }
 
 static int check_product_call(tl_ctx* ctx, const char* what, int way, const void* a, const void* b, const void* out, const int* offsets, int max_rows, int K, int N,
@@ -162,23 +636,62 @@ static int check_product_call(tl_ctx* ctx, const char* what, int way, const void
   return check_op_ctx(ctx);
 }
 
-// The small tile where the large ones would leave compute units without work.
-static bool small_tiles(const tl_ctx* ctx, long tiles256) { return tiles256 < ctx->num_cus; }
+template <bool GRAD_X, bool WIDE, int NW, int NC>
+static int launch_few(ProductParams& p, int ndim, hipStream_t s) {
+  p.nbn = ceil_div(ndim, FewShape<GRAD_X, 1, WIDE>::CW);
+  const long row_tiles = (p.max_rows < p.E ? p.max_rows : p.E) + p.max_rows / kFewRows;       // at most
+  const long grid = (row_tiles * p.nbn + kXcds * NC - 1) / (kXcds * NC) * kXcds;
+  constexpr int kWaves = NW * NC;
+  TL_HIP(hipFuncSetAttribute((const void*)moe_few_rows_kernel<GRAD_X, WIDE, NW, NC>, hipFuncAttributeMaxDynamicSharedMemorySize, kWaves * kFewRing));
+  hipLaunchKernelGGL((moe_few_rows_kernel<GRAD_X, WIDE, NW, NC>), dim3((unsigned)grid), dim3(kWaves * 64), kWaves * kFewRing, s, p);
+  TL_HIP(hipGetLastError());
+  return TL_OK;
+}
 
+// Rounds of tiles of `tile` rows and columns.  The host knows all rows, not the experts': whole tiles, and one that is partly filled for more
+// than every other expert.
+static long product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, int tile) {
+  const double tiles = (ceil_div(p.max_rows, tile) + 0.6 * (p.E - 1)) * ceil_div(ndim, tile);
+  return (long)(tiles / ctx->num_cus) + 1;
+}
+
+// Up to 48 rows an expert in the mean the few-row kernel: 32 experts of 2048 x 1536 with 32 rows each 43.7 us against 49 (small tiles) and 53 (large),
+// with 64 rows 73 against 53 and 58; 8 of 4096 x 2048 with 40 rows 34 against 45, with 80 rows 61 against 44.
+// Beyond, the tile whose rounds take less: a 256 x 256 tile takes 1.96 us for 64 values of the sum, a 128 x 128 tile 0.70, all compute units at
+// work (2048 x 1536, 32 experts, 4096 rows: forward 65 us large, 71 small; dX 84 large, 65 small).
 template <bool GRAD_X>
 static int launch_product(tl_ctx* ctx, ProductParams& p, hipStream_t s) {
   const int ndim = GRAD_X ? p.K : p.N;
-  const long tiles = (long)(ceil_div(p.max_rows, 256) + p.E / 2) * ceil_div(ndim, 256);
-  p.swizzle = 1;
+  if (p.max_rows <= 48L * p.E) {
+    // Blocks of twice the columns, one for every wave, where they make a wave for every compute unit (31 experts of 2048 x 1536: 41 us against 44.7);
+    // else the narrow ones, with two or four waves for the summed axis (7 of 4096 x 2048: 26 us against 39 with one; a single one
+    // of 4096 x 4096: 19 us against 21 with two).
+    const long used = min(p.max_rows, p.E);
+    if (used * ceil_div(ndim, FewShape<GRAD_X, 1, true>::CW) >= ctx->num_cus) return launch_few<GRAD_X, true, 1, 2>(p, ndim, s);
+    if (used * ceil_div(ndim, FewShape<GRAD_X, 1, false>::CW) * 2 >= ctx->num_cus) return launch_few<GRAD_X, false, 2, 1>(p, ndim, s);
+    return launch_few<GRAD_X, false, 4, 1>(p, ndim, s);
+  }
   p.group_m = 4;
-  if (small_tiles(ctx, tiles)) {
+  if (0.70 * product_rounds(ctx, p, ndim, 128) < 1.96 * product_rounds(ctx, p, ndim, 256)) {
     p.nbn = ceil_div(ndim, 128);
-    typedef typename std::conditional<GRAD_X, CfgX128, Cfg128x128>::type Cfg;
-    return launch_fused<Cfg>(moe_product_kernel<Cfg, GRAD_X>, p, ctx->num_cus, s);
+    typedef ProductSmall<GRAD_X> Cfg;
+    return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X>, p, ctx->num_cus, s);
   }
   p.nbn = ceil_div(ndim, 256);
-  typedef typename std::conditional<GRAD_X, CfgX256, Cfg256x256>::type Cfg;
-  return launch_fused<Cfg>(moe_product_kernel<Cfg, GRAD_X>, p, ctx->num_cus, s);
+  typedef ProductBig<GRAD_X> Cfg;
+  return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductBigHalf<GRAD_X>, GRAD_X>, p, ctx->num_cus, s);
+}
+
+template <class Cfg, class Out>
+static int launch_grad_w(const GradWParams& g, long grid, hipStream_t s) {
+  hipLaunchKernelGGL(moe_grad_w_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, g);
+  TL_HIP(hipGetLastError());
+  if (int e = launch_fused<Cfg>(moe_grad_w_kernel<Cfg, Out>, g, (int)grid, s)) return e;
+  if (g.places) {
+    hipLaunchKernelGGL((moe_grad_w_join_kernel<Cfg::BM, Out>), dim3(2048), dim3(256), 0, s, g);
+    TL_HIP(hipGetLastError());
+  }
+  return TL_OK;
 }
 
 }  // namespace tl
@@ -192,7 +705,8 @@ int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, in
   if (!ws_bytes) return fail(TL_ERR_INVALID_ARG, "tl_moe_gemm_query: ws_bytes must not be null");
   if (way != TL_MOE_FORWARD && way != TL_MOE_GRAD_X && way != TL_MOE_GRAD_W) return fail(TL_ERR_INVALID_ARG, "tl_moe_gemm_query: %d is not one of the three products", way);
   if (int e = check_product("tl_moe_gemm_query", max_rows, K, N, E)) return e;
-  *ws_bytes = 256;
+  if (way == TL_MOE_GRAD_W && (long)E * ceil_div(K, 128) * ceil_div(N, 128) >= (1L << 22)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_moe_gemm_query: E*K*N has 2^22 tiles or more");
+  *ws_bytes = way == TL_MOE_GRAD_W ? grad_w_shape(ctx, max_rows, K, N, E).ws_bytes : 256;
   return TL_OK;
 }
 
@@ -222,20 +736,25 @@ int tl_moe_gemm_grad_w(tl_ctx* ctx, const void* x, const void* dy, const int* ex
   if (dw_add && !dw_f32) return fail(TL_ERR_INVALID_ARG, "tl_moe_gemm_grad_w: dw_add needs dw in fp32");
   if (!aligned16(dw_add)) return fail(TL_ERR_INVALID_ARG, "tl_moe_gemm_grad_w: dw_add must be 16-byte aligned");
   if (int e = check_product_call(ctx, "tl_moe_gemm_grad_w", TL_MOE_GRAD_W, x, dy, dw, expert_offsets, max_rows, K, N, E, workspace, ws_bytes)) return e;
-  ProductParams p;
-  memset(&p, 0, sizeof p);
+  const GradWShape shape = grad_w_shape(ctx, max_rows, K, N, E);
+  GradWParams g;
+  memset(&g, 0, sizeof g);
+  ProductParams& p = g.p;
   p.x = (const bf16_t*)x; p.dy = (const bf16_t*)dy; p.offsets = expert_offsets;
   p.out = (bf16_t*)dw; p.out32 = (float*)dw; p.add = dw_add;
   p.max_rows = max_rows; p.K = K; p.N = N; p.E = E;
-  const bool small = small_tiles(ctx, (long)E * ceil_div(K, 256) * ceil_div(N, 256));
-  const int tile = small ? 128 : 256;
-  p.nbm = ceil_div(K, tile);
-  p.nbn = ceil_div(N, tile);
-  const long grid = (long)E * p.nbm * p.nbn;
-  if (grid >= (1L << 22)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_moe_gemm_grad_w: E*K*N is too large for one launch");
+  p.nbm = shape.nbm; p.nbn = shape.nbn;
+  char* ws = (char*)workspace;
+  g.plan = (GradWPlan*)ws;
+  g.items = (GradWItem*)(ws + shape.items_at);
+  g.cut = (CutTile*)(ws + shape.cut_at);
+  g.partial = (float*)(ws + shape.partial_at);
+  g.places = shape.places;
+  g.share_of = ctx->num_cus;
+  g.run = shape.run;
   hipStream_t s = (hipStream_t)stream;
-  if (dw_f32) return small ? launch_fused<CfgW128>(moe_grad_w_kernel<CfgW128, AddRows32>, p, (int)grid, s) : launch_fused<CfgW256>(moe_grad_w_kernel<CfgW256, AddRows32>, p, (int)grid, s);
-  return small ? launch_fused<CfgW128>(moe_grad_w_kernel<CfgW128, DenseRows>, p, (int)grid, s) : launch_fused<CfgW256>(moe_grad_w_kernel<CfgW256, DenseRows>, p, (int)grid, s);
+  if (shape.tile == 128) return dw_f32 ? launch_grad_w<CfgW128, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW128, GradRows16>(g, shape.grid, s);
+  return dw_f32 ? launch_grad_w<CfgW256, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW256, GradRows16>(g, shape.grid, s);
 }
 
 }  // extern "C"

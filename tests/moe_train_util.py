@@ -78,4 +78,4 @@ def sort_call(ctx, ids, first, E, stream=None, ws=None):
 
 def product_ws(ctx, way, rows, K, N, E):
     n = tl.tl_moe_gemm_query(ctx, way, rows, K, N, E)
-    return torch.zeros(n // 4, dtype=I32, device="cuda"), n
+    return torch.full((n // 4,), -1, dtype=I32, device="cuda"), n        # needs no preparation

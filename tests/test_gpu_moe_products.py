@@ -59,7 +59,8 @@ def to_bf16(a):
 # the ring of steps holds, tiles' edges and one beside them, more experts than compute units' worth of work
 COUNTS = [([1], 8, 8, 0, 0), ([0], 16, 24, 0, 3), ([1, 0, 2], 72, 40, 0, 1), ([5, 0, 0, 64, 1], 136, 264, 2, 2), ([65, 63, 7], 256, 520, 0, 0),
           ([129, 127, 128], 512, 128, 0, 0), ([300, 0, 257], 264, 1032, 0, 5), ([256] * 3, 1000, 256, 1, 0), ([1] * 70, 64, 72, 0, 0), ([3, 1] * 128, 32, 16, 0, 0),
-          ([700, 11], 40, 2056, 0, 0), ([1100], 776, 8, 0, 0), ([0, 0, 33], 2056, 96, 0, 0)]
+          ([700, 11], 40, 2056, 0, 0), ([1100], 776, 8, 0, 0), ([0, 0, 33], 2056, 96, 0, 0), ([2500, 3, 900, 0, 1], 264, 520, 0, 7),
+          ([257, 2049, 255], 1288, 2072, 0, 0)]
 
 
 def ints(seed):
@@ -144,7 +145,7 @@ def test_one_workspace_for_all():
     with Lib() as ctx:
         calls = [Call(ints(i), counts, K, N) for i, (counts, K, N) in enumerate([([2000], 256, 136), ([1, 1, 3], 4096, 64), ([300] * 4, 128, 512)])]
         n = max(tl.tl_moe_gemm_query(ctx, way, *c.sizes()[1:]) for c in calls for way in (FORWARD, GRAD_X, GRAD_W))
-        ws = (torch.zeros(n // 4, dtype=I32, device="cuda"), n)
+        ws = (torch.full((n // 4,), -1, dtype=I32, device="cuda"), n)
         for _ in range(2):
             for c in calls:
                 y, dw, dx = c.forward(ctx, ws), c.grad_w(ctx, c.new_dw(), ws=ws), c.grad_x(ctx, ws)

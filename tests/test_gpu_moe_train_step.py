@@ -33,7 +33,7 @@ class Layer:
         self.sort_bytes = tl.tl_moe_sort_query(ctx, self.T, self.k, self.E)
         n = max(tl.tl_moe_gemm_query(ctx, way, self.rows, a, b, self.E) for way in range(3) for a, b in ((self.H, self.F), (self.F, self.H)))
         self.sort_ws = torch.zeros(self.sort_bytes // 4, dtype=I32, device="cuda")
-        self.ws = torch.zeros(n // 4, dtype=I32, device="cuda"), n
+        self.ws = torch.full((n // 4,), -1, dtype=I32, device="cuda"), n
         torch.cuda.synchronize()
 
     def step(self, ctx, s):

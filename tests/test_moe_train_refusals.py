@@ -84,7 +84,7 @@ def test_sizes_are_positive(ctx, name, arg):
   + [(n, SHAPE, "31 bits", dict(T=1 << 30)) for n in ("dispatch", "dispatch_grad", "combine", "combine_grad")]
   + [(n, SHAPE, "multiples of 8", d) for n in WAYS for d in (dict(K=60), dict(N=90))]
   + [(n, SHAPE, "256", dict(E=257)) for n in WAYS] + [(n, SHAPE, "2^20", d) for n in WAYS for d in (dict(K=(1 << 20) + 8), dict(N=(1 << 20) + 8))]
-  + [(n, ARG, "128-byte", dict(workspace=P + 64)) for n in WAYS], ids=str)
+  + [("grad_w", SHAPE, "2^22", dict(K=1 << 20, N=1 << 16))] + [(n, ARG, "128-byte", dict(workspace=P + 64)) for n in WAYS], ids=str)
 def test_values(ctx, name, status, text, change):
     refused(status, text, CALLS[name](**change), ctx)
 
