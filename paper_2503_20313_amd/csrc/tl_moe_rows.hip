@@ -71,8 +71,8 @@ __global__ void __launch_bounds__(kSortThreads) moe_count_kernel(const SortParam
 template <int RPT, bool ONE>       // ONE: this is the only chunk
 __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParams p) {
   __shared__ int s_cnt[kSortWaves][kMaxSortExperts];
-  __shared__ int s_sum[2][kSortWaves / 4][kMaxSortExperts];     // rows of an expert in the chunks before this one, and in all
-  __shared__ int s_base[kMaxSortExperts];
+  __shared__ int s_sum[2][kSortThreads];     // rows of an expert in the chunks before this one, and in all: by groups of chunks
+  __shared__ int s_base[kMaxSortExperts], s_scan[kMaxSortExperts];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bits = 32 - __builtin_clz(max(p.E - 1, 1));
   const unsigned long long below = (1ull << lane) - 1;
@@ -81,18 +81,24 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParam
   int e[RPT];
 #pragma unroll
   for (int u = 0; u < RPT; u++) e[u] = own_expert(p, lo + u * 64 + lane);
+  const int room = 1 << bits;                // experts, up to a power of two
   if constexpr (!ONE) {
-    // thread (g, x): chunks g, g + 4, .. of expert x
-    const int x = tid & (kMaxSortExperts - 1), g = tid / kMaxSortExperts;
+    // thread (g, x): chunks g, g + groups, .. of expert x, eight at a time in flight
+    const int x = tid & (room - 1), g = tid >> bits, groups = kSortThreads >> bits;
     int before = 0, all = 0;
     if (x < p.E)
-      for (int c = g; c < p.chunks; c += kSortWaves / 4) {
-        const int v = p.hist[(long)c * p.E + x];
-        all += v;
-        if (c < (int)blockIdx.x) before += v;
+      for (int c0 = g; c0 < p.chunks; c0 += 8 * groups) {
+        int v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = c0 + i * groups < p.chunks ? p.hist[(long)(c0 + i * groups) * p.E + x] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          all += v[i];
+          if (c0 + i * groups < (int)blockIdx.x) before += v[i];
+        }
       }
-    s_sum[0][g][x] = before;
-    s_sum[1][g][x] = all;
+    s_sum[0][tid] = before;
+    s_sum[1][tid] = all;
   }
   __syncthreads();
   // ---- rank of every row among the wave's rows of its expert
@@ -121,8 +127,8 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParam
     int before = 0, all = run;
     if constexpr (!ONE) {
       all = 0;
-#pragma unroll
-      for (int g = 0; g < kSortWaves / 4; g++) { before += s_sum[0][g][tid]; all += s_sum[1][g][tid]; }
+      if (tid < room)
+        for (int g = tid; g < kSortThreads; g += room) { before += s_sum[0][g]; all += s_sum[1][g]; }
     }
     int scan = all;      // inclusive, over the wave's 64 experts
 #pragma unroll
@@ -130,16 +136,16 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParam
       const int o = __shfl_up(scan, d);
       if (lane >= d) scan += o;
     }
-    s_sum[1][0][tid] = scan;
+    s_scan[tid] = scan;
     s_base[tid] = scan - all + before;
   }
   __syncthreads();
   if (tid < kMaxSortExperts) {
     int start = 0;       // all rows of the experts of the waves before
-    for (int w = 0; w < wave; w++) start += s_sum[1][0][w * 64 + 63];
+    for (int w = 0; w < wave; w++) start += s_scan[w * 64 + 63];
     s_base[tid] += start;
     if (blockIdx.x == 0 && tid < p.E) {
-      p.offsets[tid + 1] = start + s_sum[1][0][tid];
+      p.offsets[tid + 1] = start + s_scan[tid];
       if (tid == 0) p.offsets[0] = 0;
     }
   }
@@ -158,8 +164,21 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParam
 }
 
 // ======================================================================================
-// Rows of tokens <-> rows sorted by expert.  Bound by memory: every row is read or written once.
+// Rows of tokens <-> rows sorted by expert.  Bound by memory: every row is read or written once, a wave to 1 KiB of a row (of 2 or 4 KiB: the
+// same within 3 %).  Matrices larger than the caches are read and written as streaming: 8192 tokens of 4096, top-5, dispatched in 78.7 us without, 63.5 with
+// (6.3 TB/s), combined 91.8 and 73.7, their gradients 148 and 134 us (5.5 TB/s, reads and writes in equal parts).  Smaller ones
+// are not: their rows may still be there from the product before, or be there for the one behind (1024 tokens, top-8, gradients of
+// combine: 24.4 us, with streaming loads 30.9).
 // ======================================================================================
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_piece(const u32x4* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p); else return *p;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_piece(u32x4* p, u32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p); else *p = v;
+}
+
 struct RowsParams {
   const bf16_t *x, *ys, *add;      // token rows; sorted rows; token rows or null
   const float* w;
@@ -177,85 +196,77 @@ __device__ __forceinline__ unsigned long long places_of(const RowsParams& p, lon
   return __builtin_amdgcn_ballot_w64((unsigned)*pos < (unsigned)p.max_rows);
 }
 
-template <int U>
+template <bool STREAM>
 __global__ void __launch_bounds__(256) moe_dispatch_kernel(const RowsParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long items = p.T * p.segs;
   for (long it = (long)blockIdx.x * 4 + wave; it < items; it += (long)gridDim.x * 4) {
     const long t = it / p.segs;
-    const int c0 = (int)(it - t * p.segs) * (64 * U) + lane;
+    const int c = (int)(it - t * p.segs) * 64 + lane;
     int pos;
     unsigned long long part = places_of(p, t, lane, &pos);
-    if (!part) continue;
-    const u32x4* src = (const u32x4*)p.x + t * p.H8;
-    u32x4 v[U];
-#pragma unroll
-    for (int u = 0; u < U; u++)
-      if (c0 + u * 64 < p.H8) v[u] = src[c0 + u * 64];
+    if (!part || c >= p.H8) continue;
+    const u32x4 v = ((const u32x4*)p.x)[t * p.H8 + c];
     while (part) {
       const int j = __builtin_ctzll(part);
       part &= part - 1;
-      u32x4* dst = (u32x4*)p.out + (long)__builtin_amdgcn_readlane(pos, j) * p.H8;
-#pragma unroll
-      for (int u = 0; u < U; u++)
-        if (c0 + u * 64 < p.H8) dst[c0 + u * 64] = v[u];
+      store_piece<STREAM>((u32x4*)p.out + (long)__builtin_amdgcn_readlane(pos, j) * p.H8 + c, v);
     }
   }
 }
 
 // out[t] = (add[t] +) sum over j, in their order, of (w[t, j]) ys[row_pos[t, j]]; one rounding.
-template <int U, bool WEIGHTED>
+template <bool WEIGHTED, bool STREAM>
 __global__ void __launch_bounds__(256) moe_gather_sum_kernel(const RowsParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long items = p.T * p.segs;
   for (long it = (long)blockIdx.x * 4 + wave; it < items; it += (long)gridDim.x * 4) {
     const long t = it / p.segs;
-    const int c0 = (int)(it - t * p.segs) * (64 * U) + lane;
+    const int c = (int)(it - t * p.segs) * 64 + lane;
     int pos;
     unsigned long long part = places_of(p, t, lane, &pos);
     float w = 0.f;
     if (WEIGHTED && lane < p.topk) w = p.w[t * p.topk + lane];
-    float acc[U][8];
+    float acc[8];
 #pragma unroll
-    for (int u = 0; u < U; u++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) acc[u][e] = 0.f;
-    if (WEIGHTED && p.add) {
-      const u32x4* src = (const u32x4*)p.add + t * p.H8;
-#pragma unroll
-      for (int u = 0; u < U; u++)
-        if (c0 + u * 64 < p.H8) acc_bf16x8(acc[u], src[c0 + u * 64]);
-    }
+    for (int e = 0; e < 8; e++) acc[e] = 0.f;
+    const bool in = c < p.H8;
+    if (WEIGHTED && p.add && in) acc_bf16x8(acc, ((const u32x4*)p.add)[t * p.H8 + c]);
+    // four rows at a time, their loads in flight together
     while (part) {
-      const int j = __builtin_ctzll(part);
-      part &= part - 1;
-      const u32x4* src = (const u32x4*)p.ys + (long)__builtin_amdgcn_readlane(pos, j) * p.H8;
-      const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
+      u32x4 v[4];
+      float wj[4];
 #pragma unroll
-      for (int u = 0; u < U; u++) {
-        if (c0 + u * 64 >= p.H8) continue;
-        const u32x4 v = src[c0 + u * 64];
+      for (int q = 0; q < 4; q++) {
+        v[q] = u32x4{0, 0, 0, 0};
+        wj[q] = 0.f;
+        if (part) {
+          const int j = __builtin_ctzll(part);
+          part &= part - 1;
+          if (WEIGHTED) wj[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
+          if (in) v[q] = load_piece<STREAM>((const u32x4*)p.ys + (long)__builtin_amdgcn_readlane(pos, j) * p.H8 + c);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
         if constexpr (WEIGHTED) {
 #pragma unroll
           for (int e = 0; e < 4; e++) {
-            acc[u][2 * e] = __builtin_fmaf(wj, __uint_as_float(v[e] << 16), acc[u][2 * e]);
-            acc[u][2 * e + 1] = __builtin_fmaf(wj, __uint_as_float(v[e] & 0xffff0000u), acc[u][2 * e + 1]);
+            acc[2 * e] = __builtin_fmaf(wj[q], __uint_as_float(v[q][e] << 16), acc[2 * e]);
+            acc[2 * e + 1] = __builtin_fmaf(wj[q], __uint_as_float(v[q][e] & 0xffff0000u), acc[2 * e + 1]);
           }
         } else {
-          acc_bf16x8(acc[u], v);
+          acc_bf16x8(acc, v[q]);
         }
       }
     }
-    u32x4* dst = (u32x4*)p.out + t * p.H8;
-#pragma unroll
-    for (int u = 0; u < U; u++)
-      if (c0 + u * 64 < p.H8) dst[c0 + u * 64] = pack_bf16x8(acc[u]);
+    if (in) store_piece<STREAM>((u32x4*)p.out + t * p.H8 + c, pack_bf16x8(acc));
   }
 }
 
 // dys[row_pos[t, j]] = w[t, j] dout[t], dw[t, j] = <dout[t], ys[row_pos[t, j]]>.  A workgroup takes a token; a row of ys is read
 // before its place is written, by the same lane, so dys may be ys.
-template <int U>
+template <int U, bool STREAM_LOADS, bool STREAM_STORES>
 __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams p) {
   __shared__ float s_dot[4][kMaxChoices];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -284,7 +295,7 @@ __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams 
 #pragma unroll
         for (int u = 0; u < U; u++) {
           v[u] = u32x4{0, 0, 0, 0};
-          if (c0 + u * 256 < p.H8) v[u] = y[c0 + u * 256];
+          if (c0 + u * 256 < p.H8) v[u] = load_piece<STREAM_LOADS>(y + c0 + u * 256);
         }
         float dot = 0.f;
 #pragma unroll
@@ -298,7 +309,7 @@ __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams 
             o[2 * e] = wj * g0;
             o[2 * e + 1] = wj * g1;
           }
-          if (c0 + u * 256 < p.H8) d[c0 + u * 256] = pack_bf16x8(o);
+          if (c0 + u * 256 < p.H8) store_piece<STREAM_STORES>(d + c0 + u * 256, pack_bf16x8(o));
         }
         dot = wave_sum(dot);
         if (lane == 0) s_dot[wave][j] += dot;
@@ -314,7 +325,8 @@ __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams 
 // Gradient of the routing weights with respect to the logits.  With p = softmax(logits) and e_j the chosen experts:
 //   w_j = p_{e_j}:                     dl_i = p_i (sum_{j: e_j = i} dw_j - sum_k p_{e_k} dw_k)
 //   w_j = p_{e_j} / sum_k p_{e_k}:     dl_i = sum_{j: e_j = i} w_j (dw_j - sum_k w_k dw_k),  w the softmax over the chosen logits
-// LANES lanes hold a token's logits, PER each, and one choice each.  Everything is fp32: the exponentials are of differences to the
+// LANES lanes hold a token's logits, PER each, and one choice each: as few as hold the choices, for the reductions over them are what the
+// time goes into (16384 tokens, 64 experts, top-8: 9.7 us with 64 lanes of one logit, 5.5 with 16 of four).  Everything is fp32: the exponentials are of differences to the
 // largest logit, the sums of at most 256 terms.
 // ======================================================================================
 struct RouteGradParams {
@@ -428,6 +440,15 @@ static RowsParams rows_params(const int* row_pos, int T, int H, int topk, int ma
   return p;
 }
 
+// From here on sorted rows go past the caches -- counted as all there can be, for how many take part is known on the device only.  Stores: beyond the
+// dies' L2 together (1024 tokens of 4096, top-8, gradients of combine: 33.2 us, streaming stores 24.4).  Loads: beyond the memory's own cache,
+// and beyond half of it in the gradient of combine, whose rows are the forward pass's (16384 tokens of 2048, top-2: 67 us, streaming loads 57).
+constexpr long kStreamStores = 32L << 20, kStreamLoads = 256L << 20;
+static long sorted_bytes(int T, int H, int topk, int max_rows) {
+  const long rows = (long)T * topk;
+  return (rows < max_rows ? rows : max_rows) * H * 2;
+}
+
 constexpr long kMaxGrid = 1 << 20;     // workgroups; each goes on to further tokens
 static int rows_grid(long waves) { return (int)((waves + 3) / 4 < kMaxGrid ? (waves + 3) / 4 : kMaxGrid); }
 
@@ -505,8 +526,10 @@ int tl_moe_dispatch(tl_ctx* ctx, const void* x, const int* row_pos, int T, int H
   if (int e = check_op_ctx(ctx)) return e;
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.x = (const bf16_t*)x; p.out = (bf16_t*)xs;
-  p.segs = ceil_div(p.H8, 64 * 2);
-  hipLaunchKernelGGL(moe_dispatch_kernel<2>, dim3(rows_grid(p.T * p.segs)), dim3(256), 0, (hipStream_t)stream, p);
+  p.segs = ceil_div(p.H8, 64);
+  const dim3 grid(rows_grid(p.T * p.segs));
+  if (sorted_bytes(T, H, topk, max_rows) > kStreamStores) hipLaunchKernelGGL(moe_dispatch_kernel<true>, grid, dim3(256), 0, (hipStream_t)stream, p);
+  else hipLaunchKernelGGL(moe_dispatch_kernel<false>, grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -520,7 +543,9 @@ int tl_moe_dispatch_grad(tl_ctx* ctx, const void* dxs, const int* row_pos, int T
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.ys = (const bf16_t*)dxs; p.out = (bf16_t*)dx;
   p.segs = ceil_div(p.H8, 64);
-  hipLaunchKernelGGL((moe_gather_sum_kernel<1, false>), dim3(rows_grid(p.T * p.segs)), dim3(256), 0, (hipStream_t)stream, p);
+  const dim3 grid(rows_grid(p.T * p.segs));
+  if (sorted_bytes(T, H, topk, max_rows) > kStreamLoads) hipLaunchKernelGGL((moe_gather_sum_kernel<false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  else hipLaunchKernelGGL((moe_gather_sum_kernel<false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -535,7 +560,9 @@ int tl_moe_combine(tl_ctx* ctx, const void* ys, const float* topk_w, const int* 
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.ys = (const bf16_t*)ys; p.w = topk_w; p.add = (const bf16_t*)add; p.out = (bf16_t*)out;
   p.segs = ceil_div(p.H8, 64);
-  hipLaunchKernelGGL((moe_gather_sum_kernel<1, true>), dim3(rows_grid(p.T * p.segs)), dim3(256), 0, (hipStream_t)stream, p);
+  const dim3 grid(rows_grid(p.T * p.segs));
+  if (sorted_bytes(T, H, topk, max_rows) > kStreamLoads) hipLaunchKernelGGL((moe_gather_sum_kernel<true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  else hipLaunchKernelGGL((moe_gather_sum_kernel<true, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -550,7 +577,11 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout, const void* ys, const flo
   if (int e = check_op_ctx(ctx)) return e;
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.x = (const bf16_t*)dout; p.ys = (const bf16_t*)ys; p.w = topk_w; p.dys = (bf16_t*)dys; p.dw = dtopk_w;
-  hipLaunchKernelGGL(moe_combine_grad_kernel<2>, dim3((int)(p.T < kMaxGrid ? p.T : kMaxGrid)), dim3(256), 0, (hipStream_t)stream, p);
+  const dim3 grid((int)(p.T < kMaxGrid ? p.T : kMaxGrid));
+  const long bytes = sorted_bytes(T, H, topk, max_rows);
+  if (bytes > kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<2, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  else if (bytes > kStreamStores) hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  else hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -575,12 +606,15 @@ int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits, const int* topk_ids
     hipLaunchKernelGGL((moe_route_grad_kernel<LANES, PER>), dim3(ceil_div(T, 256 / LANES)), dim3(256), 0, (hipStream_t)stream, p);
   };
   using std::integral_constant;
-  if (E <= 8) go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-  else if (E <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-  else if (E <= 32) go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-  else if (E <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  else if (E <= 128) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  else go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  auto per = [&](auto lanes_c) {      // logits of a lane
+    constexpr int LANES = decltype(lanes_c)::value;
+    if (E <= LANES) go(lanes_c, integral_constant<int, 1>{});
+    else if (E <= 2 * LANES) go(lanes_c, integral_constant<int, 2>{});
+    else if (E <= 4 * LANES) go(lanes_c, integral_constant<int, 4>{});
+    else if (E <= 8 * LANES) go(lanes_c, integral_constant<int, 8>{});
+    else go(lanes_c, integral_constant<int, 256 / LANES>{});
+  };
+  if (topk <= 16) per(integral_constant<int, 16>{}); else per(integral_constant<int, 32>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
