@@ -21,7 +21,8 @@ struct ProductParams {
   int group_m;
 };
 
-// Where dW goes: stored as streaming (the layer's weights are larger than the caches, and nobody reads their gradient soon).
+// Where dW goes: stored as streaming (the layer's weights are larger than the caches, and nobody reads their gradient soon: 32 of
+// 4096 x 1792 288 -> 270 us).
 struct GradRows16 {
   static constexpr bool SCALED = false, GATED = false;
   bf16_t* c;
@@ -159,11 +160,14 @@ __global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const Produc
 
 // ======================================================================================
 // Few rows for an expert (single tokens being decoded, a small batch over many experts): bound by reading the weights once.  A unit is up
-// to 64 rows of an expert times a block of output columns; NW waves take its steps along the summed axis in turn, each through a ring of
-// its own in LDS, so that no wave waits for another; their sums are joined at the end, in the order of the waves.  Per step
+// to 64 rows of an expert times a block of output columns; it is a wave's alone, or NW waves take its steps along the summed axis in turn,
+// each through a ring of its own in LDS, so that no wave waits for another; their sums are joined at the end, in the order of the waves.
+// Per step
 //   Y^T[columns, rows] += W^T . X^T   (16x16x32 matrix instructions; a lane owns one row and four columns)
-// W as it lies (forward: 32 k-rows of 64 columns, transposing LDS reads) or along its rows (dX: 32 rows of 64 values, plain reads):
-// either way 4 KiB in pieces of a whole 128-byte line.
+// W as it lies (forward: 32 k-rows, transposing LDS reads) or along its rows (dX: pieces of 64 values, plain reads), 4 KiB or, WIDE, 8 KiB of
+// it a step.  Measured for 320 rows of 32 experts of 2048 x 1536 (195 MB): 64 columns a wave 44.7 us, 128 columns 42.9, two waves side by side
+// on 256 columns -- half a KiB of every row -- 40.8, four 57.5 (a compute unit takes no more than about 60 GB/s by direct-to-LDS
+// loads); marked as streaming 42.9 against 45.7.  The kernel alone reaches 5.5 to 6.3 TB/s.
 // ======================================================================================
 struct FewUnit {
   const bf16_t *x, *w;      // first row; W at the unit's first column
@@ -173,7 +177,7 @@ struct FewUnit {
   bool once;                // the weights are this unit's alone: streaming loads
 };
 
-constexpr int kFewRing = 40 * 1024;       // LDS of a wave: four waves a compute unit, with up to 140 KiB in flight together
+constexpr int kFewRing = 40 * 1024;       // LDS of a wave: four waves a compute unit, up to 40 KiB of each in flight
 constexpr int kFewRows = 64;
 
 template <bool NK, int RT, bool WIDE>     // RT: row tiles of 16
@@ -356,7 +360,7 @@ __global__ void __launch_bounds__(NW * NC * 64) moe_few_rows_kernel(const Produc
     const int o = __shfl_up(scan, d);
     if (lane >= d) scan += o;
   }
-  // ---- a die takes a run of units
+  // ---- a die takes a run of units, whose rows of X it then reads once (1024 rows of 32 experts 51.6 -> 47.4 us; no difference with fewer)
   const int units = __builtin_amdgcn_readlane(scan, 63) * p.nbn;
   const int per = (units + kXcds * NC - 1) / (kXcds * NC) * NC, i = blockIdx.x / kXcds * NC + beside, unit = (blockIdx.x % kXcds) * per + i;
   if (i >= per || unit >= units) return;                // (there are fewer than the grid has room for)
@@ -393,123 +397,124 @@ __global__ void __launch_bounds__(NW * NC * 64) moe_few_rows_kernel(const Produc
 // ======================================================================================
 // dW.  An expert's tiles sum over its rows, many or few, so the work is laid out by length, by a launch of its own (one workgroup): an even
 // share of all rows x tiles for every compute unit is the longest an item should be, a longer sum is cut into parts, and the items stand
-// in the order of their length, the longest first, for the hardware to hand out.  The parts of a cut sum go to the workspace in fp32,
+// in the order of their length, the longest first, for the hardware to hand out (8 gradients of 2048 x 1536 over 114 .. 4701 rows, added in fp32:
+// 184 us uncut in the experts' order, 152 so; 2 of 1024 x 1024 over 32768 rows 504 and 147).  The parts of a cut sum go to the workspace in fp32,
 // and a third launch adds them up in their order.
 // A workgroup takes one item: it may end while its stores are on their way.  (A persistent one that requests the next item's first stages
 // before it stores this one's result has to wait, a few steps later, for those stores to be complete, as loads and stores are counted
-// together: 32 gradients of 4096 x 1792 over 512 rows each 284 us against 262.)
+// together: 32 gradients of 4096 x 1792 over 512 rows each 284 us against 272.  Two smaller workgroups a compute unit, of 128 x 256, are held up by
+// their direct-to-LDS loads: 285.)
 // ======================================================================================
 constexpr int kMaxParts = 8;
 constexpr int kMinPart = 256;             // rows
-struct GradWItem {                        // (a 16-byte load)
+struct GradWExpert {                      // (a 16-byte load)
   int row, rows;                          // of x and dy
-  unsigned what;                          // expert, parts << 8, place << 12 (of the part's sums)
-  int tile;
+  unsigned what;                          // expert, parts << 8
+  int place;                              // of its first part's sums
 };
-struct CutTile {
-  int e, tile, parts, place;              // the first part's place
+// At the front of the workspace: the experts by their rows, most first, each with the number of its first item.  Items of an expert: part
+// by part, all tiles of each.
+struct GradWPlan {
+  int first[kMaxProductExperts];
+  GradWExpert expert[kMaxProductExperts];
+  int n_items, n_cut;                     // cut tiles
 };
-struct GradWPlan {                        // at the front of the workspace; items and cut tiles behind it
-  int n_items, n_cut;
-};
-constexpr int kPlanHeader = 128;
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 256;
 
 struct GradWParams {
   ProductParams p;
   GradWPlan* plan;
-  GradWItem* items;
-  CutTile* cut;
   float* partial;          // [places][BM * BN]
   int places, share_of;    // places of partial sums; compute units that share the work
   int run;
 };
 
 __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const GradWParams g) {
-  __shared__ int s_lo[kMaxProductExperts], s_n[kMaxProductExperts], s_expert[kMaxProductExperts], s_first[kMaxProductExperts], s_place[kMaxProductExperts];
-  __shared__ int s_chunk, s_items;
+  static_assert(kPlanThreads == kMaxProductExperts, "an expert to a thread");
+  __shared__ int s_n[kMaxProductExperts], s_rank[kMaxProductExperts], s_by_rank[kMaxProductExperts];
   const ProductParams& p = g.p;
   const int tid = threadIdx.x, lane = tid & 63;
   const int per = p.nbm * p.nbn;
-  if (tid < kMaxProductExperts) {
-    int lo = 0, n = -1;
-    if (tid < p.E) rows_of(p, tid, &lo, &n);
-    s_lo[tid] = lo;
-    s_n[tid] = n;
+  int lo = 0, n = -1;
+  if (tid < p.E) rows_of(p, tid, &lo, &n);
+  s_n[tid] = n;
+  __syncthreads();
+  int rank = 0;
+  long all = 0;
+  for (int o = 0; o < p.E; o++) {
+    const int m = s_n[o];
+    rank += m > n || (m == n && o < tid);
+    all += m;
+  }
+  // the longest part there is to be
+  const long share = (all * per + g.share_of - 1) / g.share_of;
+  const unsigned chunk = g.places ? (unsigned)max(min(share, 0x7fffffffL), (long)kMinPart) : 0x7fffffffu;
+  auto parts_of = [&](int m) { return max(min((int)(((unsigned)max(m, 0) + (chunk - 1)) / chunk), kMaxParts), 1); };     // (both below 2^31)
+  s_by_rank[tid] = -1;
+  // Many rounds of items: those of more than 1.5 times the mean first, the others as they come, so that some workgroups store while others
+  // multiply (64 gradients of 2048 x 1536 over 256 rows each in the mean 190 us longest first, 179 so); what the last round is then left
+  // with weighs little.
+  const bool cut_any = __syncthreads_or(parts_of(n) > 1);
+  if (!cut_any && (long)p.E * per >= 4L * g.share_of) {
+    const int some = (int)min(all * 3 / (2 * p.E), 0x7fffffffL);
+    if (n <= some) {
+      rank = 0;
+      for (int o = 0; o < p.E; o++) rank += s_n[o] > some || o < tid;
+    }
+  }
+  if (tid < p.E) {
+    s_by_rank[rank] = n;
+    s_rank[tid] = rank;
   }
   __syncthreads();
-  if (tid < p.E) {     // the experts by their rows, most first
-    const int n = s_n[tid];
-    int rank = 0;
-    for (int o = 0; o < p.E; o++) rank += s_n[o] > n || (s_n[o] == n && o < tid);
-    s_expert[rank] = tid;
-  }
-  if (tid < 64) {      // the longest part there is to be
-    long all = 0;
-#pragma unroll
-    for (int i = 0; i < 4; i++) all += max(s_n[lane * 4 + i], 0);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
-    const long share = (all * per + g.share_of - 1) / g.share_of;
-    if (lane == 0) s_chunk = g.places ? (int)max(min(share, 0x7fffffffL), (long)kMinPart) : 0x7fffffff;
-  }
-  __syncthreads();
-  const unsigned chunk = (unsigned)s_chunk;
-  auto parts_of = [&](int n) { return max(min((int)(((unsigned)max(n, 0) + (chunk - 1)) / chunk), kMaxParts), 1); };     // (both below 2^31)
   if (tid < 64) {
-    int items[4], places[4], at[4], pl[4];
+    int items[4], places[4], at[4], pl[4], cut = 0;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const int r = lane * 4 + i, parts = r < p.E ? parts_of(s_n[s_expert[r]]) : 0;
+      const int r = lane * 4 + i, parts = r < p.E ? parts_of(s_by_rank[r]) : 0;
       items[i] = parts * per;
       places[i] = parts > 1 ? items[i] : 0;
+      cut += parts > 1 ? per : 0;
     }
-    const int n_items = scan_starts(items, at), n_places = scan_starts(places, pl);
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      s_first[lane * 4 + i] = at[i];
-      s_place[lane * 4 + i] = pl[i];
-    }
-    int cut = 0;
-#pragma unroll
-    for (int i = 0; i < 4; i++) cut += places[i] ? per : 0;
+    const int n_items = scan_starts(items, at);
+    scan_starts(places, pl);       // (at most g.places: see grad_w_shape)
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) cut += __shfl_xor(cut, d);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      g.plan->first[lane * 4 + i] = at[i];
+      s_n[lane * 4 + i] = pl[i];
+    }
     if (lane == 0) {
-      s_items = n_items;
       g.plan->n_items = n_items;
       g.plan->n_cut = cut;
     }
-    (void)n_places;      // (at most g.places: see grad_w_shape)
   }
   __syncthreads();
-  const int n_items = s_items;
-  for (int l = tid; l < n_items; l += kPlanThreads) {
-    int r = 0;    // the last of the sorted experts whose items start at or before l
-#pragma unroll
-    for (int d = kMaxProductExperts / 2; d >= 1; d /= 2)
-      if (r + d < p.E && s_first[r + d] <= l) r += d;
-    const int e = s_expert[r], n = s_n[e], parts = parts_of(n);
-    const int item = l - s_first[r], part = item / per, tile = item - part * per;
-    const int k0 = n / parts * part + min(part, n % parts), k1 = n / parts * (part + 1) + min(part + 1, n % parts);
-    const int place0 = s_place[r] + tile * parts;
-    g.items[l] = GradWItem{s_lo[e] + k0, k1 - k0, (unsigned)e | (unsigned)parts << 8 | (unsigned)(parts > 1 ? place0 + part : 0) << 12, tile};
-    // (experts with cut sums come first: their tiles are numbers r * per + tile)
-    if (parts > 1 && part == 0) g.cut[r * per + tile] = CutTile{e, tile, parts, place0};
-  }
+  if (tid < p.E) g.plan->expert[s_rank[tid]] = GradWExpert{lo, n, (unsigned)tid | (unsigned)parts_of(n) << 8, s_n[s_rank[tid]]};
 }
+
+// Where part number `part` of n rows in `parts` begins.
+__device__ __forceinline__ int part_start(int n, int parts, int part) { return n / parts * part + min(part, n % parts); }
 
 template <class Cfg, class Out>
 __global__ void __launch_bounds__(Cfg::NTHREADS) moe_grad_w_kernel(const GradWParams g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const ProductParams& p = g.p;
-  // runs of g.run items go to one die, which then reads its part of the rows once
+  // runs of g.run items go to one die, which then reads its part of the rows once (32 gradients of 4096 x 1792: 322 us without, 288 with)
   const int i = blockIdx.x / kXcds, l = ((i / g.run) * kXcds + blockIdx.x % kXcds) * g.run + i % g.run;
-  const u32x4 rec = *(const u32x4*)(g.items + l);       // (whatever it is where there is no such item: there is room for the whole grid)
+  const u32x4 starts = ((const u32x4*)g.plan->first)[threadIdx.x & 63];
   if (l >= g.plan->n_items) return;
-  const int row0 = __builtin_amdgcn_readfirstlane(rec[0]), n = __builtin_amdgcn_readfirstlane(rec[1]), tile = __builtin_amdgcn_readfirstlane(rec[3]);
+  int start[4];
+#pragma unroll
+  for (int c = 0; c < 4; c++) start[c] = (int)starts[c];
+  const int r = last_start(start, l);
+  const u32x4 rec = ((const u32x4*)g.plan->expert)[r];
+  const int lo = __builtin_amdgcn_readfirstlane(rec[0]), all = __builtin_amdgcn_readfirstlane(rec[1]), place0 = __builtin_amdgcn_readfirstlane(rec[3]);
   const unsigned what = __builtin_amdgcn_readfirstlane(rec[2]);
-  const int e = what & 255, parts = (what >> 8) & 15, place = what >> 12;
+  const int e = what & 255, parts = what >> 8;
+  const int per = p.nbm * p.nbn, item = l - __builtin_amdgcn_readfirstlane(g.plan->first[r]), part = item / per, tile = item - part * per;
+  const int k0 = part_start(all, parts, part), n = part_start(all, parts, part + 1) - k0, row0 = lo + k0, place = place0 + tile * parts + part;
   const int bm = tile / p.nbn, bn = tile - bm * p.nbn;
   const int row = bm * Cfg::BM, rows = min(Cfg::BM, p.K - row), col = bn * Cfg::BN, cols = min(Cfg::BN, p.N - col);
   const long at = ((long)e * p.K + row) * p.N + col;
@@ -538,18 +543,19 @@ template <int TILE, class Out>
 __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams g) {
   const ProductParams& p = g.p;
   constexpr int kSlices = TILE * TILE / 8 / 256;
-  const int n = g.plan->n_cut * kSlices;
+  const int n = g.plan->n_cut * kSlices, per = p.nbm * p.nbn;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const CutTile t = g.cut[i / kSlices];
+    const GradWExpert x4 = g.plan->expert[i / kSlices / per];           // (the experts with cut sums come first)
+    const int e = x4.what & 255, parts = x4.what >> 8, tile = i / kSlices % per;
     const int chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (TILE / 8), x = chunk % (TILE / 8) * 8;
-    const int bm = t.tile / p.nbn, bn = t.tile - bm * p.nbn;
+    const int bm = tile / p.nbn, bn = tile - bm * p.nbn;
     if (bm * TILE + y >= p.K || bn * TILE + x >= p.N) continue;
-    const float* src = g.partial + (long)t.place * (TILE * TILE) + y * TILE + x;
+    const float* src = g.partial + ((long)x4.place + (long)tile * parts) * (TILE * TILE) + y * TILE + x;
     floatx4 v[kMaxParts][2];
 #pragma unroll
     for (int q = 0; q < kMaxParts; q++) {
       v[q][0] = v[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (q < t.parts) {
+      if (q < parts) {
         v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE)));
         v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE) + 4));
       }
@@ -561,7 +567,7 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
     for (int q = 1; q < kMaxParts; q++)
 #pragma unroll
       for (int c = 0; c < 8; c++) o[c] += v[q][c / 4][c % 4];
-    const long at = ((long)t.e * p.K + bm * TILE) * p.N + bn * TILE;
+    const long at = ((long)e * p.K + bm * TILE) * p.N + bn * TILE;
     if constexpr (StoresF32<Out>::value) {
       const Out out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
 #pragma unroll
@@ -598,7 +604,7 @@ static int check_product(const char* what, int max_rows, int K, int N, int E) {
 struct GradWShape {
   int tile, nbm, nbn, places, run;
   long grid;                                   // items at most, in whole runs for every die
-  size_t items_at, cut_at, partial_at, ws_bytes;
+  size_t partial_at, ws_bytes;
 };
 static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, int E) {
   GradWShape s;
@@ -611,14 +617,12 @@ static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, in
   const long per = (long)s.nbm * s.nbn;
   // A share is all rows x tiles over the compute units, and no sum is longer than all rows: none is cut where every expert has a tile for every
   // unit.  A cut one of n rows has fewer than 2 n / share parts in each of its tiles, all together fewer than two for every unit.
-  s.places = per < cus && max_rows > kMinPart ? 2 * cus : 0;
+  s.places = per < cus && max_rows > 2 * kMinPart ? 2 * cus : 0;
   s.run = (int)min((per + kXcds - 1) / kXcds, 32L);
   const long span = (long)s.run * kXcds;
   s.grid = (E * per + s.places + span - 1) / span * span;
   auto up = [](size_t b) { return (b + 127) / 128 * 128; };
-  s.items_at = kPlanHeader;
-  s.cut_at = up(s.items_at + s.grid * sizeof(GradWItem));
-  s.partial_at = up(s.cut_at + s.places / 2 * sizeof(CutTile));
+  s.partial_at = up(sizeof(GradWPlan));
   s.ws_bytes = up(s.partial_at + (size_t)s.places * s.tile * s.tile * sizeof(float));
   return s;
 }
@@ -688,7 +692,7 @@ static int launch_grad_w(const GradWParams& g, long grid, hipStream_t s) {
   TL_HIP(hipGetLastError());
   if (int e = launch_fused<Cfg>(moe_grad_w_kernel<Cfg, Out>, g, (int)grid, s)) return e;
   if (g.places) {
-    hipLaunchKernelGGL((moe_grad_w_join_kernel<Cfg::BM, Out>), dim3(2048), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((moe_grad_w_join_kernel<Cfg::BM, Out>), dim3(512), dim3(256), 0, s, g);
     TL_HIP(hipGetLastError());
   }
   return TL_OK;
@@ -746,8 +750,6 @@ int tl_moe_gemm_grad_w(tl_ctx* ctx, const void* x, const void* dy, const int* ex
   p.nbm = shape.nbm; p.nbn = shape.nbn;
   char* ws = (char*)workspace;
   g.plan = (GradWPlan*)ws;
-  g.items = (GradWItem*)(ws + shape.items_at);
-  g.cut = (CutTile*)(ws + shape.cut_at);
   g.partial = (float*)(ws + shape.partial_at);
   g.places = shape.places;
   g.share_of = ctx->num_cus;

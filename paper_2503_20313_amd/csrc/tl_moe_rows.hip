@@ -579,7 +579,7 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout, const void* ys, const flo
   p.x = (const bf16_t*)dout; p.ys = (const bf16_t*)ys; p.w = topk_w; p.dys = (bf16_t*)dys; p.dw = dtopk_w;
   const dim3 grid((int)(p.T < kMaxGrid ? p.T : kMaxGrid));
   const long bytes = sorted_bytes(T, H, topk, max_rows);
-  if (bytes > kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<2, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  if (bytes >= kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<2, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
   else if (bytes > kStreamStores) hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
   else hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
