@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(NW * NC * 64) moe_few_rows_kernel(const Produc
 // A workgroup takes one item: it may end while its stores are on their way.  (A persistent one that requests the next item's first stages
 // before it stores this one's result has to wait, a few steps later, for those stores to be complete, as loads and stores are counted
 // together: 32 gradients of 4096 x 1792 over 512 rows each 284 us against 272.  Two smaller workgroups a compute unit, of 128 x 256, are held up by
-// their direct-to-LDS loads: 285.)
+// their direct-to-LDS loads: 289.)
 // ======================================================================================
 constexpr int kMaxParts = 8;
 constexpr int kMinPart = 256;             // rows
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const Gra
 __device__ __forceinline__ int part_start(int n, int parts, int part) { return n / parts * part + min(part, n % parts); }
 
 template <class Cfg, class Out>
-__global__ void __launch_bounds__(Cfg::NTHREADS) moe_grad_w_kernel(const GradWParams g) {
+__global__ void __launch_bounds__(Cfg::NTHREADS, Cfg::LDS_BYTES <= 80 * 1024 ? 2 : 1) moe_grad_w_kernel(const GradWParams g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const ProductParams& p = g.p;
   // runs of g.run items go to one die, which then reads its part of the rows once (32 gradients of 4096 x 1792: 322 us without, 288 with)
@@ -539,25 +539,25 @@ __global__ void __launch_bounds__(Cfg::NTHREADS) moe_grad_w_kernel(const GradWPa
 }
 
 // The cut sums: eight neighbouring columns to a thread.
-template <int TILE, class Out>
+template <class Cfg, class Out>
 __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams g) {
   const ProductParams& p = g.p;
-  constexpr int kSlices = TILE * TILE / 8 / 256;
+  constexpr int BM = Cfg::BM, BN = Cfg::BN, kSlices = BM * BN / 8 / 256;
   const int n = g.plan->n_cut * kSlices, per = p.nbm * p.nbn;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const GradWExpert x4 = g.plan->expert[i / kSlices / per];           // (the experts with cut sums come first)
     const int e = x4.what & 255, parts = x4.what >> 8, tile = i / kSlices % per;
-    const int chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (TILE / 8), x = chunk % (TILE / 8) * 8;
+    const int chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (BN / 8), x = chunk % (BN / 8) * 8;
     const int bm = tile / p.nbn, bn = tile - bm * p.nbn;
-    if (bm * TILE + y >= p.K || bn * TILE + x >= p.N) continue;
-    const float* src = g.partial + ((long)x4.place + (long)tile * parts) * (TILE * TILE) + y * TILE + x;
+    if (bm * BM + y >= p.K || bn * BN + x >= p.N) continue;
+    const float* src = g.partial + ((long)x4.place + (long)tile * parts) * (BM * BN) + y * BN + x;
     floatx4 v[kMaxParts][2];
 #pragma unroll
     for (int q = 0; q < kMaxParts; q++) {
       v[q][0] = v[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (q < parts) {
-        v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE)));
-        v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (TILE * TILE) + 4));
+        v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (BM * BN)));
+        v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (BM * BN) + 4));
       }
     }
     float o[8];
@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
     for (int q = 1; q < kMaxParts; q++)
 #pragma unroll
       for (int c = 0; c < 8; c++) o[c] += v[q][c / 4][c % 4];
-    const long at = ((long)e * p.K + bm * TILE) * p.N + bn * TILE;
+    const long at = ((long)e * p.K + bm * BM) * p.N + bn * BN;
     if constexpr (StoresF32<Out>::value) {
       const Out out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
 #pragma unroll
@@ -591,6 +591,7 @@ template <bool NK> using ProductBigHalf = TileCfg<128, 256, 2, 4, 32, 4, false, 
 template <bool NK> using ProductSmall = TileCfg<128, 128, 2, 2, 64, 4, false, NK>;
 template <bool NK> using ProductSmallHalf = TileCfg<64, 128, 2, 2, 64, 4, false, NK>;
 typedef TileCfg<256, 256, 2, 4, 32, 4, true, false> CfgW256;
+typedef TileCfg<128, 256, 2, 2, 32, 3, true, false> CfgW128x256;      // two workgroups a compute unit
 typedef TileCfg<128, 128, 2, 2, 64, 4, true, false> CfgW128;
 
 static int check_product(const char* what, int max_rows, int K, int N, int E) {
@@ -602,18 +603,22 @@ static int check_product(const char* what, int max_rows, int K, int N, int E) {
 }
 
 struct GradWShape {
-  int tile, nbm, nbn, places, run;
+  int bm, bn, nbm, nbn, places, run;
   long grid;                                   // items at most, in whole runs for every die
   size_t partial_at, ws_bytes;
 };
 static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, int E) {
   GradWShape s;
   const int cus = min(ctx->num_cus, 1 << 16);
-  // The large tile, unless even its cut sums would leave compute units without work.
+  // The large tile; the half one, two workgroups a compute unit, where large ones make one to two rounds: they are too coarse for that, and its ends
+  // run beside another's sum (8 gradients of 2048 x 1536 over 114 .. 4701 rows in fp32 145 -> 133 us, 4 of 2048 x 2048 over 512 rows 53 -> 27;
+  // but 8 of 4096 x 2048 over 2048 rows, four rounds, 223 -> 243).  The small one where even the cut sums of large ones would leave compute
+  // units without work (4 of 512 x 512 over 4096 rows: 54.7 us uncut, 37.6).
   const long tiles = (long)E * ceil_div(K, 256) * ceil_div(N, 256), parts = max(min(max_rows / E / kMinPart, kMaxParts), 1);
-  s.tile = tiles * parts < cus ? 128 : 256;
-  s.nbm = ceil_div(K, s.tile);
-  s.nbn = ceil_div(N, s.tile);
+  s.bm = s.bn = tiles * parts < cus ? 128 : 256;
+  if (tiles >= cus && tiles < 2L * cus) s.bm = 128;
+  s.nbm = ceil_div(K, s.bm);
+  s.nbn = ceil_div(N, s.bn);
   const long per = (long)s.nbm * s.nbn;
   // A share is all rows x tiles over the compute units, and no sum is longer than all rows: none is cut where every expert has a tile for every
   // unit.  A cut one of n rows has fewer than 2 n / share parts in each of its tiles, all together fewer than two for every unit.
@@ -623,7 +628,7 @@ static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, in
   s.grid = (E * per + s.places + span - 1) / span * span;
   auto up = [](size_t b) { return (b + 127) / 128 * 128; };
   s.partial_at = up(sizeof(GradWPlan));
-  s.ws_bytes = up(s.partial_at + (size_t)s.places * s.tile * s.tile * sizeof(float));
+  s.ws_bytes = up(s.partial_at + (size_t)s.places * s.bm * s.bn * sizeof(float));
   return s;
 }
 
@@ -692,7 +697,7 @@ static int launch_grad_w(const GradWParams& g, long grid, hipStream_t s) {
   TL_HIP(hipGetLastError());
   if (int e = launch_fused<Cfg>(moe_grad_w_kernel<Cfg, Out>, g, (int)grid, s)) return e;
   if (g.places) {
-    hipLaunchKernelGGL((moe_grad_w_join_kernel<Cfg::BM, Out>), dim3(512), dim3(256), 0, s, g);
+    hipLaunchKernelGGL((moe_grad_w_join_kernel<Cfg, Out>), dim3(512), dim3(256), 0, s, g);
     TL_HIP(hipGetLastError());
   }
   return TL_OK;
@@ -755,7 +760,8 @@ int tl_moe_gemm_grad_w(tl_ctx* ctx, const void* x, const void* dy, const int* ex
   g.share_of = ctx->num_cus;
   g.run = shape.run;
   hipStream_t s = (hipStream_t)stream;
-  if (shape.tile == 128) return dw_f32 ? launch_grad_w<CfgW128, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW128, GradRows16>(g, shape.grid, s);
+  if (shape.bm != shape.bn) return dw_f32 ? launch_grad_w<CfgW128x256, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW128x256, GradRows16>(g, shape.grid, s);
+  if (shape.bm == 128) return dw_f32 ? launch_grad_w<CfgW128, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW128, GradRows16>(g, shape.grid, s);
   return dw_f32 ? launch_grad_w<CfgW256, GradRows32>(g, shape.grid, s) : launch_grad_w<CfgW256, GradRows16>(g, shape.grid, s);
 }
 
