@@ -9,6 +9,8 @@
 namespace tl {
 
 constexpr int kMaxProductExperts = 256;
+constexpr int kMaxParts = 8;              // of a cut sum
+constexpr int kPartUnit = 64;             // values of Y's and dX's sums that parts are made of
 
 struct ProductParams {
   const bf16_t *x, *w, *dy;
@@ -18,6 +20,9 @@ struct ProductParams {
   float* out32;
   int max_rows, K, N, E;
   int nbm, nbn;            // column blocks; for dW also row blocks of an expert's K x N
+  int parts, k_units;      // Y and dX with a cut sum: parts, units of kPartUnit values,
+  int most;                // tiles that the workspace has room for: all there can be, unless the experts' rows overlap
+  float* partial;
   int group_m;
 };
 
@@ -63,6 +68,9 @@ __device__ __forceinline__ void rows_of(const ProductParams& p, int e, int* lo, 
   *n = max(min(max(p.offsets[e + 1], 0), p.max_rows) - *lo, 0);
 }
 
+// Where part number `part` of n things in `parts` begins.
+__device__ __forceinline__ int part_start(int n, int parts, int part) { return n / parts * part + min(part, n % parts); }
+
 // The number, among ascending starts, of the last start at or before x, for a wave whose lane i holds starts 4i .. 4i + 3.
 __device__ __forceinline__ int last_start(const int (&start)[4], int x) {
   int c = 0;
@@ -89,45 +97,50 @@ __device__ __forceinline__ int scan_starts(const int (&count)[4], int (&start)[4
 // Y and dX.  An expert's rows make tiles of BM rows, and a half one where the rest fits into that (an expert's last tile is half empty in the
 // mean; with whole ones alone 16384 rows of 32 experts cost a fifth more); whole tiles first, in patches that share rows and columns in
 // a die's L2, then the half ones.
-template <class Big, class Half, bool GRAD_X>
-__global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const ProductParams p) {
-  static_assert(Big::NTHREADS == Half::NTHREADS && Big::BN == Half::BN && Big::BM == 2 * Half::BM, "the two shapes share workgroup and columns");
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  __shared__ int s_lo[kMaxProductExperts], s_n[kMaxProductExperts], s_at[kMaxProductExperts];     // an expert's rows, its first whole tile
-  const int tid = threadIdx.x, lane = tid & 63;
-  for (int e = tid; e < kMaxProductExperts; e += Big::NTHREADS) {
-    int lo = 0, n = 0;
-    if (e < p.E) rows_of(p, e, &lo, &n);
-    s_lo[e] = lo;
-    s_n[e] = n;
-  }
-  __syncthreads();
-  int big[4], half[4], big_at[4], half_at[4];
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int n = s_n[lane * 4 + i], rest = n % Big::BM;
-    half[i] = rest > 0 && rest <= Half::BM ? 1 : 0;
-    big[i] = n / Big::BM + (rest > Half::BM ? 1 : 0);
-  }
+struct ProductJob { bool big; int e, rows, col, cols; long at; };
+
+template <int BM, int BN>
+struct ProductTiles {
+  int big_at[4], half_at[4];      // first whole and first half tile of experts 4 lane .. 4 lane + 3
   Sched sc;
-  sc.nbm = scan_starts(big, big_at);
-  const int n_half = scan_starts(half, half_at);
-  if (tid < 64) {
+  int n_all;
+  const int *s_lo, *s_n, *s_at;   // in LDS: an expert's rows, its first whole tile
+  // By all threads of the workgroup.
+  __device__ __forceinline__ void init(const ProductParams& p, int grid, int (&lds)[3][kMaxProductExperts]) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    for (int e = tid; e < kMaxProductExperts; e += blockDim.x) {
+      int lo = 0, n = 0;
+      if (e < p.E) rows_of(p, e, &lo, &n);
+      lds[0][e] = lo;
+      lds[1][e] = n;
+    }
+    __syncthreads();
+    int big[4], half[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) s_at[lane * 4 + i] = big_at[i];
+    for (int i = 0; i < 4; i++) {
+      const int n = lds[1][lane * 4 + i], rest = n % BM;
+      half[i] = rest > 0 && rest <= BM / 2 ? 1 : 0;
+      big[i] = n / BM + (rest > BM / 2 ? 1 : 0);
+    }
+    sc.nbm = scan_starts(big, big_at);
+    const int n_half = scan_starts(half, half_at);
+    if (tid < 64) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) lds[2][lane * 4 + i] = big_at[i];
+    }
+    __syncthreads();
+    s_lo = lds[0]; s_n = lds[1]; s_at = lds[2];
+    sc.nbn = p.nbn;
+    sc.n_tiles = sc.nbm * sc.nbn;
+    sc.G = grid;
+    sc.first_block = 0;
+    sc.swizzle = 1;
+    sc.group_m = p.group_m < sc.nbm ? p.group_m : (sc.nbm > 0 ? sc.nbm : 1);
+    n_all = sc.n_tiles + n_half * sc.nbn;
   }
-  __syncthreads();
-  sc.nbn = p.nbn;
-  sc.n_tiles = sc.nbm * sc.nbn;
-  sc.G = gridDim.x;
-  sc.first_block = 0;
-  sc.swizzle = 1;
-  sc.group_m = p.group_m < sc.nbm ? p.group_m : (sc.nbm > 0 ? sc.nbm : 1);
-  const int n_all = sc.n_tiles + n_half * sc.nbn;
-  const int kdim = GRAD_X ? p.N : p.K, ndim = GRAD_X ? p.K : p.N;
-  struct Job { bool big; int e, rows, col, cols; long at; };
-  auto job_at = [&](int pos) {
-    Job j;
+  // Tile number pos < n_all; by whole waves.
+  __device__ __forceinline__ ProductJob at(int pos, int ndim) const {
+    ProductJob j;
     j.big = pos < sc.n_tiles;
     int bm, bn, r0;
     if (j.big) {
@@ -135,26 +148,85 @@ __global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const Produc
       bm = tile / sc.nbn;
       bn = tile - bm * sc.nbn;
       j.e = last_start(big_at, bm);
-      r0 = (bm - __builtin_amdgcn_readfirstlane(s_at[j.e])) * Big::BM;
+      r0 = (bm - __builtin_amdgcn_readfirstlane(s_at[j.e])) * BM;
     } else {
       bm = (pos - sc.n_tiles) / sc.nbn;
       bn = pos - sc.n_tiles - bm * sc.nbn;
       j.e = last_start(half_at, bm);
-      r0 = __builtin_amdgcn_readfirstlane(s_n[j.e]) / Big::BM * Big::BM;
+      r0 = __builtin_amdgcn_readfirstlane(s_n[j.e]) / BM * BM;
     }
-    j.rows = min(__builtin_amdgcn_readfirstlane(s_n[j.e]) - r0, Big::BM);
+    j.rows = min(__builtin_amdgcn_readfirstlane(s_n[j.e]) - r0, BM);
     j.at = __builtin_amdgcn_readfirstlane(s_lo[j.e]) + r0;
-    j.col = bn * Big::BN;
-    j.cols = min(Big::BN, ndim - j.col);
+    j.col = bn * BN;
+    j.cols = min(BN, ndim - j.col);
     return j;
-  };
-  for (int pos = blockIdx.x; pos < n_all; pos += gridDim.x) {
-    const Job j = job_at(pos);
-    const DenseRows out{p.out + j.at * ndim + j.col, ndim};
-    const bf16_t* a = (GRAD_X ? p.dy : p.x) + j.at * kdim;
-    const bf16_t* b = p.w + (long)j.e * p.K * p.N + (GRAD_X ? (long)j.col * p.N : (long)j.col);
-    if (j.big) gemm_tile<Big>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, kdim, smem);
-    else gemm_tile<Half>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, kdim, smem);
+  }
+};
+
+// CUT: the summed axis is cut into p.parts parts, whose sums go to the workspace (place tile * parts + part) for the join kernel.
+template <class Big, class Half, bool GRAD_X, bool CUT>
+__global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const ProductParams p) {
+  static_assert(Big::NTHREADS == Half::NTHREADS && Big::BN == Half::BN && Big::BM == 2 * Half::BM, "the two shapes share workgroup and columns");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ int s_experts[3][kMaxProductExperts];
+  ProductTiles<Big::BM, Big::BN> tiles;
+  tiles.init(p, gridDim.x, s_experts);
+  const int kdim = GRAD_X ? p.N : p.K, ndim = GRAD_X ? p.K : p.N;
+  if constexpr (CUT) tiles.n_all = min(tiles.n_all, p.most);
+  const int n_items = CUT ? tiles.n_all * p.parts : tiles.n_all;
+  for (int pos = blockIdx.x; pos < n_items; pos += gridDim.x) {
+    const int part = CUT ? pos / tiles.n_all : 0, tile = pos - part * tiles.n_all;
+    const ProductJob j = tiles.at(tile, ndim);
+    const int k0 = CUT ? part_start(p.k_units, p.parts, part) * kPartUnit : 0;
+    const int k = CUT ? min(part_start(p.k_units, p.parts, part + 1) * kPartUnit, kdim) - k0 : kdim;
+    const bf16_t* a = (GRAD_X ? p.dy : p.x) + j.at * kdim + k0;
+    const bf16_t* b = p.w + (long)j.e * p.K * p.N + (GRAD_X ? (long)j.col * p.N + k0 : (long)k0 * p.N + j.col);
+    if constexpr (CUT) {
+      const PartRows out{p.partial + ((long)tile * p.parts + part) * (Big::BM * Big::BN), Big::BN};
+      if (j.big) gemm_tile<Big>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
+      else gemm_tile<Half>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
+    } else {
+      const DenseRows out{p.out + j.at * ndim + j.col, ndim};
+      if (j.big) gemm_tile<Big>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
+      else gemm_tile<Half>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
+    }
+  }
+}
+
+// Sum of up to kMaxParts partial results of eight neighbouring columns, `step` apart, in their order: all loads in flight together.
+__device__ __forceinline__ void join_parts(const float* src, long step, int parts, float (&o)[8]) {
+  floatx4 v[kMaxParts][2];
+#pragma unroll
+  for (int q = 0; q < kMaxParts; q++) {
+    v[q][0] = v[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (q < parts) {
+      v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + q * step));
+      v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + q * step + 4));
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 8; c++) o[c] = v[0][c / 4][c % 4];
+#pragma unroll
+  for (int q = 1; q < kMaxParts; q++)
+#pragma unroll
+    for (int c = 0; c < 8; c++) o[c] += v[q][c / 4][c % 4];
+}
+
+template <int BM, int BN, bool GRAD_X>
+__global__ void __launch_bounds__(256) moe_product_join_kernel(const ProductParams p, int grid) {
+  __shared__ int s_experts[3][kMaxProductExperts];
+  ProductTiles<BM, BN> tiles;
+  tiles.init(p, grid, s_experts);
+  tiles.n_all = min(tiles.n_all, p.most);
+  const int ndim = GRAD_X ? p.K : p.N;
+  constexpr int kSlices = BM * BN / 8 / 256;
+  for (int i = blockIdx.x; i < tiles.n_all * kSlices; i += gridDim.x) {
+    const int tile = i / kSlices, chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (BN / 8), x = chunk % (BN / 8) * 8;
+    const ProductJob j = tiles.at(tile, ndim);
+    if (y >= j.rows || x >= j.cols) continue;
+    float o[8];
+    join_parts(p.partial + (long)tile * p.parts * (BM * BN) + y * BN + x, BM * BN, p.parts, o);
+    *(u32x4*)(p.out + (j.at + y) * ndim + j.col + x) = pack_bf16x8(o);
   }
 }
 
@@ -405,7 +477,6 @@ __global__ void __launch_bounds__(NW * NC * 64) moe_few_rows_kernel(const Produc
 // together: 32 gradients of 4096 x 1792 over 512 rows each 284 us against 272.  Two smaller workgroups a compute unit, of 128 x 256, are held up by
 // their direct-to-LDS loads: 289.)
 // ======================================================================================
-constexpr int kMaxParts = 8;
 constexpr int kMinPart = 256;             // rows
 struct GradWExpert {                      // (a 16-byte load)
   int row, rows;                          // of x and dy
@@ -494,9 +565,6 @@ __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const Gra
   if (tid < p.E) g.plan->expert[s_rank[tid]] = GradWExpert{lo, n, (unsigned)tid | (unsigned)parts_of(n) << 8, s_n[s_rank[tid]]};
 }
 
-// Where part number `part` of n rows in `parts` begins.
-__device__ __forceinline__ int part_start(int n, int parts, int part) { return n / parts * part + min(part, n % parts); }
-
 template <class Cfg, class Out>
 __global__ void __launch_bounds__(Cfg::NTHREADS, Cfg::LDS_BYTES <= 80 * 1024 ? 2 : 1) moe_grad_w_kernel(const GradWParams g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -551,22 +619,8 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
     const int bm = tile / p.nbn, bn = tile - bm * p.nbn;
     if (bm * BM + y >= p.K || bn * BN + x >= p.N) continue;
     const float* src = g.partial + ((long)x4.place + (long)tile * parts) * (BM * BN) + y * BN + x;
-    floatx4 v[kMaxParts][2];
-#pragma unroll
-    for (int q = 0; q < kMaxParts; q++) {
-      v[q][0] = v[q][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (q < parts) {
-        v[q][0] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (BM * BN)));
-        v[q][1] = __builtin_nontemporal_load((const floatx4*)(src + (long)q * (BM * BN) + 4));
-      }
-    }
     float o[8];
-#pragma unroll
-    for (int c = 0; c < 8; c++) o[c] = v[0][c / 4][c % 4];
-#pragma unroll
-    for (int q = 1; q < kMaxParts; q++)
-#pragma unroll
-      for (int c = 0; c < 8; c++) o[c] += v[q][c / 4][c % 4];
+    join_parts(src, BM * BN, parts, o);
     const long at = ((long)e * p.K + bm * BM) * p.N + bn * BN;
     if constexpr (StoresF32<Out>::value) {
       const Out out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
@@ -586,6 +640,24 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
 // ======================================================================================
 // Host side
 // ======================================================================================
+constexpr long kFewMean = 48;              // rows of an expert, in the mean, up to which the few-row kernel is taken
+
+// Y's and dX's cut sums: where tiles of 128 x 128, as many as there can be at most, leave three quarters of the compute units without work and the
+// sum is long (a single row through 8192 x 1024 28 -> 13 us, 128 rows of 2 experts of 8192 x 512 45 -> 17, 64 of 4096 x 4096 23 -> 17.5; a sum
+// of 2048 gains nothing, and dX's few rows, whose weights arrive in whole lines, nothing at 4096: 14 us against 12).  All parts have a unit at
+// least.
+struct ProductCut {
+  int parts, tiles;
+  size_t bytes;
+};
+static ProductCut product_cut(const tl_ctx* ctx, bool grad_x, int max_rows, int K, int N, int E) {
+  const int kdim = grad_x ? N : K, ndim = grad_x ? K : N;
+  const long tiles = ((long)max_rows / 128 + min(max_rows, E)) * ceil_div(ndim, 128);
+  const long parts = min(ctx->num_cus / tiles, (long)kMaxParts);
+  if (parts < 4 || kdim <= (grad_x && max_rows <= kFewMean * E ? 4096 : 2048)) return {1, 0, 0};
+  return {(int)parts, (int)tiles, (size_t)tiles * parts * 128 * 128 * sizeof(float)};
+}
+
 template <bool NK> using ProductBig = TileCfg<256, 256, 2, 4, 32, 4, false, NK>;
 template <bool NK> using ProductBigHalf = TileCfg<128, 256, 2, 4, 32, 4, false, NK>;
 template <bool NK> using ProductSmall = TileCfg<128, 128, 2, 2, 64, 4, false, NK>;
@@ -669,9 +741,23 @@ static long product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, 
 // Beyond, the tile whose rounds take less: a 256 x 256 tile takes 1.96 us for 64 values of the sum, a 128 x 128 tile 0.70, all compute units at
 // work (2048 x 1536, 32 experts, 4096 rows: forward 65 us large, 71 small; dX 84 large, 65 small).
 template <bool GRAD_X>
-static int launch_product(tl_ctx* ctx, ProductParams& p, hipStream_t s) {
+static int launch_product(tl_ctx* ctx, ProductParams& p, void* workspace, hipStream_t s) {
   const int ndim = GRAD_X ? p.K : p.N;
-  if (p.max_rows <= 48L * p.E) {
+  const ProductCut cut = product_cut(ctx, GRAD_X, p.max_rows, p.K, p.N, p.E);
+  if (cut.parts > 1) {
+    p.group_m = 4;
+    p.parts = cut.parts;
+    p.most = cut.tiles;
+    p.k_units = ceil_div(GRAD_X ? p.N : p.K, kPartUnit);
+    p.partial = (float*)workspace;
+    p.nbn = ceil_div(ndim, 128);
+    typedef ProductSmall<GRAD_X> Cfg;
+    if (int e = launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X, true>, p, ctx->num_cus, s)) return e;
+    hipLaunchKernelGGL((moe_product_join_kernel<128, 128, GRAD_X>), dim3(ctx->num_cus), dim3(256), 0, s, p, ctx->num_cus);
+    TL_HIP(hipGetLastError());
+    return TL_OK;
+  }
+  if (p.max_rows <= kFewMean * p.E) {
     // Blocks of twice the columns, one for every wave, where they make a wave for every compute unit (31 experts of 2048 x 1536: 41 us against 44.7);
     // else the narrow ones, with two or four waves for the summed axis (7 of 4096 x 2048: 26 us against 39 with one; a single one
     // of 4096 x 4096: 19 us against 21 with two).
@@ -684,11 +770,11 @@ static int launch_product(tl_ctx* ctx, ProductParams& p, hipStream_t s) {
   if (0.70 * product_rounds(ctx, p, ndim, 128) < 1.96 * product_rounds(ctx, p, ndim, 256)) {
     p.nbn = ceil_div(ndim, 128);
     typedef ProductSmall<GRAD_X> Cfg;
-    return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X>, p, ctx->num_cus, s);
+    return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X, false>, p, ctx->num_cus, s);
   }
   p.nbn = ceil_div(ndim, 256);
   typedef ProductBig<GRAD_X> Cfg;
-  return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductBigHalf<GRAD_X>, GRAD_X>, p, ctx->num_cus, s);
+  return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductBigHalf<GRAD_X>, GRAD_X, false>, p, ctx->num_cus, s);
 }
 
 template <class Cfg, class Out>
@@ -715,7 +801,8 @@ int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, in
   if (way != TL_MOE_FORWARD && way != TL_MOE_GRAD_X && way != TL_MOE_GRAD_W) return fail(TL_ERR_INVALID_ARG, "tl_moe_gemm_query: %d is not one of the three products", way);
   if (int e = check_product("tl_moe_gemm_query", max_rows, K, N, E)) return e;
   if (way == TL_MOE_GRAD_W && (long)E * ceil_div(K, 128) * ceil_div(N, 128) >= (1L << 22)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_moe_gemm_query: E*K*N has 2^22 tiles or more");
-  *ws_bytes = way == TL_MOE_GRAD_W ? grad_w_shape(ctx, max_rows, K, N, E).ws_bytes : 256;
+  if (way == TL_MOE_GRAD_W) *ws_bytes = grad_w_shape(ctx, max_rows, K, N, E).ws_bytes;
+  else *ws_bytes = 256 + product_cut(ctx, way == TL_MOE_GRAD_X, max_rows, K, N, E).bytes;
   return TL_OK;
 }
 
@@ -726,7 +813,7 @@ int tl_moe_gemm(tl_ctx* ctx, const void* x, const void* w, const int* expert_off
   memset(&p, 0, sizeof p);
   p.x = (const bf16_t*)x; p.w = (const bf16_t*)w; p.out = (bf16_t*)y; p.offsets = expert_offsets;
   p.max_rows = max_rows; p.K = K; p.N = N; p.E = E;
-  return launch_product<false>(ctx, p, (hipStream_t)stream);
+  return launch_product<false>(ctx, p, workspace, (hipStream_t)stream);
 }
 
 int tl_moe_gemm_grad_x(tl_ctx* ctx, const void* dy, const void* w, const int* expert_offsets, int max_rows, int K, int N, int E, void* dx, void* workspace,
@@ -736,7 +823,7 @@ int tl_moe_gemm_grad_x(tl_ctx* ctx, const void* dy, const void* w, const int* ex
   memset(&p, 0, sizeof p);
   p.dy = (const bf16_t*)dy; p.w = (const bf16_t*)w; p.out = (bf16_t*)dx; p.offsets = expert_offsets;
   p.max_rows = max_rows; p.K = K; p.N = N; p.E = E;
-  return launch_product<true>(ctx, p, (hipStream_t)stream);
+  return launch_product<true>(ctx, p, workspace, (hipStream_t)stream);
 }
 
 int tl_moe_gemm_grad_w(tl_ctx* ctx, const void* x, const void* dy, const int* expert_offsets, int max_rows, int K, int N, int E, const float* dw_add, void* dw,

@@ -60,7 +60,9 @@ def to_bf16(a):
 COUNTS = [([1], 8, 8, 0, 0), ([0], 16, 24, 0, 3), ([1, 0, 2], 72, 40, 0, 1), ([5, 0, 0, 64, 1], 136, 264, 2, 2), ([65, 63, 7], 256, 520, 0, 0),
           ([129, 127, 128], 512, 128, 0, 0), ([300, 0, 257], 264, 1032, 0, 5), ([256] * 3, 1000, 256, 1, 0), ([1] * 70, 64, 72, 0, 0), ([3, 1] * 128, 32, 16, 0, 0),
           ([700, 11], 40, 2056, 0, 0), ([1100], 776, 8, 0, 0), ([0, 0, 33], 2056, 96, 0, 0), ([2500, 3, 900, 0, 1], 264, 520, 0, 7),
-          ([257, 2049, 255], 1288, 2072, 0, 0)]
+          ([257, 2049, 255], 1288, 2072, 0, 0),
+          # few tiles, long sums: cut
+          ([1], 4104, 136, 0, 2), ([0, 130, 3], 2120, 264, 1, 0), ([70, 1], 264, 4168, 0, 0), ([200, 9], 136, 2120, 0, 3), ([3], 1000, 8200, 0, 0)]
 
 
 def ints(seed):
@@ -89,7 +91,7 @@ def slack(n, size):
 
 # the large tiles (whole and with edges), a few rows of many experts against much of K, long sums into few tiles
 @pytest.mark.parametrize("counts,K,N", [([700, 900, 300, 1000, 20, 0, 513, 400], 1032, 2120), ([2, 0, 1, 16, 17, 3] * 5, 2048, 776), ([3000, 1], 264, 136),
-                                        ([40, 90], 4104, 72)], ids=str)
+                                        ([40, 90], 4104, 72), ([5, 150, 0], 6152, 200), ([150, 30], 200, 6152)], ids=str)
 def test_values(counts, K, N):
     rng = np.random.default_rng(K)
     c = Call(lambda *s: bf16_normal(rng, *s, scale=0.3), counts, K, N)
@@ -126,9 +128,10 @@ def test_gradients_against_differences():
     assert np.array_equal(host(dx), to_bf16(o.products_grad_x(c.dyr, c.wr, c.off)))
 
 
-def test_offsets_that_leave_the_rows_are_cut():
+@pytest.mark.parametrize("K,N", [(64, 72), (2120, 72)])      # a sum in one piece, and cut
+def test_offsets_that_leave_the_rows_are_cut(K, N):
     """Rows from max_rows on are not there, whatever expert_offsets says; the rest is as it would be."""
-    c = Call(ints(5), [100, 50, 60], 64, 72)
+    c = Call(ints(5), [100, 50, 60], K, N)
     c.offd = gpu([0, 100, 150, 1 << 30], I32)
     with Lib() as ctx:
         y, dw = c.forward(ctx), c.grad_w(ctx, c.new_dw())
@@ -138,6 +141,22 @@ def test_offsets_that_leave_the_rows_are_cut():
         y = host(c.forward(ctx))
         assert np.array_equal(y[:90], to_bf16(o.products(c.xr[:100], c.wr[:1], off))[:90])
         assert not host(c.grad_w(ctx, c.new_dw()))[1].any()
+
+
+def test_experts_whose_rows_overlap_stay_inside_workspace_and_results():
+    """More tiles than there can be: what does not fit the workspace is left out, nothing is written beside it."""
+    c = Call(ints(6), [300], 4104, 136)
+    E, n = 16, tl.tl_moe_gemm_query
+    w = torch.zeros(E, 4104, 136, dtype=BF16, device="cuda")
+    off = gpu([0, 300] * 8 + [0], I32)
+    with Lib() as ctx:
+        need = n(ctx, FORWARD, 300, 4104, 136, E)
+        assert need > 256                                   # (a cut sum)
+        ws = torch.full((need // 4 + 1024,), -1, dtype=I32, device="cuda")
+        y = torch.full((301, 136), LEFT, dtype=BF16, device="cuda")
+        tl.tl_moe_gemm(ctx, c.x, w, off, 300, 4104, 136, E, y, ws, need)
+        torch.cuda.synchronize()
+        assert (ws[need // 4:] == -1).all() and (host(y)[300] == LEFT).all()
 
 
 def test_one_workspace_for_all():
