@@ -732,7 +732,7 @@ static int launch_few(ProductParams& p, int ndim, hipStream_t s) {
 // Rounds of tiles of `tile` rows and columns.  The host knows all rows, not the experts': whole tiles, and one that is partly filled for more
 // than every other expert.
 static long product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, int tile) {
-  const double tiles = (ceil_div(p.max_rows, tile) + 0.6 * (p.E - 1)) * ceil_div(ndim, tile);
+  const double tiles = (((long)p.max_rows + tile - 1) / tile + 0.6 * (p.E - 1)) * ceil_div(ndim, tile);
   return (long)(tiles / ctx->num_cus) + 1;
 }
 

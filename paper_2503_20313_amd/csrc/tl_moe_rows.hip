@@ -488,7 +488,7 @@ int tl_moe_sort(tl_ctx* ctx, const int* topk_ids, int T, int topk, int first_exp
   if (int e = check_ctx(ctx)) return e;
   size_t need;
   if (int e = check_sort("tl_moe_sort", T, topk, E)) return e;
-  if (first_expert < 0) return fail(TL_ERR_INVALID_ARG, "tl_moe_sort: first_expert must not be negative");
+  if (first_expert < 0 || (long)first_expert + E > (1L << 31)) return fail(TL_ERR_INVALID_ARG, "tl_moe_sort: first_expert must not be negative, nor the last expert beyond 2^31 - 1");
   if (!topk_ids || !expert_offsets || !sorted_row || !row_pos || !workspace) return fail(TL_ERR_INVALID_ARG, "tl_moe_sort: null pointer argument");
   if (!aligned4(topk_ids) || !aligned4(expert_offsets) || !aligned4(sorted_row) || !aligned4(row_pos) || !aligned4(workspace))
     return fail(TL_ERR_INVALID_ARG, "tl_moe_sort: pointers must be 4-byte aligned");

@@ -75,7 +75,7 @@ def test_sizes_are_positive(ctx, name, arg):
 
 
 @pytest.mark.parametrize("name,status,text,change", [
-    ("sort", ARG, "first_expert", dict(first_expert=-1)), ("sort", SHAPE, "256", dict(E=257)), ("sort", SHAPE, "32", dict(topk=33)),
+    ("sort", ARG, "first_expert", dict(first_expert=-1)), ("sort", ARG, "first_expert", dict(first_expert=(1 << 31) - 7)), ("sort", SHAPE, "256", dict(E=257)), ("sort", SHAPE, "32", dict(topk=33)),
     ("sort", SHAPE, "2^20", dict(T=(1 << 20) // 3 + 1)), ("sort", SHAPE, "31 bits", dict(T=1 << 30)),
     ("route_grad", SHAPE, "256", dict(E=257)), ("route_grad", SHAPE, "topk <= E", dict(topk=9)), ("route_grad", SHAPE, "2^24", dict(T=(1 << 24) + 1)),
     ("grad_w", ARG, "fp32", dict(dw_f32=0)),
@@ -109,6 +109,7 @@ def test_workspaces(ctx):
 
 def test_right_calls_at_the_limits(ctx):
     refused(ARG, "tl_ctx_create_host", CALLS["sort"](T=1 << 15, topk=32, E=256), ctx)
+    refused(ARG, "tl_ctx_create_host", CALLS["sort"](first_expert=(1 << 31) - 8, E=8), ctx)
     refused(ARG, "tl_ctx_create_host", CALLS["route_grad"](T=1 << 24, E=256, topk=32), ctx)
     refused(ARG, "tl_ctx_create_host", CALLS["dispatch"](T=(1 << 26) - 1, topk=32, H=8, max_rows=(1 << 31) - 1), ctx)
     refused(ARG, "tl_ctx_create_host", CALLS["grad_w"](dw_add=None, dw_f32=0), ctx)
