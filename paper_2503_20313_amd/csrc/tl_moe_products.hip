@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const Gra
   auto parts_of = [&](int m) { return max(min((int)(((unsigned)max(m, 0) + (chunk - 1)) / chunk), kMaxParts), 1); };     // (both below 2^31)
   s_by_rank[tid] = -1;
   // Many rounds of items: those of more than 1.5 times the mean first, the others as they come, so that some workgroups store while others
-  // multiply (64 gradients of 2048 x 1536 over 256 rows each in the mean 190 us longest first, 179 so); what the last round is then left
+  // multiply (64 gradients of 2048 x 1536 over 256 rows each in the mean 190 us longest first, 179 so, before the dies took turns); what the last round is then left
   // with weighs little.
   const bool cut_any = __syncthreads_or(parts_of(n) > 1);
   if (!cut_any && (long)p.E * per >= 4L * g.share_of) {
@@ -569,8 +569,11 @@ template <class Cfg, class Out>
 __global__ void __launch_bounds__(Cfg::NTHREADS, Cfg::LDS_BYTES <= 80 * 1024 ? 2 : 1) moe_grad_w_kernel(const GradWParams g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const ProductParams& p = g.p;
-  // runs of g.run items go to one die, which then reads its part of the rows once (32 gradients of 4096 x 1792: 322 us without, 288 with)
-  const int i = blockIdx.x / kXcds, l = ((i / g.run) * kXcds + blockIdx.x % kXcds) * g.run + i % g.run;
+  // Runs of g.run items, a quarter of an expert's, go to one die, which then reads its part of the rows once (32 gradients of 4096 x 1792: 322 us
+  // without, 288 with eighths; quarters 2 to 10 % less where sums are of one length, halves leave dies without work); every other turn in
+  // reverse, or the first die would get the longest item of each (64 gradients of 2048 x 1536: 190 -> 172 us).
+  const int i = blockIdx.x / kXcds, turn = i / g.run, die = blockIdx.x % kXcds;
+  const int l = (turn * kXcds + (turn % 2 ? kXcds - 1 - die : die)) * g.run + i % g.run;
   const u32x4 starts = ((const u32x4*)g.plan->first)[threadIdx.x & 63];
   if (l >= g.plan->n_items) return;
   int start[4];
@@ -695,7 +698,7 @@ static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, in
   // A share is all rows x tiles over the compute units, and no sum is longer than all rows: none is cut where every expert has a tile for every
   // unit.  A cut one of n rows has fewer than 2 n / share parts in each of its tiles, all together fewer than two for every unit.
   s.places = per < cus && max_rows > 2 * kMinPart ? 2 * cus : 0;
-  s.run = (int)min((per + kXcds - 1) / kXcds, 32L);
+  s.run = (int)min((per + 3) / 4, 64L);
   const long span = (long)s.run * kXcds;
   s.grid = (E * per + s.places + span - 1) / span * span;
   auto up = [](size_t b) { return (b + 127) / 128 * 128; };
