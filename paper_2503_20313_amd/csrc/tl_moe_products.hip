@@ -512,6 +512,7 @@ __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const Gra
   __syncthreads();
   int rank = 0;
   long all = 0;
+#pragma unroll 8
   for (int o = 0; o < p.E; o++) {
     const int m = s_n[o];
     rank += m > n || (m == n && o < tid);
@@ -530,6 +531,7 @@ __global__ void __launch_bounds__(kPlanThreads) moe_grad_w_plan_kernel(const Gra
     const int some = (int)min(all * 3 / (2 * p.E), 0x7fffffffL);
     if (n <= some) {
       rank = 0;
+#pragma unroll 8
       for (int o = 0; o < p.E; o++) rank += s_n[o] > some || o < tid;
     }
   }
@@ -733,15 +735,17 @@ static int launch_few(ProductParams& p, int ndim, hipStream_t s) {
 }
 
 // Rounds of tiles of `tile` rows and columns.  The host knows all rows, not the experts': whole tiles, and one that is partly filled for more
-// than every other expert.
-static long product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, int tile) {
-  const double tiles = (((long)p.max_rows + tile - 1) / tile + 0.6 * (p.E - 1)) * ceil_div(ndim, tile);
-  return (long)(tiles / ctx->num_cus) + 1;
+// than every other expert.  A round that is not full takes half of a full one's time and its share of the other half: its tiles have the
+// memory and the chip's power to themselves.
+static double product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, int tile) {
+  const double rounds = (((long)p.max_rows + tile - 1) / tile + 0.6 * (p.E - 1)) * ceil_div(ndim, tile) / ctx->num_cus;
+  const double whole = (double)(long)rounds, rest = rounds - whole;
+  return rounds < 1.0 ? 1.0 : whole + (rest > 0 ? 0.5 + 0.5 * rest : 0.0);
 }
 
 // Up to 48 rows an expert in the mean the few-row kernel: 32 experts of 2048 x 1536 with 32 rows each 43.7 us against 49 (small tiles) and 53 (large),
 // with 64 rows 73 against 53 and 58; 8 of 4096 x 2048 with 40 rows 34 against 45, with 80 rows 61 against 44.
-// Beyond, the tile whose rounds take less: a 256 x 256 tile takes 1.96 us for 64 values of the sum, a 128 x 128 tile 0.70, all compute units at
+// Beyond, the tile whose rounds take less: a 256 x 256 tile takes 1.96 us for 64 values of the sum, a 128 x 128 tile 0.73, all compute units at
 // work (2048 x 1536, 32 experts, 4096 rows: forward 65 us large, 71 small; dX 84 large, 65 small).
 template <bool GRAD_X>
 static int launch_product(tl_ctx* ctx, ProductParams& p, void* workspace, hipStream_t s) {
@@ -770,7 +774,7 @@ static int launch_product(tl_ctx* ctx, ProductParams& p, void* workspace, hipStr
     return launch_few<GRAD_X, false, 4, 1>(p, ndim, s);
   }
   p.group_m = 4;
-  if (0.70 * product_rounds(ctx, p, ndim, 128) < 1.96 * product_rounds(ctx, p, ndim, 256)) {
+  if (0.73 * product_rounds(ctx, p, ndim, 128) < 1.96 * product_rounds(ctx, p, ndim, 256)) {
     p.nbn = ceil_div(ndim, 128);
     typedef ProductSmall<GRAD_X> Cfg;
     return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X, false>, p, ctx->num_cus, s);
