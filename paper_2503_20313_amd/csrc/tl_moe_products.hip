@@ -647,8 +647,9 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
 // ======================================================================================
 constexpr long kFewMean = 48;              // rows of an expert, in the mean, up to which the few-row kernel is taken
 
-// Y's and dX's cut sums: where tiles of 128 x 128, as many as there can be at most, leave three quarters of the compute units without work and the
-// sum is long (a single row through 8192 x 1024 28 -> 13 us, 128 rows of 2 experts of 8192 x 512 45 -> 17, 64 of 4096 x 4096 23 -> 17.5; a sum
+// Y's and dX's cut sums: where tiles of 128 x 128, as many as there can be at most, leave two thirds of the compute units without work and the
+// sum is long (a single row through 8192 x 1024 28 -> 13 us, 128 rows of 2 experts of 8192 x 512 45 -> 17, 64 of 4096 x 4096 23 -> 17.5; three
+// parts, 160 rows of 4 experts of 7168 x 2048 59 -> 31, 1000 of 2 of 8192 x 1024 46 -> 33; two gain and lose alike; a sum
 // of 2048 gains nothing, and dX's few rows, whose weights arrive in whole lines, nothing at 4096: 14 us against 12).  All parts have a unit at
 // least.
 struct ProductCut {
@@ -659,7 +660,7 @@ static ProductCut product_cut(const tl_ctx* ctx, bool grad_x, int max_rows, int 
   const int kdim = grad_x ? N : K, ndim = grad_x ? K : N;
   const long tiles = ((long)max_rows / 128 + min(max_rows, E)) * ceil_div(ndim, 128);
   const long parts = min(ctx->num_cus / tiles, (long)kMaxParts);
-  if (parts < 4 || kdim <= (grad_x && max_rows <= kFewMean * E ? 4096 : 2048)) return {1, 0, 0};
+  if (parts < 3 || kdim <= (grad_x && max_rows <= kFewMean * E ? 4096 : 2048)) return {1, 0, 0};
   return {(int)parts, (int)tiles, (size_t)tiles * parts * 128 * 128 * sizeof(float)};
 }
 
@@ -765,11 +766,15 @@ static int launch_product(tl_ctx* ctx, ProductParams& p, void* workspace, hipStr
     return TL_OK;
   }
   if (p.max_rows <= kFewMean * p.E) {
-    // Blocks of twice the columns, one for every wave, where they make a wave for every compute unit (31 experts of 2048 x 1536: 41 us against 44.7);
-    // else the narrow ones, with two or four waves for the summed axis (7 of 4096 x 2048: 26 us against 39 with one; a single one
-    // of 4096 x 4096: 19 us against 21 with two).
+    // A compute unit takes about 60 GB/s whatever its waves are, and more of them with longer lines, so: the widest units that leave none
+    // with twice the others' share.  Wide ones side by side where there is more than one for each compute unit (31 experts of
+    // 2048 x 1536: 30 us, one a workgroup with two waves for the summed axis 39); one a workgroup, two waves, where there is one for each or for
+    // more than half (320 rows of 8 of 4096 x 4096: 48 us, side by side 76, 16 rows 42 and 52; 64 rows of 6 of 4096 x 3584 37, narrow 54); else
+    // narrow ones, with two or four waves (7 of 4096 x 2048: 26 us against 39 with one; a single one of 4096 x 4096: 19 us against 21 with two).
     const long used = min(p.max_rows, p.E);
-    if (used * ceil_div(ndim, FewShape<GRAD_X, 1, true>::CW) >= ctx->num_cus) return launch_few<GRAD_X, true, 1, 2>(p, ndim, s);
+    const long wide = used * ceil_div(ndim, FewShape<GRAD_X, 1, true>::CW);
+    if (wide > ctx->num_cus) return launch_few<GRAD_X, true, 1, 2>(p, ndim, s);
+    if (wide * 2 > ctx->num_cus) return launch_few<GRAD_X, true, 2, 1>(p, ndim, s);
     if (used * ceil_div(ndim, FewShape<GRAD_X, 1, false>::CW) * 2 >= ctx->num_cus) return launch_few<GRAD_X, false, 2, 1>(p, ndim, s);
     return launch_few<GRAD_X, false, 4, 1>(p, ndim, s);
   }

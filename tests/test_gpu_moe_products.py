@@ -62,7 +62,9 @@ COUNTS = [([1], 8, 8, 0, 0), ([0], 16, 24, 0, 3), ([1, 0, 2], 72, 40, 0, 1), ([5
           ([700, 11], 40, 2056, 0, 0), ([1100], 776, 8, 0, 0), ([0, 0, 33], 2056, 96, 0, 0), ([2500, 3, 900, 0, 1], 264, 520, 0, 7),
           ([257, 2049, 255], 1288, 2072, 0, 0),
           # few tiles, long sums: cut
-          ([1], 4104, 136, 0, 2), ([0, 130, 3], 2120, 264, 1, 0), ([70, 1], 264, 4168, 0, 0), ([200, 9], 136, 2120, 0, 3), ([3], 1000, 8200, 0, 0)]
+          ([1], 4104, 136, 0, 2), ([0, 130, 3], 2120, 264, 1, 0), ([70, 1], 264, 4168, 0, 0), ([200, 9], 136, 2120, 0, 3), ([3], 1000, 8200, 0, 0), ([100, 0, 59, 1], 2120, 2040, 0, 1),
+          # few rows, a wide block of columns for two waves
+          ([3, 0, 17, 40, 1, 2], 1992, 3208, 1, 0)]
 
 
 def ints(seed):
