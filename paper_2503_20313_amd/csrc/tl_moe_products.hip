@@ -483,8 +483,8 @@ struct GradWExpert {                      // (a 16-byte load)
   unsigned what;                          // expert, parts << 8
   int place;                              // of its first part's sums
 };
-// At the front of the workspace: the experts by their rows, most first, each with the number of its first item.  Items of an expert: part
-// by part, all tiles of each.
+// At the front of the workspace: the experts by their rows, most first (of many rounds only those with many more than the mean), each
+// with the number of its first item.  Items of an expert: part by part, all tiles of each.
 struct GradWPlan {
   int first[kMaxProductExperts];
   GradWExpert expert[kMaxProductExperts];

@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams 
     float w = 0.f;
     if (lane < p.topk) w = p.w[t * p.topk + lane];
     if (lane < kMaxChoices) s_dot[wave][lane] = 0.f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (lane 0 adds to them)
     const u32x4* src = (const u32x4*)p.x + t * p.H8;
     for (int base = 0; base < p.H8; base += 256 * U) {
       const int c0 = base + tid;
