@@ -20,8 +20,7 @@ struct ProductParams {
   float* out32;
   int max_rows, K, N, E;
   int nbm, nbn;            // column blocks; for dW also row blocks of an expert's K x N
-  int parts, k_units;      // Y and dX with a cut sum: parts, units of kPartUnit values,
-  int most;                // tiles that the workspace has room for: all there can be, unless the experts' rows overlap
+  int k_units;             // Y and dX: units of kPartUnit values of a sum that may be cut
   float* partial;
   int group_m;
 };
@@ -163,7 +162,17 @@ struct ProductTiles {
   }
 };
 
-// CUT: the summed axis is cut into p.parts parts, whose sums go to the workspace (place tile * parts + part) for the join kernel.
+// The tiles of the last round, where they would leave half the workgroups or more without one: their sums are cut, into as many
+// parts as there are workgroups for each.  Parts go to the workspace (place (tile - first) * parts + part), the join kernel adds them up in their order.
+struct ProductRest {
+  int first, n, parts;      // tiles; parts of a sum, 1: uncut
+  __device__ __forceinline__ ProductRest(const ProductParams& p, int n_all, int grid) {
+    n = n_all % grid;
+    first = n_all - n;
+    parts = n > 0 ? min(min(grid / n, kMaxParts), p.k_units) : 1;
+  }
+};
+
 template <class Big, class Half, bool GRAD_X, bool CUT>
 __global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const ProductParams p) {
   static_assert(Big::NTHREADS == Half::NTHREADS && Big::BN == Half::BN && Big::BM == 2 * Half::BM, "the two shapes share workgroup and columns");
@@ -172,17 +181,21 @@ __global__ void __launch_bounds__(Big::NTHREADS) moe_product_kernel(const Produc
   ProductTiles<Big::BM, Big::BN> tiles;
   tiles.init(p, gridDim.x, s_experts);
   const int kdim = GRAD_X ? p.N : p.K, ndim = GRAD_X ? p.K : p.N;
-  if constexpr (CUT) tiles.n_all = min(tiles.n_all, p.most);
-  const int n_items = CUT ? tiles.n_all * p.parts : tiles.n_all;
+  const ProductRest rest(p, tiles.n_all, gridDim.x);
+  const int n_items = CUT ? rest.first + rest.n * rest.parts : tiles.n_all;
   for (int pos = blockIdx.x; pos < n_items; pos += gridDim.x) {
-    const int part = CUT ? pos / tiles.n_all : 0, tile = pos - part * tiles.n_all;
+    int tile = pos, part = 0, k0 = 0, k = kdim;
+    if (CUT && pos >= rest.first) {
+      part = (pos - rest.first) / rest.n;
+      tile = pos - part * rest.n;
+      k0 = part_start(p.k_units, rest.parts, part) * kPartUnit;
+      k = min(part_start(p.k_units, rest.parts, part + 1) * kPartUnit, kdim) - k0;
+    }
     const ProductJob j = tiles.at(tile, ndim);
-    const int k0 = CUT ? part_start(p.k_units, p.parts, part) * kPartUnit : 0;
-    const int k = CUT ? min(part_start(p.k_units, p.parts, part + 1) * kPartUnit, kdim) - k0 : kdim;
     const bf16_t* a = (GRAD_X ? p.dy : p.x) + j.at * kdim + k0;
     const bf16_t* b = p.w + (long)j.e * p.K * p.N + (GRAD_X ? (long)j.col * p.N + k0 : (long)k0 * p.N + j.col);
-    if constexpr (CUT) {
-      const PartRows out{p.partial + ((long)tile * p.parts + part) * (Big::BM * Big::BN), Big::BN};
+    if (CUT && pos >= rest.first && rest.parts > 1) {
+      const PartRows out{p.partial + ((long)(tile - rest.first) * rest.parts + part) * (Big::BM * Big::BN), Big::BN};
       if (j.big) gemm_tile<Big>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
       else gemm_tile<Half>(a, kdim, nullptr, 1, b, p.N, out, j.rows, j.cols, k, smem);
     } else {
@@ -217,15 +230,16 @@ __global__ void __launch_bounds__(256) moe_product_join_kernel(const ProductPara
   __shared__ int s_experts[3][kMaxProductExperts];
   ProductTiles<BM, BN> tiles;
   tiles.init(p, grid, s_experts);
-  tiles.n_all = min(tiles.n_all, p.most);
+  const ProductRest rest(p, tiles.n_all, grid);
+  if (rest.parts == 1) return;
   const int ndim = GRAD_X ? p.K : p.N;
   constexpr int kSlices = BM * BN / 8 / 256;
-  for (int i = blockIdx.x; i < tiles.n_all * kSlices; i += gridDim.x) {
-    const int tile = i / kSlices, chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (BN / 8), x = chunk % (BN / 8) * 8;
+  for (int i = blockIdx.x; i < rest.n * kSlices; i += gridDim.x) {
+    const int tile = rest.first + i / kSlices, chunk = i % kSlices * 256 + threadIdx.x, y = chunk / (BN / 8), x = chunk % (BN / 8) * 8;
     const ProductJob j = tiles.at(tile, ndim);
     if (y >= j.rows || x >= j.cols) continue;
     float o[8];
-    join_parts(p.partial + (long)tile * p.parts * (BM * BN) + y * BN + x, BM * BN, p.parts, o);
+    join_parts(p.partial + (long)(tile - rest.first) * rest.parts * (BM * BN) + y * BN + x, BM * BN, rest.parts, o);
     *(u32x4*)(p.out + (j.at + y) * ndim + j.col + x) = pack_bf16x8(o);
   }
 }
@@ -645,23 +659,56 @@ __global__ void __launch_bounds__(256) moe_grad_w_join_kernel(const GradWParams 
 // ======================================================================================
 // Host side
 // ======================================================================================
-constexpr long kFewMean = 48;              // rows of an expert, in the mean, up to which the few-row kernel is taken
-
-// Y's and dX's cut sums: where tiles of 128 x 128, as many as there can be at most, leave two thirds of the compute units without work and the
-// sum is long (a single row through 8192 x 1024 28 -> 13 us, 128 rows of 2 experts of 8192 x 512 45 -> 17, 64 of 4096 x 4096 23 -> 17.5; three
-// parts, 160 rows of 4 experts of 7168 x 2048 59 -> 31, 1000 of 2 of 8192 x 1024 46 -> 33; two gain and lose alike; a sum
-// of 2048 gains nothing, and dX's few rows, whose weights arrive in whole lines, nothing at 4096: 14 us against 12).  All parts have a unit at
-// least.
-struct ProductCut {
-  int parts, tiles;
-  size_t bytes;
+// Which kernel Y and dX take, by all rows; how they fall to the experts is known on the device only.  Times below are of even rows and of uneven
+// ones (shares exp(0.7 gauss), one expert without).
+//
+// The few-row kernel takes a wide unit (128 columns; dX 64) of up to 64 rows at the speed of a compute unit's loads, so rows beyond 64 of an
+// expert cost a whole unit more.  With more than a unit for each compute unit it is taken up to 48 rows an expert in the mean (32 experts
+// of 2048 x 1536 with 40 rows: 42 and 42 us, tiles 50 and 50), dX, whose tiles load less, up to 32 (with 40 rows 40 and 56, tiles 45 and 45).  With
+// fewer units tiles need one round, too: with a sum up to 2048 Y gains nothing from it beyond 4 rows (8 of 1024 x 4096 with 12 rows 15 and 16 us, tiles 15
+// and 15; with 40 rows 17 and 26, tiles 16 and 18; but a single row through 2048 x 2048 8.8, tiles 11.6), with a longer one up to 32 rows (8 of 4096 x 2048 with 24 rows 31 and 29, tiles 38 and 37; with 40 33
+// and 60, tiles 39 and 36), dX up to 48.  Not where few tiles of 128 x 128 share a long sum, which is then cut: a single row through 8192 x 1024 28 ->
+// 13 us, 128 rows of 2 experts of 8192 x 512 45 -> 17, 160 of 4 of 7168 x 2048 59 -> 31; dX's few rows, whose weights arrive in whole lines, gain
+// nothing at 4096.
+//
+// Otherwise tiles of 256 or of 128, the last round's sums cut or not, whichever takes less by this model, in us: a round of large tiles takes 1.6
+// for 64 values of the sum, one of small ones 0.65; a last round that is not full half of that and its share of the other half, for its
+// tiles have the memory and the chip's power to themselves; a cut one its part; the join of large tiles' parts 35, of small ones' 10.  Cut only
+// sums beyond 2048: of the shorter ones as many lose by the join's launch, 3 us of 100, as gain.  8 experts of 4096 x 2048 with 2048 rows each
+// 270 -> 243 us, dX of 8 of 4096 x 14336 with 512 rows 696 -> 488, 2 of 4096 x 4096 with 2048 150 -> 122.  Over 460 calls of 96 to 4096 rows an
+// expert the choice takes 2 % more than the best of the four.
+constexpr int kCutSum = 2048;
+struct ProductShape {
+  int tile;                // 0: the few-row kernel
+  bool cut;
+  size_t ws_bytes;
 };
-static ProductCut product_cut(const tl_ctx* ctx, bool grad_x, int max_rows, int K, int N, int E) {
+// Rounds of tiles: whole ones, and one that is partly filled for more than every other expert.
+static double product_rounds(const tl_ctx* ctx, int max_rows, int E, int ndim, int tile, bool cut) {
+  const double rounds = (((long)max_rows + tile - 1) / tile + 0.6 * (min(max_rows, E) - 1)) * ceil_div(ndim, tile) / ctx->num_cus;
+  const double whole = (double)(long)rounds, rest = rounds - whole;
+  if (rest <= 0) return whole;
+  if (cut && rest <= 0.5) return whole + 1.0 / (rest * kMaxParts < 1 ? kMaxParts : (int)(1 / rest));
+  return whole < 1 && !cut ? 1.0 : whole + 0.5 + 0.5 * rest;
+}
+static ProductShape product_shape(const tl_ctx* ctx, bool grad_x, int max_rows, int K, int N, int E) {
   const int kdim = grad_x ? N : K, ndim = grad_x ? K : N;
-  const long tiles = ((long)max_rows / 128 + min(max_rows, E)) * ceil_div(ndim, 128);
-  const long parts = min(ctx->num_cus / tiles, (long)kMaxParts);
-  if (parts < 3 || kdim <= (grad_x && max_rows <= kFewMean * E ? 4096 : 2048)) return {1, 0, 0};
-  return {(int)parts, (int)tiles, (size_t)tiles * parts * 128 * 128 * sizeof(float)};
+  const long used = min(max_rows, E), units = used * ceil_div(ndim, grad_x ? 64 : 128);
+  const long mean = units > ctx->num_cus ? (grad_x ? 32 : 48) : grad_x ? 48 : kdim <= 2048 ? 4 : 32;
+  const bool long_sum = 3 * ((long)max_rows / 128 + used) * ceil_div(ndim, 128) <= ctx->num_cus && kdim > (grad_x ? 4096 : 2048);
+  if (max_rows <= mean * E && !long_sum) return {0, false, 256};
+  ProductShape s = {};
+  double least = 0;
+  for (int tile = 128; tile <= 256; tile += 128)
+    for (int cut = 0; cut <= (kdim > kCutSum); cut++) {
+      const double us = kdim / 64.0 * (tile == 128 ? 0.65 : 1.6) * product_rounds(ctx, max_rows, E, ndim, tile, cut) + (!cut ? 0 : tile == 128 ? 10 : 35);
+      if (s.tile && us >= least) continue;
+      least = us;
+      s.tile = tile;
+      s.cut = cut;
+    }
+  s.ws_bytes = 256 + (s.cut ? (size_t)ctx->num_cus * s.tile * s.tile * sizeof(float) : 0);
+  return s;
 }
 
 template <bool NK> using ProductBig = TileCfg<256, 256, 2, 4, 32, 4, false, NK>;
@@ -735,58 +782,37 @@ static int launch_few(ProductParams& p, int ndim, hipStream_t s) {
   return TL_OK;
 }
 
-// Rounds of tiles of `tile` rows and columns.  The host knows all rows, not the experts': whole tiles, and one that is partly filled for more
-// than every other expert.  A round that is not full takes half of a full one's time and its share of the other half: its tiles have the
-// memory and the chip's power to themselves.
-static double product_rounds(const tl_ctx* ctx, const ProductParams& p, int ndim, int tile) {
-  const double rounds = (((long)p.max_rows + tile - 1) / tile + 0.6 * (p.E - 1)) * ceil_div(ndim, tile) / ctx->num_cus;
-  const double whole = (double)(long)rounds, rest = rounds - whole;
-  return rounds < 1.0 ? 1.0 : whole + (rest > 0 ? 0.5 + 0.5 * rest : 0.0);
+template <class Big, class Half, bool GRAD_X>
+static int launch_tiles(tl_ctx* ctx, ProductParams& p, bool cut, int ndim, hipStream_t s) {
+  p.nbn = ceil_div(ndim, Big::BN);
+  if (!cut) return launch_fused<Big>(moe_product_kernel<Big, Half, GRAD_X, false>, p, ctx->num_cus, s);
+  if (int e = launch_fused<Big>(moe_product_kernel<Big, Half, GRAD_X, true>, p, ctx->num_cus, s)) return e;
+  hipLaunchKernelGGL((moe_product_join_kernel<Big::BM, Big::BN, GRAD_X>), dim3(ctx->num_cus), dim3(256), 0, s, p, ctx->num_cus);
+  TL_HIP(hipGetLastError());
+  return TL_OK;
 }
 
-// Up to 48 rows an expert in the mean the few-row kernel: 32 experts of 2048 x 1536 with 32 rows each 43.7 us against 49 (small tiles) and 53 (large),
-// with 64 rows 73 against 53 and 58; 8 of 4096 x 2048 with 40 rows 34 against 45, with 80 rows 61 against 44.
-// Beyond, the tile whose rounds take less: a 256 x 256 tile takes 1.96 us for 64 values of the sum, a 128 x 128 tile 0.73, all compute units at
-// work (2048 x 1536, 32 experts, 4096 rows: forward 65 us large, 71 small; dX 84 large, 65 small).
 template <bool GRAD_X>
 static int launch_product(tl_ctx* ctx, ProductParams& p, void* workspace, hipStream_t s) {
   const int ndim = GRAD_X ? p.K : p.N;
-  const ProductCut cut = product_cut(ctx, GRAD_X, p.max_rows, p.K, p.N, p.E);
-  if (cut.parts > 1) {
-    p.group_m = 4;
-    p.parts = cut.parts;
-    p.most = cut.tiles;
-    p.k_units = ceil_div(GRAD_X ? p.N : p.K, kPartUnit);
-    p.partial = (float*)workspace;
-    p.nbn = ceil_div(ndim, 128);
-    typedef ProductSmall<GRAD_X> Cfg;
-    if (int e = launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X, true>, p, ctx->num_cus, s)) return e;
-    hipLaunchKernelGGL((moe_product_join_kernel<128, 128, GRAD_X>), dim3(ctx->num_cus), dim3(256), 0, s, p, ctx->num_cus);
-    TL_HIP(hipGetLastError());
-    return TL_OK;
-  }
-  if (p.max_rows <= kFewMean * p.E) {
+  const ProductShape shape = product_shape(ctx, GRAD_X, p.max_rows, p.K, p.N, p.E);
+  if (!shape.tile) {
     // A compute unit takes about 60 GB/s whatever its waves are, and more of them with longer lines, so: the widest units that leave none
     // with twice the others' share.  Wide ones side by side where there is more than one for each compute unit (31 experts of
     // 2048 x 1536: 30 us, one a workgroup with two waves for the summed axis 39); one a workgroup, two waves, where there is one for each or for
     // more than half (320 rows of 8 of 4096 x 4096: 48 us, side by side 76, 16 rows 42 and 52; 64 rows of 6 of 4096 x 3584 37, narrow 54); else
     // narrow ones, with two or four waves (7 of 4096 x 2048: 26 us against 39 with one; a single one of 4096 x 4096: 19 us against 21 with two).
-    const long used = min(p.max_rows, p.E);
-    const long wide = used * ceil_div(ndim, FewShape<GRAD_X, 1, true>::CW);
+    const long used = min(p.max_rows, p.E), wide = used * ceil_div(ndim, FewShape<GRAD_X, 1, true>::CW);
     if (wide > ctx->num_cus) return launch_few<GRAD_X, true, 1, 2>(p, ndim, s);
     if (wide * 2 > ctx->num_cus) return launch_few<GRAD_X, true, 2, 1>(p, ndim, s);
     if (used * ceil_div(ndim, FewShape<GRAD_X, 1, false>::CW) * 2 >= ctx->num_cus) return launch_few<GRAD_X, false, 2, 1>(p, ndim, s);
     return launch_few<GRAD_X, false, 4, 1>(p, ndim, s);
   }
   p.group_m = 4;
-  if (0.73 * product_rounds(ctx, p, ndim, 128) < 1.96 * product_rounds(ctx, p, ndim, 256)) {
-    p.nbn = ceil_div(ndim, 128);
-    typedef ProductSmall<GRAD_X> Cfg;
-    return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductSmallHalf<GRAD_X>, GRAD_X, false>, p, ctx->num_cus, s);
-  }
-  p.nbn = ceil_div(ndim, 256);
-  typedef ProductBig<GRAD_X> Cfg;
-  return launch_fused<Cfg>(moe_product_kernel<Cfg, ProductBigHalf<GRAD_X>, GRAD_X, false>, p, ctx->num_cus, s);
+  p.k_units = ceil_div(GRAD_X ? p.N : p.K, kPartUnit);
+  p.partial = (float*)workspace;
+  if (shape.tile == 128) return launch_tiles<ProductSmall<GRAD_X>, ProductSmallHalf<GRAD_X>, GRAD_X>(ctx, p, shape.cut, ndim, s);
+  return launch_tiles<ProductBig<GRAD_X>, ProductBigHalf<GRAD_X>, GRAD_X>(ctx, p, shape.cut, ndim, s);
 }
 
 template <class Cfg, class Out>
@@ -814,7 +840,7 @@ int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, in
   if (int e = check_product("tl_moe_gemm_query", max_rows, K, N, E)) return e;
   if (way == TL_MOE_GRAD_W && (long)E * ceil_div(K, 128) * ceil_div(N, 128) >= (1L << 22)) return fail(TL_ERR_UNSUPPORTED_SHAPE, "tl_moe_gemm_query: E*K*N has 2^22 tiles or more");
   if (way == TL_MOE_GRAD_W) *ws_bytes = grad_w_shape(ctx, max_rows, K, N, E).ws_bytes;
-  else *ws_bytes = 256 + product_cut(ctx, way == TL_MOE_GRAD_X, max_rows, K, N, E).bytes;
+  else *ws_bytes = product_shape(ctx, way == TL_MOE_GRAD_X, max_rows, K, N, E).ws_bytes;
   return TL_OK;
 }
 

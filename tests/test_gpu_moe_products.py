@@ -145,8 +145,24 @@ def test_offsets_that_leave_the_rows_are_cut(K, N):
         assert not host(c.grad_w(ctx, c.new_dw()))[1].any()
 
 
+# a round and a few tiles, small and large, of which some are whole, half, and at an edge; no whole round; a round of small ones and a bit
+@pytest.mark.parametrize("counts,K,N", [([2000, 0, 60, 197], 4104, 2056), ([7000, 3, 400], 4104, 2056), ([3, 300, 120], 6152, 264), ([4100, 70], 4104, 1032)], ids=str)
+def test_last_round_is_cut(counts, K, N):
+    """Whole numbers, against products in fp32, which are exact; dX of the matrices the other way round."""
+    with Lib() as ctx:
+        for way, c in ((FORWARD, Call(ints(K), counts, K, N, 1, 2)), (GRAD_X, Call(ints(N), counts, N, K, 1, 2))):
+            assert tl.tl_moe_gemm_query(ctx, way, *c.sizes()[1:]) > 256          # (room for parts)
+            got, again = [c.forward(ctx) if way == FORWARD else c.grad_x(ctx) for _ in range(2)]
+            ref = torch.full_like(got, LEFT)
+            for e in range(c.E):
+                lo, hi = int(c.off[e]), int(c.off[e + 1])
+                w = c.w[e].float()
+                ref[lo:hi] = (c.x[lo:hi].float() @ w if way == FORWARD else c.dy[lo:hi].float() @ w.T.contiguous()).to(BF16)
+            assert torch.equal(got, ref) and torch.equal(got, again)
+
+
 def test_experts_whose_rows_overlap_stay_inside_workspace_and_results():
-    """More tiles than there can be: what does not fit the workspace is left out, nothing is written beside it."""
+    """More tiles than there can be: nothing is written beside workspace and results."""
     c = Call(ints(6), [300], 4104, 136)
     E, n = 16, tl.tl_moe_gemm_query
     w = torch.zeros(E, 4104, 136, dtype=BF16, device="cuda")
