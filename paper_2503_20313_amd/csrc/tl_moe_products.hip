@@ -608,13 +608,27 @@ __global__ void __launch_bounds__(Cfg::NTHREADS, Cfg::LDS_BYTES <= 80 * 1024 ? 2
   Out out;
   if constexpr (StoresF32<Out>::value) out = Out{p.add ? p.add + at : nullptr, p.out32 + at, p.N};
   else out = Out{p.out + at, p.N};
-  if (n == 0) {     // an expert without rows
-    for (int c = threadIdx.x; c < rows * (cols / 8); c += Cfg::NTHREADS) {
-      const int y = c / (cols / 8), x = (c - y * (cols / 8)) * 8;
-      if constexpr (StoresF32<Out>::value) {
-        out.store4(y, x, out.load4(y, x));
-        out.store4(y, x + 4, out.load4(y, x + 4));
-      } else {
+  if (n == 0) {     // an expert without rows: zeros, or what there was (whole lines, four
+                    // of them in flight: 32 experts of 2048 x 1536, 24 of them without, 308 -> 154 us)
+    if constexpr (StoresF32<Out>::value) {
+      if (p.add == p.out32) return;
+      const int width = cols / 4, pieces = rows * width;
+      for (int c0 = threadIdx.x; c0 < pieces; c0 += 4 * Cfg::NTHREADS) {
+        floatx4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          const int c = c0 + u * Cfg::NTHREADS;
+          if (c < pieces) v[u] = out.load4(c / width, c % width * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          const int c = c0 + u * Cfg::NTHREADS;
+          if (c < pieces) out.store4(c / width, c % width * 4, v[u]);
+        }
+      }
+    } else {
+      for (int c = threadIdx.x; c < rows * (cols / 8); c += Cfg::NTHREADS) {
+        const int y = c / (cols / 8), x = (c - y * (cols / 8)) * 8;
         out.store(y, x, u32x4{0, 0, 0, 0});
       }
     }
@@ -735,19 +749,22 @@ struct GradWShape {
 static GradWShape grad_w_shape(const tl_ctx* ctx, int max_rows, int K, int N, int E) {
   GradWShape s;
   const int cus = min(ctx->num_cus, 1 << 16);
-  // The large tile; the half one, two workgroups a compute unit, where large ones make one to two rounds: they are too coarse for that, and its ends
-  // run beside another's sum (8 gradients of 2048 x 1536 over 114 .. 4701 rows in fp32 145 -> 133 us, 4 of 2048 x 2048 over 512 rows 53 -> 27;
-  // but 8 of 4096 x 2048 over 2048 rows, four rounds, 223 -> 243).  The small one where even the cut sums of large ones would leave compute
-  // units without work (4 of 512 x 512 over 4096 rows: 54.7 us uncut, 37.6).
-  const long tiles = (long)E * ceil_div(K, 256) * ceil_div(N, 256), parts = max(min(max_rows / E / kMinPart, kMaxParts), 1);
-  s.bm = s.bn = tiles * parts < cus ? 128 : 256;
-  if (tiles >= cus && tiles < 2L * cus) s.bm = 128;
+  // By the rounds that tiles of 256 x 256 would make.  Up to 0.6: 128 x 128 (8 experts of 1024 x 1024 over 512 rows 23 us, 128 x 256 24, large 29; over
+  // 2048 47, 57, 73).  Beyond: 128 x 256 with two workgroups a compute unit, whose beginnings and ends run beside another's sum (4 of
+  // 2048 x 2048 over 512 rows 29 us, large 32, small 38; 32 of 2048 x 1536 over 256 rows 73, 81, 118).  Large ones, which need less loaded for a product, where sums
+  // are long, in 2.5 rounds and more (16 of 1024 x 2816 over 1024 rows 100 us, half ones 111; 32 of 2048 x 1536 199 and 212) or cut evenly (one
+  // of 8192 x 1024 over 8192 rows 137, small ones 160).
+  const long tiles = (long)E * ceil_div(K, 256) * ceil_div(N, 256);
+  const bool small = 5 * tiles <= 3L * cus, large = (2 * tiles >= 5L * cus || (small && E == 1)) && tiles * max_rows / E >= 2500L * cus;
+  s.bm = large ? 256 : 128;
+  s.bn = small && !large ? 128 : 256;
   s.nbm = ceil_div(K, s.bm);
   s.nbn = ceil_div(N, s.bn);
   const long per = (long)s.nbm * s.nbn;
   // A share is all rows x tiles over the compute units, and no sum is longer than all rows: none is cut where every expert has a tile for every
   // unit.  A cut one of n rows has fewer than 2 n / share parts in each of its tiles, all together fewer than two for every unit.
-  s.places = per < cus && max_rows > 2 * kMinPart ? 2 * cus : 0;
+  // Nor are sums of fewer than 1536 rows in the mean, where the cut and its join cost more than uneven ones (16 of 1024 x 2816 over 1024 rows 100 us, cut 107).
+  s.places = per < cus && max_rows >= 1536L * E ? 2 * cus : 0;
   s.run = (int)min((per + 3) / 4, 64L);
   const long span = (long)s.run * kXcds;
   s.grid = (E * per + s.places + span - 1) / span * span;

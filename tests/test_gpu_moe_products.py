@@ -79,11 +79,13 @@ def test_whole_numbers_are_exact(counts, K, N, before, behind):
     with Lib() as ctx:
         y, dx, dw, dw32 = c.forward(ctx), c.grad_x(ctx), c.grad_w(ctx, c.new_dw()), c.grad_w(ctx, c.new_dw(F32))
         add, add_ref = torch.full_like(dw32, 3.0), np.full(dw32.shape, 3.0)
-        dw_add = c.grad_w(ctx, add, add)                   # in place
+        dw_add = c.grad_w(ctx, c.new_dw(F32), add)
+        dw_own = c.grad_w(ctx, add, add)                   # in place
     for got, ref in ((y, o.products(c.xr, c.wr, c.off)), (dx, o.products_grad_x(c.dyr, c.wr, c.off))):
         assert np.array_equal(host(got)[c.own], to_bf16(ref[c.own])) and (host(got)[~c.own] == LEFT).all()
     ref = o.products_grad_w(c.xr, c.dyr, c.off)
-    assert np.array_equal(host(dw), to_bf16(ref)) and np.array_equal(host(dw32), ref) and np.array_equal(host(dw_add), ref + add_ref)
+    assert np.array_equal(host(dw), to_bf16(ref)) and np.array_equal(host(dw32), ref)
+    assert np.array_equal(host(dw_add), ref + add_ref) and np.array_equal(host(dw_own), ref + add_ref)
 
 
 def slack(n, size):
@@ -159,6 +161,27 @@ def test_last_round_is_cut(counts, K, N):
                 w = c.w[e].float()
                 ref[lo:hi] = (c.x[lo:hi].float() @ w if way == FORWARD else c.dy[lo:hi].float() @ w.T.contiguous()).to(BF16)
             assert torch.equal(got, ref) and torch.equal(got, again)
+
+
+# tiles of the three shapes, their sums cut and not
+@pytest.mark.parametrize("counts,K,N,cut", [([4700, 0, 220], 264, 520, True), ([3000, 150], 2056, 2056, True), ([14300], 2056, 1032, True), ([700, 0, 1900], 264, 520, False),
+                                            ([900, 150], 2056, 2056, False), ([5000, 3, 0, 700, 2200, 1600, 900, 1500], 2056, 2056, False)], ids=str)
+def test_gradients_of_weights_over_long_sums(counts, K, N, cut):
+    """Whole numbers, against products in fp32, which are exact."""
+    c = Call(ints(K + N), counts, K, N, 1, 2)
+    ref = torch.zeros(c.E, K, N, device="cuda")
+    for e in range(c.E):
+        rows = slice(int(c.off[e]), int(c.off[e + 1]))
+        if counts[e]:
+            ref[e] = c.x[rows].float().T.contiguous() @ c.dy[rows].float()
+    add = torch.arange(K * N, device="cuda").remainder(17).float().reshape(K, N).expand(c.E, K, N).contiguous()
+    with Lib() as ctx:
+        assert (tl.tl_moe_gemm_query(ctx, GRAD_W, *c.sizes()[1:]) > 1 << 20) == cut
+        for _ in range(2):
+            assert torch.equal(c.grad_w(ctx, c.new_dw()), ref.to(BF16)) and torch.equal(c.grad_w(ctx, c.new_dw(F32)), ref)
+            assert torch.equal(c.grad_w(ctx, c.new_dw(F32), add), ref + add)
+        total = ref + add
+        assert torch.equal(c.grad_w(ctx, add, add), total)
 
 
 def test_experts_whose_rows_overlap_stay_inside_workspace_and_results():
