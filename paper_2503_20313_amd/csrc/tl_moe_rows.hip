@@ -269,61 +269,78 @@ __global__ void __launch_bounds__(256) moe_gather_sum_kernel(const RowsParams p)
   }
 }
 
-// dys[row_pos[t, j]] = w[t, j] dout[t], dw[t, j] = <dout[t], ys[row_pos[t, j]]>.  A workgroup takes a token; a row of ys is read
-// before its place is written, by the same lane, so dys may be ys.
-template <int U, bool STREAM_LOADS, bool STREAM_STORES>
+// dys[row_pos[t, j]] = w[t, j] dout[t], dw[t, j] = <dout[t], ys[row_pos[t, j]]>.  WAVES waves take a token, two rows of it at a time, their loads
+// in flight together (8192 tokens of 4096, top-5, 131 us, one row 134, four 132; one token of 7640, top-8, 12.0, 14.3 and 14.6); a row of ys is read before its place
+// is written, by the same lane, so dys may be ys.  Lane j of a wave keeps its share of dw[t, j].  (68
+// registers, seven waves a SIMD; held to 64, eight are spilled: 135 us.)
+template <int WAVES, bool STREAM_LOADS, bool STREAM_STORES>
 __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams p) {
+  constexpr int U = 2, R = 2, STEP = 64 * WAVES;
   __shared__ float s_dot[4][kMaxChoices];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  for (long t = blockIdx.x; t < p.T; t += gridDim.x) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % WAVES;
+  for (long t = (long)blockIdx.x * (4 / WAVES) + wave / WAVES; t < p.T; t += (long)gridDim.x * (4 / WAVES)) {
     int pos;
     const unsigned long long part = places_of(p, t, lane, &pos);
-    float w = 0.f;
+    float w = 0.f, mine = 0.f;
     if (lane < p.topk) w = p.w[t * p.topk + lane];
-    if (lane < kMaxChoices) s_dot[wave][lane] = 0.f;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (lane 0 adds to them)
     const u32x4* src = (const u32x4*)p.x + t * p.H8;
-    for (int base = 0; base < p.H8; base += 256 * U) {
-      const int c0 = base + tid;
+    for (int c0 = share * 64 + lane; c0 - lane < p.H8; c0 += STEP * U) {
       u32x4 g[U];
 #pragma unroll
       for (int u = 0; u < U; u++) {
         g[u] = u32x4{0, 0, 0, 0};
-        if (c0 + u * 256 < p.H8) g[u] = src[c0 + u * 256];
+        if (c0 + u * STEP < p.H8) g[u] = src[c0 + u * STEP];
       }
-      for (unsigned long long left = part; left; left &= left - 1) {
-        const int j = __builtin_ctzll(left);
-        const long row = (long)__builtin_amdgcn_readlane(pos, j) * p.H8;
-        const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
-        const u32x4* y = (const u32x4*)p.ys + row;
-        u32x4* d = (u32x4*)p.dys + row;
-        u32x4 v[U];
+      for (unsigned long long left = part; left;) {
+        u32x4 v[R][U];
+        long row[R];
+        int j[R];
+        float wj[R];
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-          v[u] = u32x4{0, 0, 0, 0};
-          if (c0 + u * 256 < p.H8) v[u] = load_piece<STREAM_LOADS>(y + c0 + u * 256);
-        }
-        float dot = 0.f;
+        for (int q = 0; q < R; q++) {
+          j[q] = -1;
+          if (!left) continue;
+          j[q] = __builtin_ctzll(left);
+          left &= left - 1;
+          row[q] = (long)__builtin_amdgcn_readlane(pos, j[q]) * p.H8;
+          wj[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j[q]));
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-          float o[8];
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float g0 = __uint_as_float(g[u][e] << 16), g1 = __uint_as_float(g[u][e] & 0xffff0000u);
-            dot = __builtin_fmaf(g0, __uint_as_float(v[u][e] << 16), dot);
-            dot = __builtin_fmaf(g1, __uint_as_float(v[u][e] & 0xffff0000u), dot);
-            o[2 * e] = wj * g0;
-            o[2 * e + 1] = wj * g1;
+          for (int u = 0; u < U; u++) {
+            v[q][u] = u32x4{0, 0, 0, 0};
+            if (c0 + u * STEP < p.H8) v[q][u] = load_piece<STREAM_LOADS>((const u32x4*)p.ys + row[q] + c0 + u * STEP);
           }
-          if (c0 + u * 256 < p.H8) store_piece<STREAM_STORES>(d + c0 + u * 256, pack_bf16x8(o));
         }
-        dot = wave_sum(dot);
-        if (lane == 0) s_dot[wave][j] += dot;
+#pragma unroll
+        for (int q = 0; q < R; q++) {
+          if (j[q] < 0) continue;
+          float dot = 0.f;
+#pragma unroll
+          for (int u = 0; u < U; u++) {
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const float g0 = __uint_as_float(g[u][e] << 16), g1 = __uint_as_float(g[u][e] & 0xffff0000u);
+              dot = __builtin_fmaf(g0, __uint_as_float(v[q][u][e] << 16), dot);
+              dot = __builtin_fmaf(g1, __uint_as_float(v[q][u][e] & 0xffff0000u), dot);
+              o[2 * e] = wj[q] * g0;
+              o[2 * e + 1] = wj[q] * g1;
+            }
+            if (c0 + u * STEP < p.H8) store_piece<STREAM_STORES>((u32x4*)p.dys + row[q] + c0 + u * STEP, pack_bf16x8(o));
+          }
+          dot = wave_sum(dot);
+          if (lane == j[q]) mine += dot;
+        }
       }
     }
-    __syncthreads();
-    if (tid < p.topk) p.dw[t * p.topk + tid] = s_dot[0][tid] + s_dot[1][tid] + s_dot[2][tid] + s_dot[3][tid];
-    __syncthreads();
+    if constexpr (WAVES == 1) {
+      if (lane < p.topk) p.dw[t * p.topk + lane] = mine;
+    } else {
+      static_assert(WAVES == 4, "a workgroup to a token");
+      if (lane < kMaxChoices) s_dot[wave][lane] = mine;
+      __syncthreads();
+      if (threadIdx.x < (unsigned)p.topk) p.dw[t * p.topk + threadIdx.x] = s_dot[0][threadIdx.x] + s_dot[1][threadIdx.x] + s_dot[2][threadIdx.x] + s_dot[3][threadIdx.x];
+      __syncthreads();
+    }
   }
 }
 
@@ -455,6 +472,9 @@ static long sorted_bytes(int T, int H, int topk, int max_rows) {
   return (rows < max_rows ? rows : max_rows) * H * 2;
 }
 
+// The gradient of combine: up to here a row is a wave's alone (14000 tokens of 160, top-6: 18 us, 39 with four waves a token; 8192 of 1024, top-5, 37 and 41;
+// 4096 of 2048, top-8, 78 and 56).
+constexpr int kWaveRow = 1024;
 constexpr long kMaxGrid = 1 << 20;     // workgroups; each goes on to further tokens
 static int rows_grid(long waves) { return (int)((waves + 3) / 4 < kMaxGrid ? (waves + 3) / 4 : kMaxGrid); }
 
@@ -583,11 +603,15 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout, const void* ys, const flo
   if (int e = check_op_ctx(ctx)) return e;
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.x = (const bf16_t*)dout; p.ys = (const bf16_t*)ys; p.w = topk_w; p.dys = (bf16_t*)dys; p.dw = dtopk_w;
-  const dim3 grid((int)(p.T < kMaxGrid ? p.T : kMaxGrid));
   const long bytes = sorted_bytes(T, H, topk, max_rows);
-  if (bytes >= kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<2, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
-  else if (bytes > kStreamStores) hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
-  else hipLaunchKernelGGL((moe_combine_grad_kernel<2, false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  auto go = [&](auto waves_c) {
+    constexpr int WAVES = decltype(waves_c)::value;
+    const dim3 grid(rows_grid(p.T * WAVES));
+    if (bytes >= kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    else if (bytes > kStreamStores) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    else hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  };
+  if (H <= kWaveRow) go(std::integral_constant<int, 1>{}); else go(std::integral_constant<int, 4>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
 }

@@ -13,7 +13,8 @@ NAN = float("nan")
 # T, H, topk, experts, ranks, room: one token, rows shorter than a wave's piece and longer than a workgroup's, odd numbers of pieces,
 # ranks that hold a part of the experts, full buffers
 CASES = [(1, 8, 1, 2, 1, 1), (1, 4096, 2, 8, 1, 1), (3, 520, 3, 4, 1, 1), (17, 1032, 5, 8, 4, 1), (64, 2056, 2, 8, 2, 0.7), (33, 4104, 8, 16, 1, 0.5),
-         (5, 8192, 32, 64, 1, 1), (2, 20488, 4, 8, 1, 1), (300, 136, 6, 8, 3, 1), (1000, 64, 2, 4, 1, 0.9), (7, 512, 4, 4, 9, 1)]
+         (5, 8192, 32, 64, 1, 1), (2, 20488, 4, 8, 1, 1), (300, 136, 6, 8, 3, 1), (1000, 64, 2, 4, 1, 0.9), (7, 512, 4, 4, 9, 1),
+         (9, 1024, 7, 16, 1, 0.8), (50, 776, 32, 64, 2, 1)]
 
 
 def setup(T, H, k, E, ranks, room):
