@@ -4,13 +4,9 @@
 // Row (t, j), number t*topk + j, is token t at its j-th expert; row_pos[t, j] is its place in the matrices whose rows are sorted by
 // expert.  A place outside [0, max_rows) takes no part, and nothing is read or written for it: whatever row_pos holds, every
 // access stays inside the matrices.
-#include "tl_host.h"
+#include "tl_moe_choice.h"
 
 namespace tl {
-
-constexpr int kMaxChoices = 32;         // topk
-constexpr int kMaxSortExperts = 256;
-constexpr int kMaxSortRows = 1 << 20;
 
 // Sum over the 64 lanes of a wave, in every lane, always in the same order.
 __device__ __forceinline__ float wave_sum(float x) {
@@ -27,8 +23,6 @@ __device__ __forceinline__ float wave_sum(float x) {
 // Inside a chunk wave w owns a run of 64*RPT rows and walks it 64 rows at a time; the lanes with the same expert are found with one
 // ballot per bit of the expert's number, which gives every row its rank among them.
 // ======================================================================================
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-
 struct SortParams {
   const int* ids;
   int n, first, E;
@@ -463,26 +457,8 @@ static RowsParams rows_params(const int* row_pos, int T, int H, int topk, int ma
   return p;
 }
 
-// From here on sorted rows go past the caches -- counted as all there can be, for how many take part is known on the device only.  Stores: beyond the
-// dies' L2 together (1024 tokens of 4096, top-8, gradients of combine: 33.2 us, streaming stores 24.4).  Loads: beyond the memory's own cache,
-// and beyond half of it in the gradient of combine, whose rows are the forward pass's (16384 tokens of 2048, top-2: 67 us, streaming loads 57).
-constexpr long kStreamStores = 32L << 20, kStreamLoads = 256L << 20;
-static long sorted_bytes(int T, int H, int topk, int max_rows) {
-  const long rows = (long)T * topk;
-  return (rows < max_rows ? rows : max_rows) * H * 2;
-}
-
-// The gradient of combine: up to here a row is a wave's alone (14000 tokens of 160, top-6: 18 us, 39 with four waves a token; 8192 of 1024, top-5, 37 and 41;
-// 4096 of 2048, top-8, 78 and 56).
-constexpr int kWaveRow = 1024;
 constexpr long kMaxGrid = 1 << 20;     // workgroups; each goes on to further tokens
 static int rows_grid(long waves) { return (int)((waves + 3) / 4 < kMaxGrid ? (waves + 3) / 4 : kMaxGrid); }
-
-static int sort_rows_per_thread(long n) {
-  int r = 1;
-  while (r < 8 && (n + (long)kSortThreads * r - 1) / ((long)kSortThreads * r) > 128) r *= 2;
-  return r;
-}
 
 static int check_sort(const char* what, int T, int topk, int E) {
   if (int e = check_tokens(what, T, topk)) return e;
@@ -491,8 +467,6 @@ static int check_sort(const char* what, int T, int topk, int E) {
   if ((long)T * topk > kMaxSortRows) return fail(TL_ERR_UNSUPPORTED_SHAPE, "%s: at most 2^20 rows (got %ld)", what, (long)T * topk);
   return TL_OK;
 }
-
-static int sort_chunks(long n) { const long c = (long)kSortThreads * sort_rows_per_thread(n); return (int)((n + c - 1) / c); }
 
 }  // namespace tl
 
@@ -554,7 +528,7 @@ int tl_moe_dispatch(tl_ctx* ctx, const void* x, const int* row_pos, int T, int H
   p.x = (const bf16_t*)x; p.out = (bf16_t*)xs;
   p.segs = ceil_div(p.H8, 64);
   const dim3 grid(rows_grid(p.T * p.segs));
-  if (sorted_bytes(T, H, topk, max_rows) > kStreamStores) hipLaunchKernelGGL(moe_dispatch_kernel<true>, grid, dim3(256), 0, (hipStream_t)stream, p);
+  if (dispatch_choice(T, H, topk, max_rows).stream_stores) hipLaunchKernelGGL(moe_dispatch_kernel<true>, grid, dim3(256), 0, (hipStream_t)stream, p);
   else hipLaunchKernelGGL(moe_dispatch_kernel<false>, grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
@@ -570,7 +544,7 @@ int tl_moe_dispatch_grad(tl_ctx* ctx, const void* dxs, const int* row_pos, int T
   p.ys = (const bf16_t*)dxs; p.out = (bf16_t*)dx;
   p.segs = ceil_div(p.H8, 64);
   const dim3 grid(rows_grid(p.T * p.segs));
-  if (sorted_bytes(T, H, topk, max_rows) > kStreamLoads) hipLaunchKernelGGL((moe_gather_sum_kernel<false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  if (gather_choice(T, H, topk, max_rows).stream_loads) hipLaunchKernelGGL((moe_gather_sum_kernel<false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
   else hipLaunchKernelGGL((moe_gather_sum_kernel<false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
@@ -587,7 +561,7 @@ int tl_moe_combine(tl_ctx* ctx, const void* ys, const float* topk_w, const int* 
   p.ys = (const bf16_t*)ys; p.w = topk_w; p.add = (const bf16_t*)add; p.out = (bf16_t*)out;
   p.segs = ceil_div(p.H8, 64);
   const dim3 grid(rows_grid(p.T * p.segs));
-  if (sorted_bytes(T, H, topk, max_rows) > kStreamLoads) hipLaunchKernelGGL((moe_gather_sum_kernel<true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+  if (gather_choice(T, H, topk, max_rows).stream_loads) hipLaunchKernelGGL((moe_gather_sum_kernel<true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
   else hipLaunchKernelGGL((moe_gather_sum_kernel<true, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   TL_HIP(hipGetLastError());
   return TL_OK;
@@ -603,15 +577,15 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout, const void* ys, const flo
   if (int e = check_op_ctx(ctx)) return e;
   RowsParams p = rows_params(row_pos, T, H, topk, max_rows);
   p.x = (const bf16_t*)dout; p.ys = (const bf16_t*)ys; p.w = topk_w; p.dys = (bf16_t*)dys; p.dw = dtopk_w;
-  const long bytes = sorted_bytes(T, H, topk, max_rows);
+  const RowsChoice choice = combine_grad_choice(T, H, topk, max_rows);
   auto go = [&](auto waves_c) {
     constexpr int WAVES = decltype(waves_c)::value;
     const dim3 grid(rows_grid(p.T * WAVES));
-    if (bytes >= kStreamLoads / 2) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
-    else if (bytes > kStreamStores) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    if (choice.stream_loads) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, true, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    else if (choice.stream_stores) hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, false, true>), grid, dim3(256), 0, (hipStream_t)stream, p);
     else hipLaunchKernelGGL((moe_combine_grad_kernel<WAVES, false, false>), grid, dim3(256), 0, (hipStream_t)stream, p);
   };
-  if (H <= kWaveRow) go(std::integral_constant<int, 1>{}); else go(std::integral_constant<int, 4>{});
+  if (choice.waves == 1) go(std::integral_constant<int, 1>{}); else go(std::integral_constant<int, 4>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
@@ -636,15 +610,17 @@ int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits, const int* topk_ids
     hipLaunchKernelGGL((moe_route_grad_kernel<LANES, PER>), dim3(ceil_div(T, 256 / LANES)), dim3(256), 0, (hipStream_t)stream, p);
   };
   using std::integral_constant;
-  auto per = [&](auto lanes_c) {      // logits of a lane
+  auto per = [&](auto lanes_c) {
     constexpr int LANES = decltype(lanes_c)::value;
-    if (E <= LANES) go(lanes_c, integral_constant<int, 1>{});
-    else if (E <= 2 * LANES) go(lanes_c, integral_constant<int, 2>{});
-    else if (E <= 4 * LANES) go(lanes_c, integral_constant<int, 4>{});
-    else if (E <= 8 * LANES) go(lanes_c, integral_constant<int, 8>{});
-    else go(lanes_c, integral_constant<int, 256 / LANES>{});
+    switch (route_per(E, LANES)) {
+      case 1: go(lanes_c, integral_constant<int, 1>{}); break;
+      case 2: go(lanes_c, integral_constant<int, 2>{}); break;
+      case 4: go(lanes_c, integral_constant<int, 4>{}); break;
+      case 8: go(lanes_c, integral_constant<int, 8>{}); break;
+      default: go(lanes_c, integral_constant<int, 256 / LANES>{});
+    }
   };
-  if (topk <= 16) per(integral_constant<int, 16>{}); else per(integral_constant<int, 32>{});
+  if (route_lanes(topk) == 16) per(integral_constant<int, 16>{}); else per(integral_constant<int, 32>{});
   TL_HIP(hipGetLastError());
   return TL_OK;
 }
