@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from tests import test_gpu_moe_products_kernels as products
+from tests import test_gpu_moe_rows_streaming as rows
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PKG = os.path.join(ROOT, "paper_2503_20313_amd")
@@ -38,3 +39,12 @@ def test_products(kernels_of):
     assert set(got) == {f"{op} {k}" for op in ("gemm", "gemm_grad_x") for k in few + tiles} | {f"gemm_grad_w {t} {c}" for t in ("128x128", "128x256", "256x256") for c in ("whole", "cut")}
     roomy = kernels_of([(kernel.split()[0], room, K, N, len(counts)) for kernel, counts, K, N, room in products.ROOMY])
     assert roomy == [c[0] for c in products.ROOMY]
+
+
+def test_rows(kernels_of):
+    cases = rows.FORWARD + rows.SUMS + rows.GRADIENTS
+    got = kernels_of([(variant.split()[0], *sizes) for variant, *sizes in cases])
+    assert got == [c[0] for c in cases]
+    loads = ("cached", "stream")
+    assert set(got) == ({f"dispatch cached {s}" for s in loads} | {f"{op} {l} cached" for op in ("dispatch_grad", "combine") for l in loads} |
+                        {f"combine_grad {w} {s}" for w in (1, 4) for s in ("cached cached", "cached stream", "stream stream")})
