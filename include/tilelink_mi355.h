@@ -431,8 +431,9 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout /*dev*/, const void* ys /*
  *   renormalize == 0:  w_j = p_{e_j},  dlogits_i = p_i ( sum_{j: e_j = i} dtopk_w_j - sum_k p_{e_k} dtopk_w_k )
  *   otherwise:         w_j = p_{e_j} / sum_k p_{e_k},  dlogits_i = sum_{j: e_j = i} w_j ( dtopk_w_j - sum_k w_k dtopk_w_k )
  *   gate_logits dev fp32 [T, E], topk_ids dev int[T, topk], dtopk_w dev fp32 [T, topk];  dlogits dev fp32 [T, E] (written; may be gate_logits)
- * An id outside [0, E) is no choice: it has no weight, its dtopk_w is not read.  A logit of -inf has a gradient of zero; so have all of a
- * token whose logits -- whose chosen ones, with renormalize -- are all -inf, which has no weights.  topk <= E <= 256, T <= 2^24. */
+ * An id outside [0, E) is no choice: it has no weight, its dtopk_w is not read.  A logit of -inf is a mask: its gradient is zero, and where it is
+ * chosen its dtopk_w counts for nothing, whatever it holds.  A token whose logits (with renormalize: whose chosen ones) are all -inf has no weights, and
+ * gradients of zero.  topk <= E <= 256, T <= 2^24. */
 int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits /*dev*/, const int* topk_ids /*dev*/, const float* dtopk_w /*dev*/, int T, int E, int topk,
                       int renormalize, float* dlogits /*dev*/, void* stream);
 

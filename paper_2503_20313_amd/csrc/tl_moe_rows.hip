@@ -389,6 +389,7 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
     const float v = __shfl(l[q], lane0 + (id < 0 ? 0 : id % LANES));
     if (id >= 0 && id / LANES == q) chosen = v;
   }
+  if (chosen == -INFINITY) g = 0.f;            // (no weight: 0 times whatever it was given, infinities and NaN too)
   float top;
   if (p.renormalize) top = lanes_max<LANES>(chosen);
   else {
@@ -399,11 +400,14 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
   }
   const bool none = top == -INFINITY;          // no finite logit: no weights, no gradient
   float e[PER], sum = 0.f;
+  unsigned masked = 0;
 #pragma unroll
   for (int q = 0; q < PER; q++) {
     e[q] = expf(l[q] - top);
     sum += e[q];
+    masked |= (l[q] == -INFINITY ? 1u : 0u) << q;
   }
+  asm("" : "+v"(masked));                      // (a bit a logit, or the logits themselves are kept up to the end: 75 registers, 63 so)
   const float mine = id >= 0 ? expf(chosen - top) : 0.f;
   sum = lanes_sum<LANES>(p.renormalize ? mine : sum);
   const float w = mine / sum;
@@ -424,7 +428,7 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
     if (real && i + q * LANES < p.E) {
       float v = d[q];
       if (!p.renormalize) v = e[q] / sum * (v - mean);
-      p.dlogits[t * p.E + i + q * LANES] = none ? 0.f : v;
+      p.dlogits[t * p.E + i + q * LANES] = none || (masked >> q & 1) ? 0.f : v;
     }
 }
 

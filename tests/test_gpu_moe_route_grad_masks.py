@@ -1,0 +1,42 @@
+"""tl_moe_route_grad: every number of lanes and of logits a lane, masked choices whose gradient is not finite."""
+import numpy as np
+import pytest
+
+from oracle import moe_train as o
+from tests.moe_train_util import choose, within
+from tests.test_gpu_moe_route_grad import bound, grad
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+# kernel (lanes of a token, logits of a lane), tokens, experts, choices
+SHAPES = [("16 1", 33, 9, 3), ("16 2", 40, 32, 5), ("16 4", 65, 33, 8), ("16 8", 20, 128, 16), ("16 16", 50, 200, 7), ("32 1", 9, 32, 17), ("32 2", 70, 50, 20),
+          ("32 4", 41, 100, 32), ("32 8", 37, 200, 17)]
+
+
+def normal(T, E, k):
+    rng = np.random.default_rng(T + E + k)
+    f32 = lambda *s: rng.normal(size=s).astype(np.float32).astype(np.float64)
+    return f32(T, E) * 2, choose(rng, T, E, k), f32(T, k)
+
+
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("kernel,T,E,k", SHAPES, ids=str)
+def test_gradient(kernel, T, E, k, renormalize):
+    logits, ids, dw = normal(T, E, k)
+    within(grad(logits, ids, dw, renormalize), o.route_grad(logits, ids, dw, renormalize), bound(logits, ids, dw, renormalize), "dlogits")
+
+
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("kernel,T,E,k", SHAPES, ids=str)
+def test_what_a_masked_choice_is_given_does_not_count(kernel, T, E, k, renormalize):
+    """Logits of -inf, chosen: no weight and no gradient, whatever their dtopk_w."""
+    logits, ids, dw = normal(T, E, k)
+    given = dw.copy()
+    for t in range(T):
+        for j, bad in zip(range(t % 3 % k), (NAN, INF)):         # none, one or two of the choices
+            logits[t, ids[t, j]] = -np.inf
+            dw[t, j], given[t, j] = 0, bad if t % 2 else -bad
+    got = grad(logits, ids, given, renormalize)
+    within(got, o.route_grad(logits, ids, dw, renormalize), bound(logits, ids, dw, renormalize), "dlogits")
+    assert not got[~np.isfinite(logits)].any()

@@ -1,11 +1,10 @@
 """Every variant of the row kernels, those that stream past the caches among them: matrices of more than 32, 128 and 256 MiB, against
 plain indexing on the device in 64 bits.  That each case takes the variant it names is tested without a GPU (test_moe_train_choice.py)."""
-import numpy as np
 import pytest
 import torch
 
 import paper_2503_20313_amd as tl
-from tests.moe_train_util import BF16, F32, HALF16, HALF32, I32, Lib
+from tests.moe_train_util import BF16, HALF16, HALF32, I32, Lib
 
 NAN = float("nan")
 F64 = torch.float64

@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from tests import test_gpu_moe_products_kernels as products
+from tests import test_gpu_moe_route_grad_masks as route
 from tests import test_gpu_moe_rows_streaming as rows
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -48,3 +49,9 @@ def test_rows(kernels_of):
     loads = ("cached", "stream")
     assert set(got) == ({f"dispatch cached {s}" for s in loads} | {f"{op} {l} cached" for op in ("dispatch_grad", "combine") for l in loads} |
                         {f"combine_grad {w} {s}" for w in (1, 4) for s in ("cached cached", "cached stream", "stream stream")})
+
+
+def test_routing_weights(kernels_of):
+    got = kernels_of([("route_grad", E, k) for _, _, E, k in route.SHAPES])
+    assert got == ["route_grad " + s[0] for s in route.SHAPES]
+    assert set(got) == {f"route_grad {lanes} {per}" for lanes in (16, 32) for per in (1, 2, 4, 8, 16) if lanes * per <= 256}
