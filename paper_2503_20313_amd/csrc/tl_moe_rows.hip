@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
     for (int q = 1; q < PER; q++) top = fmaxf(top, l[q]);
     top = lanes_max<LANES>(top);
   }
-  const bool none = top == -INFINITY;          // no finite logit: no weights, no gradient
+  if (top == -INFINITY) top = 0.f;             // (nothing but masks, and NaN, which a maximum passes over: exponentials of 0 and NaN)
   float e[PER], sum = 0.f;
   unsigned masked = 0;
 #pragma unroll
@@ -410,6 +410,7 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
   asm("" : "+v"(masked));                      // (a bit a logit, or the logits themselves are kept up to the end: 75 registers, 63 so)
   const float mine = id >= 0 ? expf(chosen - top) : 0.f;
   sum = lanes_sum<LANES>(p.renormalize ? mine : sum);
+  const bool none = sum == 0.f;                // masked logits alone: no weights, no gradient
   const float w = mine / sum;
   const float mean = lanes_sum<LANES>(id >= 0 ? w * g : 0.f);
   const float a = p.renormalize ? w * (g - mean) : g;     // what choice i adds to its expert

@@ -1,4 +1,4 @@
-"""tl_moe_route_grad: every number of lanes and of logits a lane, masked choices whose gradient is not finite."""
+"""tl_moe_route_grad: every number of lanes and of logits a lane, masked choices whose gradient is not finite, logits that are not numbers."""
 import numpy as np
 import pytest
 
@@ -40,3 +40,25 @@ def test_what_a_masked_choice_is_given_does_not_count(kernel, T, E, k, renormali
     got = grad(logits, ids, given, renormalize)
     within(got, o.route_grad(logits, ids, dw, renormalize), bound(logits, ids, dw, renormalize), "dlogits")
     assert not got[~np.isfinite(logits)].any()
+
+
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("kernel,T,E,k", SHAPES, ids=str)
+def test_logits_that_are_not_numbers_are_not_masks(kernel, T, E, k, renormalize):
+    """A token with such a logit, alone, among finite ones or beside masked ones, has no weights that are numbers: so are the gradients of all
+    its logits, of the chosen ones with renormalize, but those of -inf.  The other tokens are as they would be."""
+    logits, ids, dw = normal(T, E, k)
+    clean = o.route_grad(logits, ids, dw, renormalize)
+    size = bound(logits, ids, dw, renormalize)
+    first = ids[:, 0]
+    logits[0] = NAN
+    logits[1, first[1]] = NAN
+    logits[2] = -np.inf
+    logits[2, first[2]] = NAN
+    got = grad(logits, ids, dw, renormalize)
+    for t in range(3):
+        hit = np.zeros(E, bool)
+        hit[ids[t] if renormalize else slice(None)] = True
+        hit &= logits[t] != -np.inf
+        assert np.isnan(got[t, hit]).all() and not got[t, ~hit].any(), t
+    within(got[3:], clean[3:], size[3:], "dlogits")
