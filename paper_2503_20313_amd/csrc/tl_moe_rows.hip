@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kSortThreads) moe_count_kernel(const SortParam
   if (tid < p.E) p.hist[(long)blockIdx.x * p.E + tid] = s_cnt[tid];
 }
 
-template <int RPT, bool ONE>       // ONE: this is the only chunk
+template <int RPT, bool ONE>       // ONE: this is the only chunk (RPT is 1 then)
 __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortParams p) {
   __shared__ int s_cnt[kSortWaves][kMaxSortExperts];
   __shared__ int s_sum[2][kSortThreads];     // rows of an expert in the chunks before this one, and in all: by groups of chunks
@@ -507,9 +507,13 @@ int tl_moe_sort(tl_ctx* ctx, const int* topk_ids, int T, int topk, int first_exp
   p.hist = (int*)workspace;
   p.chunks = sort_chunks(p.n);
   hipStream_t s = (hipStream_t)stream;
+  if (p.chunks == 1) {     // (of a row a thread: more are taken where that would make more than 128 chunks)
+    hipLaunchKernelGGL((moe_place_kernel<1, true>), dim3(1), dim3(kSortThreads), 0, s, p);
+    TL_HIP(hipGetLastError());
+    return TL_OK;
+  }
   auto go = [&](auto rpt_c) {
     constexpr int RPT = decltype(rpt_c)::value;
-    if (p.chunks == 1) { hipLaunchKernelGGL((moe_place_kernel<RPT, true>), dim3(1), dim3(kSortThreads), 0, s, p); return; }
     hipLaunchKernelGGL(moe_count_kernel<RPT>, dim3(p.chunks), dim3(kSortThreads), 0, s, p);
     hipLaunchKernelGGL((moe_place_kernel<RPT, false>), dim3(p.chunks), dim3(kSortThreads), 0, s, p);
   };

@@ -8,6 +8,7 @@ import pytest
 from tests import test_gpu_moe_products_kernels as products
 from tests import test_gpu_moe_route_grad_masks as route
 from tests import test_gpu_moe_rows_streaming as rows
+from tests import test_gpu_moe_sort as sort
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PKG = os.path.join(ROOT, "paper_2503_20313_amd")
@@ -55,3 +56,8 @@ def test_routing_weights(kernels_of):
     got = kernels_of([("route_grad", E, k) for _, _, E, k in route.SHAPES])
     assert got == ["route_grad " + s[0] for s in route.SHAPES]
     assert set(got) == {f"route_grad {lanes} {per}" for lanes in (16, 32) for per in (1, 2, 4, 8, 16) if lanes * per <= 256}
+
+
+def test_sort(kernels_of):
+    cases = next(m.args[1] for m in sort.test_sort.pytestmark if m.name == "parametrize" and m.args[0] == "T,k,E")
+    assert set(kernels_of([("sort", T, k, E) for T, k, E in cases])) == {"sort one chunk 1"} | {f"sort chunks {r}" for r in (1, 2, 4, 8)}
