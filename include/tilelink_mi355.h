@@ -433,7 +433,8 @@ int tl_moe_combine_grad(tl_ctx* ctx, const void* dout /*dev*/, const void* ys /*
  *   gate_logits dev fp32 [T, E], topk_ids dev int[T, topk], dtopk_w dev fp32 [T, topk];  dlogits dev fp32 [T, E] (written; may be gate_logits)
  * An id outside [0, E) is no choice: it has no weight, its dtopk_w is not read.  A logit of -inf is a mask: its gradient is zero, and where it is
  * chosen its dtopk_w counts for nothing, whatever it holds.  A token whose logits (with renormalize: whose chosen ones) are all -inf has no weights, and
- * gradients of zero; one with a NaN among them has a gradient of NaN for each of them that is no mask.  topk <= E <= 256, T <= 2^24. */
+ * gradients of zero; one with a NaN among them has a gradient of NaN for each of them but masks (and logits more than 103 below the largest, whose
+ * exponential is zero in fp32).  topk <= E <= 256, T <= 2^24. */
 int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits /*dev*/, const int* topk_ids /*dev*/, const float* dtopk_w /*dev*/, int T, int E, int topk,
                       int renormalize, float* dlogits /*dev*/, void* stream);
 

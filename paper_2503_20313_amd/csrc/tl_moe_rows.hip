@@ -389,7 +389,6 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
     const float v = __shfl(l[q], lane0 + (id < 0 ? 0 : id % LANES));
     if (id >= 0 && id / LANES == q) chosen = v;
   }
-  if (chosen == -INFINITY) g = 0.f;            // (no weight: 0 times whatever it was given, infinities and NaN too)
   float top;
   if (p.renormalize) top = lanes_max<LANES>(chosen);
   else {
@@ -400,20 +399,17 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
   }
   if (top == -INFINITY) top = 0.f;             // (nothing but masks, and NaN, which a maximum passes over: exponentials of 0 and NaN)
   float e[PER], sum = 0.f;
-  unsigned masked = 0;
 #pragma unroll
   for (int q = 0; q < PER; q++) {
     e[q] = expf(l[q] - top);
     sum += e[q];
-    masked |= (l[q] == -INFINITY ? 1u : 0u) << q;
   }
-  asm("" : "+v"(masked));                      // (a bit a logit, or the logits themselves are kept up to the end: 75 registers, 63 so)
   const float mine = id >= 0 ? expf(chosen - top) : 0.f;
   sum = lanes_sum<LANES>(p.renormalize ? mine : sum);
-  const bool none = sum == 0.f;                // masked logits alone: no weights, no gradient
   const float w = mine / sum;
-  const float mean = lanes_sum<LANES>(id >= 0 ? w * g : 0.f);
-  const float a = p.renormalize ? w * (g - mean) : g;     // what choice i adds to its expert
+  const float mean = lanes_sum<LANES>(chosen == -INFINITY ? 0.f : w * g);
+  float a = p.renormalize ? w * (g - mean) : g;           // what choice i adds to its expert
+  if (chosen == -INFINITY) a = 0.f;
   float d[PER];
 #pragma unroll
   for (int q = 0; q < PER; q++) d[q] = 0.f;
@@ -428,8 +424,8 @@ __global__ void __launch_bounds__(256) moe_route_grad_kernel(const RouteGradPara
   for (int q = 0; q < PER; q++)
     if (real && i + q * LANES < p.E) {
       float v = d[q];
-      if (!p.renormalize) v = e[q] / sum * (v - mean);
-      p.dlogits[t * p.E + i + q * LANES] = none || (masked >> q & 1) ? 0.f : v;
+      if (!p.renormalize) v = e[q] == 0.f ? 0.f : e[q] / sum * (v - mean);      // (zero for a mask, whatever the others are)
+      p.dlogits[t * p.E + i + q * LANES] = v;
     }
 }
 
