@@ -389,6 +389,8 @@ int tl_moe_gemm_scatter_rs(tl_ctx* ctx, const void* x2, const void* w2, const in
  *   tl_moe_gemm, _grad_x, _grad_w                every expert's product on its rows, and the gradients of rows and weights
  *   tl_moe_combine, tl_moe_combine_grad          rows back to their tokens with their weights, and the gradients of rows and weights
  *   tl_moe_route_grad                            the gradient of the gate's logits from that of the routing weights
+ * What stands between two products (an activation and its gradient) is the caller's.  tl_moe_route chooses up to 8 of up to 64 experts; these calls take the
+ * ids of any router.
  * Matrices are bf16, products and sums fp32, every result rounded once.  No call reads a number of rows on the host: a step can be
  * captured into a HIP graph and replayed with another routing.  All results are the same from run to run.
  *
@@ -448,6 +450,7 @@ int tl_moe_route_grad(tl_ctx* ctx, const float* gate_logits /*dev*/, const int* 
  * Rows that are no expert's are left as they were.  An expert without rows has dW_e = 0 (+ dw_add[e]).
  *   workspace dev, 128-byte aligned, bytes from tl_moe_gemm_query (host call; `way` one of TL_MOE_*): needs no preparation, nothing of it is kept,
  *     so that calls and graphs that follow each other may share it, whatever their sizes.  One call at a time.
+ * The kernel is chosen by max_rows, which may be more than there are; the closer, the better it fits.
  * K % 8 == 0, N % 8 == 0, up to 2^20; E <= 256; for dW E*ceil(K/128)*ceil(N/128) < 2^22. */
 enum { TL_MOE_FORWARD = 0, TL_MOE_GRAD_X = 1, TL_MOE_GRAD_W = 2 };
 int tl_moe_gemm_query(const tl_ctx* ctx, int way, int max_rows, int K, int N, int E, size_t* ws_bytes /*host*/);

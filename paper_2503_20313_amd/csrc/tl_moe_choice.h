@@ -77,7 +77,9 @@ constexpr int few_columns(bool grad_x, bool wide) { return (grad_x ? 32 : 64) * 
 // tiles have the memory and the chip's power to themselves; a cut one its part; the join of large tiles' parts 35, of small ones' 10.  Cut only
 // sums beyond 2048: of the shorter ones as many lose by the join's launch, 3 us of 100, as gain.  8 experts of 4096 x 2048 with 2048 rows each
 // 270 -> 243 us, dX of 8 of 4096 x 14336 with 512 rows 696 -> 488, 2 of 4096 x 4096 with 2048 150 -> 122.  Over 460 calls of 96 to 4096 rows an
-// expert the choice takes 2 % more than the best of the four.
+// expert the choice takes 2 % more than the best of the four -- in buffers of as many rows as there are.  With room for two and four times as many the choice is
+// that of more rows: mostly the same time, up to 26 us more (Y of 1024 rows of 32 experts of 4096 x 1792 82, 95 and 108 us, dX of 4096 rows of 8 of
+// 1024 x 2816 42, 67 and 67).
 constexpr int kCutSum = 2048;
 struct ProductShape {
   int tile;                // 0: the few-row kernel

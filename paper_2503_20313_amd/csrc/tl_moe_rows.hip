@@ -343,8 +343,9 @@ __global__ void __launch_bounds__(256) moe_combine_grad_kernel(const RowsParams 
 //   w_j = p_{e_j}:                     dl_i = p_i (sum_{j: e_j = i} dw_j - sum_k p_{e_k} dw_k)
 //   w_j = p_{e_j} / sum_k p_{e_k}:     dl_i = sum_{j: e_j = i} w_j (dw_j - sum_k w_k dw_k),  w the softmax over the chosen logits
 // LANES lanes hold a token's logits, PER each, and one choice each: as few as hold the choices, for the reductions over them are what the
-// time goes into (16384 tokens, 64 experts, top-8: 9.7 us with 64 lanes of one logit, 5.5 with 16 of four).  Everything is fp32: the exponentials are of differences to the
-// largest logit, the sums of at most 256 terms.
+// time goes into (16384 tokens, 64 experts, top-8: 9.7 us with 64 lanes of one logit, 5.8 with 16 of four).  Everything is fp32: the exponentials are of differences to the
+// largest logit, the sums of at most 256 terms.  Masks (-inf) are left out of the sums and products,
+// for 0 times an infinity is NaN: a masked choice's dw reaches nobody, and what the others are does not reach a masked logit.
 // ======================================================================================
 struct RouteGradParams {
   const float *logits, *dw;
