@@ -1,9 +1,11 @@
 """tl_moe_route_grad: every number of lanes and of logits a lane, masked choices whose gradient is not finite, logits that are not numbers."""
 import numpy as np
 import pytest
+import torch
 
+import paper_2503_20313_amd as tl
 from oracle import moe_train as o
-from tests.moe_train_util import choose, within
+from tests.moe_train_util import Lib, choose, within
 from tests.test_gpu_moe_route_grad import bound, grad
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +64,19 @@ def test_logits_that_are_not_numbers_are_not_masks(kernel, T, E, k, renormalize)
         hit &= logits[t] != -np.inf
         assert np.isnan(got[t, hit]).all() and not got[t, ~hit].any(), t
     within(got[3:], clean[3:], size[3:], "dlogits")
+
+
+def test_logits_beyond_32_bits():
+    """2^24 tokens of 256 experts, 16 GiB, in place: equal logits, so that every weight is 2^-8 and all results are exact."""
+    T, E = 1 << 24, 256
+    logits, ids, dw = torch.zeros(T, E, device="cuda"), torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.zeros(T, 1, device="cuda")
+    tokens = [0, 1 << 22, (1 << 23) + 1, T - 1]
+    chosen = torch.tensor([255, 3, 0, 129], device="cuda")
+    ids[tokens, 0], dw[tokens, 0] = chosen.int(), 65536.0
+    with Lib() as ctx:
+        tl.tl_moe_route_grad(ctx, logits, ids, dw, T, E, 1, 0, logits)
+        ref = torch.full((len(tokens), E), -1.0, device="cuda")
+        ref[torch.arange(len(tokens)), chosen] = 255.0
+        assert torch.equal(logits[tokens], ref)
+        logits[tokens] = 0
+        assert not logits.any().item()

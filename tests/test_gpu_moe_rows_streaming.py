@@ -113,3 +113,36 @@ def test_combine_grad(variant, T, H, k, rows, in_place):
         terms = g * c.rows_of(kept, j)
         within(dw[:, j], terms.sum(1), H * HALF32 * terms.abs().sum(1), "dw")
         assert not dw[~part, j].any().item()
+
+
+@pytest.mark.gpu
+def test_lists_beyond_32_bits():
+    """As many choices as there can be, row_pos and weights of more than 4 GiB each: the first, a middle and the last tokens have rows."""
+    T, H, k, rows = (1 << 26) - 1, 8, 32, 64
+    pos = torch.full((T, k), -1, dtype=I32, device="cuda")
+    tokens = [0, 1 << 25, (1 << 26) - 3, T - 1]
+    at = torch.randperm(rows, device="cuda", generator=torch.Generator("cuda").manual_seed(0))[:len(tokens) * 2].reshape(-1, 2)
+    pos[tokens, 3], pos[tokens, k - 1] = at[:, 0].to(I32), at[:, 1].to(I32)
+    x = torch.ones(T, H, dtype=BF16, device="cuda")
+    x[tokens] = torch.arange(1, len(tokens) * H + 1, device="cuda").reshape(-1, H).to(BF16)
+    xs, dx = torch.full((rows, H), 7.0, dtype=BF16, device="cuda"), torch.full_like(x, NAN)
+    with Lib() as ctx:
+        tl.tl_moe_dispatch(ctx, x, pos, T, H, k, rows, xs)
+        ref = torch.full_like(xs, 7.0)
+        ref[at[:, 0]], ref[at[:, 1]] = x[tokens], x[tokens]
+        assert torch.equal(xs, ref)
+        tl.tl_moe_dispatch_grad(ctx, xs, pos, T, H, k, rows, dx)
+        has = torch.zeros(T, dtype=torch.bool, device="cuda")
+        has[tokens] = True
+        assert torch.equal(dx[tokens], 2 * x[tokens]) and not dx[~has].any().item()
+        w = torch.full((T, k), NAN, device="cuda")
+        w[tokens, 3], w[tokens, k - 1] = 2.0, 0.5
+        tl.tl_moe_combine(ctx, xs, w, pos, T, H, k, rows, x, dx)
+        assert torch.equal(dx[~has], x[~has]) and torch.equal(dx[tokens], (x[tokens] * 3.5).to(BF16))
+        dw = torch.full((T, k), NAN, device="cuda")
+        tl.tl_moe_combine_grad(ctx, x, xs, w, pos, T, H, k, rows, xs, dw)
+        size = (x[tokens].float() ** 2).sum(1)
+        assert torch.equal(xs[at[:, 0]], 2 * x[tokens]) and torch.equal(xs[at[:, 1]], 0.5 * x[tokens])
+        assert torch.equal(dw[tokens, 3], size) and torch.equal(dw[tokens, k - 1], size)
+        dw[tokens] = 0
+        assert not dw.any().item()
